@@ -71,7 +71,9 @@ typedef enum {
     MOE_ACT_GELU_ERF = 0, /* 0.5 v (1 + erf(v / sqrt 2)) */
     MOE_ACT_GELU_TANH = 1,
     MOE_ACT_RELU = 2,     /* the activation the paper names in Sec. 2.1 */
-    MOE_ACT_IDENTITY = 3
+    MOE_ACT_IDENTITY = 3,
+    MOE_ACT_SILU = 4      /* v / (1 + exp(-v)): the gated block only (moe_gated.h); the plain expert FFN
+                             and the calls that contain it refuse it */
 } moe_act;
 
 /* Shape of one layer.  T tokens, E experts (1..64), k experts per token

@@ -7,6 +7,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include "moe.h"
+
 namespace moe {
 
 // GeLU(v) = max(v, 0) - a Phi(-a) with a = |v|, and Phi(-a) = 2^P(a), P a polynomial of degree 5
@@ -53,6 +55,48 @@ __device__ __forceinline__ float gelu_erf_derivative_fast(float v)
 __device__ __forceinline__ float half_one_plus_tanh(float v)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * (-2.3022082f - 0.10294324f * v * v)));
+}
+
+// 1 / (1 + e^-v): an exponential and a reciprocal, a few units of the last place of fp32.  (0 for v far below zero, where
+// the exponential is infinite; NaN stays NaN.)
+__device__ __forceinline__ float sigmoid_fast(float v)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * v));
+}
+
+// The gated block's activation of a 16-bit layer, and with its derivative (the derivative's name for the sums: s for the
+// logistic function of silu, s = (1 + tanh u) / 2 for the tanh form).
+template <int ACT>
+__device__ __forceinline__ float gate_value(float v)
+{
+    if constexpr (ACT == MOE_ACT_SILU) return v * sigmoid_fast(v);
+    else if constexpr (ACT == MOE_ACT_GELU_ERF) return gelu_erf_fast(v);
+    else if constexpr (ACT == MOE_ACT_GELU_TANH) return v * half_one_plus_tanh(v);
+    else if constexpr (ACT == MOE_ACT_RELU) return __builtin_elementwise_maximum(v, 0.0f);
+    else return v;
+}
+template <int ACT>
+__device__ __forceinline__ void gate_value_and_slope(float v, float &value, float &slope)
+{
+    if constexpr (ACT == MOE_ACT_SILU) {
+        const float s = sigmoid_fast(v);
+        value = v * s;
+        slope = __builtin_fmaf(value, 1.0f - s, s);
+    } else if constexpr (ACT == MOE_ACT_GELU_ERF) {
+        value = gelu_erf_fast(v);
+        slope = gelu_erf_derivative_fast(v);
+    } else if constexpr (ACT == MOE_ACT_GELU_TANH) {
+        constexpr float c = 0.7978845608028654f, a = 0.044715f;
+        const float s = half_one_plus_tanh(v);
+        value = v * s;
+        slope = __builtin_fmaf(2.0f * value * (1.0f - s), c * (1.0f + 3.0f * a * v * v), s);
+    } else if constexpr (ACT == MOE_ACT_RELU) {
+        value = __builtin_elementwise_maximum(v, 0.0f);
+        slope = v > 0.0f ? 1.0f : 0.0f;
+    } else {
+        value = v;
+        slope = 1.0f;
+    }
 }
 
 }  // namespace moe

@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "gated.h"
 #include "moe_train.h"
 
 namespace moe {
@@ -105,7 +106,7 @@ bool check_shape(const moe_shape *s)
         set_error("dtype %d is neither MOE_F32 nor MOE_BF16", s->dtype);
         return false;
     }
-    if (s->act < MOE_ACT_GELU_ERF || s->act > MOE_ACT_IDENTITY) {
+    if (s->act < MOE_ACT_GELU_ERF || s->act > MOE_ACT_SILU) {
         set_error("unknown activation %d", s->act);
         return false;
     }
@@ -181,6 +182,17 @@ moe_status check_common(const moe_shape *s)
 {
     if (!check_shape(s)) return MOE_EINVAL;
     return check_supported(*s);
+}
+
+// the calls whose experts are two plain products
+moe_status check_plain_expert(const moe_shape *s)
+{
+    MOE_TRY(check_common(s));
+    if (s->act == MOE_ACT_SILU) {
+        set_error("MOE_ACT_SILU is an activation of the gated block (moe_gated.h)");
+        return MOE_EUNSUPPORTED;
+    }
+    return MOE_OK;
 }
 
 moe_status check_bias(const moe_shape &s, const float *gate_bias, int32_t stride)
@@ -263,6 +275,8 @@ moe_status scratch_address(void **out)
 }
 
 }  // namespace
+
+moe_status check_layer_shape(const moe_shape *s) { return check_common(s); }
 
 // The expert FFN of a chunked layer runs once per GROUP of consecutive chunks.  A launch
 // reads every expert's two weight matrices from HBM once whatever its row count, and is bound
@@ -517,7 +531,7 @@ moe_status moe_expert_ffn(const moe_shape *s, const void *xe, const int32_t *off
                           const void *W1p, const float *b1, const void *W2p, const float *b2,
                           void *ye, void *workspace, void *stream)
 {
-    MOE_TRY(check_common(s));
+    MOE_TRY(check_plain_expert(s));
     MOE_REQUIRE_PTR(xe);
     MOE_REQUIRE_PTR(offsets);
     MOE_REQUIRE_PTR(W1p);
@@ -560,7 +574,7 @@ moe_status layer_forward(const moe_shape *s, int32_t n_chunks, const void *x,
                          int32_t *src_of, void *xe, void *ye, void *pre, void *hid, float *y,
                          void *y_act, void *workspace, void *stream)
 {
-    MOE_TRY(check_common(s));
+    MOE_TRY(check_plain_expert(s));
     if (n_chunks < 1 || n_chunks > kMaxChunks) {
         set_error("n_chunks must be in 1..%d, got %d", kMaxChunks, n_chunks);
         return MOE_EINVAL;

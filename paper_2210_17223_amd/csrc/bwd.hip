@@ -16,6 +16,7 @@
 // work list; a weight-gradient GEMM contracts over one expert's rows.
 #include "activation.h"
 #include "common.h"
+#include "gated.h"
 #include "moe_train.h"
 
 #include <algorithm>
@@ -307,7 +308,9 @@ __global__ __launch_bounds__(256, BM + BN == 256 && !DEEP ? 2 : 1) void bwd_gemm
     constexpr bool F16 = false;
     const int32_t *const row_src = nullptr;      // packed rows
     constexpr int row_div = 1, a_rows = 0;
-    constexpr bool TILE_IN = EPI == 2;
+    constexpr bool TILE_IN = EPI == 2, TILE_PAIR = false;
+    constexpr int pair_at = 0;
+    const int tile_pitch = N;
     const uint16_t *const tile_in = reinterpret_cast<const uint16_t *>(Pbuf);
 #include "gemm_w4_body.inc"
 
@@ -462,9 +465,10 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t w)
     return f32x2_to_bf16x2(f16_half_to_f32<0>(w), f16_half_to_f32<1>(w));
 }
 
-template <bool AF16>
+// TOut: fp32, or uint16_t for sums rounded to bf16.
+template <bool AF16, typename TOut = float>
 __global__ __launch_bounds__(256, 2) void wgrad_gemm_kernel(
-    const uint16_t *__restrict__ A, const uint16_t *__restrict__ B, float *__restrict__ C,
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ B, TOut *__restrict__ C,
     const int32_t *__restrict__ offsets, int E, int M, int N, int tiles_m, int tiles_n)
 {
     constexpr int WM = 2, TM = 2, TN = 2, NT = 256;     // 2 x 2 wavefronts of 64 x 64
@@ -628,7 +632,7 @@ __global__ __launch_bounds__(256, 2) void wgrad_gemm_kernel(
 
     // acc[i][j][4*g + c]: column n0 + (wn*TN + i)*32 + 8*g + 4*(lane/32) + c,
     //                     row m0 + (wm*TM + j)*32 + lane%32
-    float *Ce = C + static_cast<size_t>(expert) * M * N;
+    TOut *Ce = C + static_cast<size_t>(expert) * M * N;
     const int fr = lane & 31;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
@@ -640,9 +644,14 @@ __global__ __launch_bounds__(256, 2) void wgrad_gemm_kernel(
             for (int g = 0; g < 4; ++g) {
                 const int n = n0 + (wn * TN + i) * 32 + 8 * g + 4 * (lane >> 5);
                 if (n >= N) continue;
-                *reinterpret_cast<float4 *>(Ce + static_cast<size_t>(m) * N + n) =
-                    make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                acc[i][j][4 * g + 3]);
+                if constexpr (std::is_same_v<TOut, float>) {
+                    *reinterpret_cast<float4 *>(Ce + static_cast<size_t>(m) * N + n) =
+                        make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                                    acc[i][j][4 * g + 3]);
+                } else {
+                    const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                    store_bf16x4(Ce + static_cast<size_t>(m) * N + n, v);
+                }
             }
         }
     }
@@ -674,9 +683,11 @@ __global__ __launch_bounds__(256, 2) void wgrad_gemm_kernel(
 // Blocks that start one after the other over the length of a tile, so that they do not store all at once: 2 %
 // less for dW1, nothing for dW2.  Tiles in squares of 4 x 4: dW1 2455 -> 2325 with one block per tile.
 // All of that with the tiles in 256 shares; in shares that give the unit back (kRunStages) 2417 / 2213 where those take 2379 / 2106.
-template <bool AF16>
+// TOut: fp32 (M and N multiples of 256), or uint16_t for sums rounded to bf16, whose tiles may end past the matrix: their
+// columns there multiply what lies behind the operands' rows, and are not stored.
+template <bool AF16, typename TOut = float>
 __global__ __launch_bounds__(256, 1) void wgrad_w4_kernel(
-    const uint16_t *__restrict__ A, const uint16_t *__restrict__ B, float *__restrict__ C,
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ B, TOut *__restrict__ C,
     const int32_t *__restrict__ offsets, int E, int M, int N, int tiles_m, int tiles_n, int share)
 {
     constexpr int TM = 8, TN = 8, HALF = 16384, STEP = 2 * HALF, RING = 5;
@@ -830,12 +841,13 @@ __global__ __launch_bounds__(256, 1) void wgrad_w4_kernel(
     };
     // In front of step p of a tile: its fragments have been read by every wavefront, so that its place is
     // free, and the step behind it is there.  A tile begins with its first three steps landed, the fourth on its way
-    // and, younger than that, up to 64 stores of the tile before.
+    // and, younger than that, up to 64 stores of the tile before (32 of bf16 values), and then three steps of loads.
+    constexpr int YOUNGER = std::is_same_v<TOut, float> ? 63 : 32 + 24;
     auto turn = [&](int p) {
         MOE_SB();
         __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0), in a form that the compiler's own counting sees
         if (p >= 3) MOE_VMCNT(24);               // three steps of loads may be on their way behind that one
-        else MOE_VMCNT(63);
+        else MOE_VMCNT(YOUNGER);
         MOE_BAR();
     };
     using S0 = integral_constant<int, 0>;
@@ -882,35 +894,71 @@ __global__ __launch_bounds__(256, 1) void wgrad_w4_kernel(
         // wavefront's accesses in order: nothing is waited for in between.)
         MOE_MATRIX_RESULTS();
         MOE_VMCNT(8);
-        float *out = C + (static_cast<size_t>(t.expert) * M + t.m0 + wm * 128) * N + t.n0 + wn * 128;
-        const __amdgpu_buffer_rsrc_t rsc = __builtin_amdgcn_make_buffer_rsrc(out, 0, 128u * static_cast<unsigned>(N) * 4u, 0x00020000);
         char *const patch = lds + at + wave * 8192;
-        const int out_lane = (lane >> 5) * N * 4 + (lane & 31) * 16;
-        u32x4 line[2][8];
-        auto through = [&](auto jc) {
-            constexpr int j = decltype(jc)::value;
+        if constexpr (std::is_same_v<TOut, float>) {
+            float *out = C + (static_cast<size_t>(t.expert) * M + t.m0 + wm * 128) * N + t.n0 + wn * 128;
+            const __amdgpu_buffer_rsrc_t rsc = __builtin_amdgcn_make_buffer_rsrc(out, 0, 128u * static_cast<unsigned>(N) * 4u, 0x00020000);
+            const int out_lane = (lane >> 5) * N * 4 + (lane & 31) * 16;
+            u32x4 line[2][8];
+            auto through = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
-                *reinterpret_cast<f32x4 *>(patch + fr * 512 + (((i * 4 + oct) ^ fr) << 4)) = acc[i][j];
+                for (int i = 0; i < TN; ++i)
+                    *reinterpret_cast<f32x4 *>(patch + fr * 512 + (((i * 4 + oct) ^ fr) << 4)) = acc[i][j];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int row = 2 * q + (lane >> 5);
-                line[j & 1][q] = *reinterpret_cast<const u32x4 *>(patch + row * 512 + (((lane & 31) ^ row) << 4));
-            }
-            MOE_SB();
-        };
-        auto leave = [&](auto jc) {
-            constexpr int j = decltype(jc)::value;
+                for (int q = 0; q < 8; ++q) {
+                    const int row = 2 * q + (lane >> 5);
+                    line[j & 1][q] = *reinterpret_cast<const u32x4 *>(patch + row * 512 + (((lane & 31) ^ row) << 4));
+                }
+                MOE_SB();
+            };
+            auto leave = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                __builtin_amdgcn_raw_buffer_store_b128(line[j & 1][q], rsc, out_lane, (j * 16 + 2 * q) * N * 4, 2);
-            MOE_SB();
-        };
-        static_for<TM>([&](auto jc) {
-            through(jc);
-            if constexpr (decltype(jc)::value > 0) leave(std::integral_constant<int, decltype(jc)::value - 1>{});
-        });
-        leave(std::integral_constant<int, TM - 1>{});
+                for (int q = 0; q < 8; ++q)
+                    __builtin_amdgcn_raw_buffer_store_b128(line[j & 1][q], rsc, out_lane, (j * 16 + 2 * q) * N * 4, 2);
+                MOE_SB();
+            };
+            static_for<TM>([&](auto jc) {
+                through(jc);
+                if constexpr (decltype(jc)::value > 0) leave(std::integral_constant<int, decltype(jc)::value - 1>{});
+            });
+            leave(std::integral_constant<int, TM - 1>{});
+        } else {
+            // the same with four rows of 128 16-bit values per instruction
+            const int row0 = t.m0 + wm * 128, col = t.n0 + wn * 128 + (lane & 15) * 8;
+            uint16_t *out = C + (static_cast<size_t>(t.expert) * M + row0) * N;
+            const __amdgpu_buffer_rsrc_t rsc = __builtin_amdgcn_make_buffer_rsrc(
+                out, 0, static_cast<unsigned>(min(max(M - row0, 0), 128)) * static_cast<unsigned>(N) * 2u, 0x00020000);
+            const int out_lane = col < N ? ((lane >> 4) * N + col) * 2 : 0x7ff00000, out_row = col < N ? N * 2 : 0;
+            u32x4 line[2][4];
+            auto through = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+#pragma unroll
+                for (int i = 0; i < TN; ++i) {
+                    const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    store_bf16x4(reinterpret_cast<uint16_t *>(patch + fr * 256 + (((i * 2 + (oct >> 1)) ^ fr) << 4) + (oct & 1) * 8), v);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int row = 4 * q + (lane >> 4);
+                    line[j & 1][q] = *reinterpret_cast<const u32x4 *>(patch + row * 256 + (((lane & 15) ^ row) << 4));
+                }
+                MOE_SB();
+            };
+            auto leave = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    __builtin_amdgcn_raw_buffer_store_b128(line[j & 1][q], rsc, out_lane + (j * 16 + 4 * q) * out_row, 0, 2);
+                MOE_SB();
+            };
+            static_for<TM>([&](auto jc) {
+                through(jc);
+                if constexpr (decltype(jc)::value > 0) leave(std::integral_constant<int, decltype(jc)::value - 1>{});
+            });
+            leave(std::integral_constant<int, TM - 1>{});
+        }
         at = next(at);
     }
     MOE_VMCNT(0);
@@ -1225,18 +1273,26 @@ bool wide_wgrad_tiles(int E, int M, int N, int64_t max_rows)
     return M % 256 == 0 && N % 256 == 0 && static_cast<int64_t>(E) * (M / 256) * (N / 256) >= 512 && span < (1ull << 31);
 }
 
+// The same for sums rounded to bf16, whose kernel takes any M and N.
+bool wide_wgrad_tiles_bf16(int E, int M, int N, int64_t max_rows)
+{
+    const uint64_t span = static_cast<uint64_t>(max_rows + 192) * static_cast<uint64_t>(std::max(M, N) + 256) * 2;
+    return static_cast<int64_t>(E) * ceil_div(M, 256) * ceil_div(N, 256) >= 256 && span < (1ull << 31);
+}
+
 // dW[e] [M][N] = A[rows of e]^T B[rows of e] from row-major operands
-template <bool AF16>
-void launch_wgrad(const uint16_t *A, const uint16_t *B, float *C, const int32_t *offsets, int E, int M,
+template <bool AF16, typename TOut>
+void launch_wgrad(const uint16_t *A, const uint16_t *B, TOut *C, const int32_t *offsets, int E, int M,
                   int N, int64_t max_rows, int stage, hipStream_t st)
 {
     hipEvent_t t0, t1;
-    if (wide_wgrad_tiles(E, M, N, max_rows)) {
+    constexpr bool F32 = std::is_same_v<TOut, float>;
+    if (F32 ? wide_wgrad_tiles(E, M, N, max_rows) : wide_wgrad_tiles_bf16(E, M, N, max_rows)) {
         constexpr size_t kLds4 = kW4Lds;
-        auto kern = wgrad_w4_kernel<AF16>;
+        auto kern = wgrad_w4_kernel<AF16, TOut>;
         static PerDeviceOnce once;
         once.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(kLds4));
-        const int tiles_m = M / 256, tiles_n = N / 256;
+        const int tiles_m = ceil_div(M, 256), tiles_n = ceil_div(N, 256);
         // (what leaves of a tile takes as long as five stages)
         const int share = std::max(1, kRunStages / (static_cast<int>((max_rows / E + 63) / 64) + 5));
         const int grid = kRunUnits * ceil_div((E * tiles_m * tiles_n + 7) / 8, kRunUnits / 8 * share);
@@ -1246,7 +1302,7 @@ void launch_wgrad(const uint16_t *A, const uint16_t *B, float *C, const int32_t 
         return;
     }
     constexpr size_t kLds = 2 * 2 * kBK * 128 * sizeof(uint16_t);
-    auto kern = wgrad_gemm_kernel<AF16>;
+    auto kern = wgrad_gemm_kernel<AF16, TOut>;
     static PerDeviceOnce once;
     once.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(kLds));
     const int tiles_m = (M + 127) / 128, tiles_n = (N + 127) / 128;
@@ -1546,6 +1602,14 @@ moe_status backward_t(const moe_shape &s, int n_chunks, const uint16_t *x, const
 }
 
 }  // namespace
+
+void launch_weight_grad_bf16(bool a_f16, const uint16_t *A, const uint16_t *B, uint16_t *C, const int32_t *offsets, int E,
+                             int M, int N, int64_t max_rows, int stage, hipStream_t st)
+{
+    if (a_f16) launch_wgrad<true>(A, B, C, offsets, E, M, N, max_rows, stage, st);
+    else launch_wgrad<false>(A, B, C, offsets, E, M, N, max_rows, stage, st);
+}
+
 }  // namespace moe
 
 using namespace moe;

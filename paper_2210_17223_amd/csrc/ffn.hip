@@ -16,6 +16,7 @@
 // fp32 layers: grouped_gemm_f32_kernel, on the fp32 matrix instruction.
 #include "activation.h"
 #include "common.h"
+#include "gated.h"
 #include <cstdio>
 
 #include <hip/hip_ext.h>
@@ -607,7 +608,8 @@ __device__ __forceinline__ void w4_gemm_tile(
     const int32_t *__restrict__ row_src, int row_div, int a_rows)
 {
     constexpr int BM = 128, BN = 128;
-    constexpr bool TILE_IN = false;
+    constexpr bool TILE_IN = false, TILE_PAIR = false;
+    constexpr int tile_pitch = 0, pair_at = 0;
     const uint16_t *const tile_in = nullptr;
 #include "gemm_w4_body.inc"
 
@@ -1005,6 +1007,26 @@ moe_status launch_ffn(const moe_shape &s, const void *xe, const void *W1p, const
         return MOE_EINVAL;
     }
 #undef MOE_FFN_CASE
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+// The second GEMM of a gated block
+moe_status launch_second_gemm(const moe_shape &s, const void *hidden, const void *W2p, void *ye, const GemmPlan &gp,
+                              const WorkItem *items, hipStream_t st)
+{
+    if (s.dtype == MOE_BF16) {
+        launch_mfma<true, _Float16, MOE_ACT_IDENTITY, false>(gp, static_cast<const uint16_t *>(hidden),
+                                                             static_cast<const uint16_t *>(W2p), nullptr,
+                                                             static_cast<_Float16 *>(ye), nullptr, items, s.d_model, s.d_ff,
+                                                             kStageGemm2, st);
+    } else {
+        auto kern = gp.bm == 64 ? grouped_gemm_f32_kernel<MOE_ACT_IDENTITY, 2, 2> : grouped_gemm_f32_kernel<MOE_ACT_IDENTITY, 1, 1>;
+        prof_begin(kStageGemm2, st);
+        hipLaunchKernelGGL(kern, dim3(gp.max_items), dim3(256), 0, st, static_cast<const float *>(hidden),
+                           static_cast<const float *>(W2p), nullptr, static_cast<float *>(ye), items, s.d_model, s.d_ff);
+        prof_end(kStageGemm2, st);
+    }
     MOE_TRY_HIP(hipGetLastError());
     return MOE_OK;
 }

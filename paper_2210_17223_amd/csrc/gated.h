@@ -1,0 +1,21 @@
+// What the gated block's translation units share (include/moe_gated.h).
+#pragma once
+
+#include "common.h"
+
+namespace moe {
+
+// Packed columns of the two first projections: sixteen of Wg and the same sixteen of Wu in turn.
+inline int gated_packed_columns(int d_ff) { return (d_ff + 15) / 16 * 32; }
+constexpr int kGatedBlock = 16;
+
+// ffn.hip: C = H W2p (fp16 operands, bf16 layers; fp32 else), one work list
+moe_status launch_second_gemm(const moe_shape &s, const void *hidden, const void *W2p, void *ye, const GemmPlan &gp,
+                              const WorkItem *items, hipStream_t st);
+// bwd.hip: dW[e] [M][N] = A[rows of e]^T B[rows of e] rounded to bf16; A holds fp16 values where a_f16
+void launch_weight_grad_bf16(bool a_f16, const uint16_t *A, const uint16_t *B, uint16_t *C, const int32_t *offsets, int E,
+                             int M, int N, int64_t max_rows, int stage, hipStream_t st);
+// api.hip: the checks that every call makes of its shape
+moe_status check_layer_shape(const moe_shape *s);
+
+}  // namespace moe

@@ -1,0 +1,946 @@
+// The gated feed-forward block on expert-major rows (include/moe_gated.h):
+//   H = act(xe Wg) * (xe Wu), ye = H W2, and its backward pass.
+//
+// Forward: one grouped GEMM over the packed first projections, in which sixteen columns of Wg and the same sixteen of Wu
+// take turns, so that a lane's accumulators hold a gate and the value that it gates: the activation and the product are
+// the epilogue, and G and U go to memory only where a backward pass will read them.  The second GEMM is the expert FFN's.
+// Backward: dH = dye W2^T with G and U brought into LDS behind its last stages, dG and dU its epilogue; dxe = [dG | dU] W13^T,
+// one product over 2 d_ff; the weight gradients are the expert FFN's kernels, rounded to bf16.
+// The loops are the expert FFN's: tiles of 256 columns on gemm_w4_run.h's, 128 x 128 on gemm_w4_body.inc's, decode steps
+// straight from global memory.
+#include "activation.h"
+#include "gated.h"
+#include "moe_gated.h"
+
+#include <algorithm>
+
+#include <hip/hip_ext.h>
+
+#include <type_traits>
+
+namespace moe {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+
+#include "gemm_w4.h"
+#include "gemm_w4_run.h"
+
+__device__ __forceinline__ void store_f16x4(char *p, const float (&v)[4])
+{
+    f16x4 h;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(v[c]);
+    *reinterpret_cast<f16x4 *>(p) = h;
+}
+__device__ __forceinline__ void store_bf16x4(char *p, const float (&v)[4])
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    u32x2 o;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        bf16x2 b;
+        b[0] = static_cast<__bf16>(v[2 * c]);
+        b[1] = static_cast<__bf16>(v[2 * c + 1]);
+        o[c] = __builtin_bit_cast(uint32_t, b);
+    }
+    *reinterpret_cast<u32x2 *>(p) = o;
+}
+
+// ---------------------------------------------------------------- first projections, tiles of 256 packed columns
+// R of a wavefront's rows, from `r` on, as they lie in the patch's rows 16 part .. (W4Place): PIECES 16-byte pieces of 8
+// columns each, to columns col0 + 8 piece of `out`; of 16 pieces the last eight go pair_at columns further on.
+template <int BM, int R, int PIECES>
+__device__ __forceinline__ void leave_gated(const W4Place<BM> &place, uint16_t *out, int pitch, int pair_at, int col0, int h,
+                                            int row0, int row1, int part)
+{
+    constexpr int ROWS = 64 / PIECES;
+    // (a row past the tile's or a column past h lies past the resource)
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        out + static_cast<size_t>(row0) * pitch, 0, static_cast<unsigned>(max(row1 - row0, 0)) * pitch * 2u, 0x00020000);
+    const int piece = place.lane % PIECES, lane_row = place.lane / PIECES, col = col0 + piece % 8 * 8;
+    const int first = col < h ? (lane_row * pitch + col + (piece >= 8 ? pair_at : 0)) * 2 : 0x7ff00000;
+    const int step = col < h ? ROWS * pitch * 2 : 0;
+    MOE_SB();
+#pragma unroll
+    for (int it = 0; it < R / ROWS; ++it) {
+        const int row = it * ROWS + lane_row;
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(place.patch + (part * 16 + row) * 256 + ((piece ^ (row & 15)) << 4));
+        __builtin_amdgcn_raw_buffer_store_b128(q, rs, first + it * step, 0, 0);
+        if (it % 4 == 3) MOE_SB();
+    }
+}
+
+// acc[2 p] and acc[2 p + 1] of a lane: gate and value of the same four columns
+template <int ACT, bool KEEP, bool KTAIL, int BM>
+__global__ __launch_bounds__(256, 1) void gated_run_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ H, uint16_t *__restrict__ Pre,
+    const WorkItem *__restrict__ items, int entries, int share, int N, int K, int h)
+{
+    struct None {};
+    w4_run<false, KTAIL, BM, 0>(A, W, items, nullptr, entries, share, N, K, nullptr, 1, 0, [](const WorkItem &, int, int) { return None{}; },
+        [&](auto &acc, const None &, const WorkItem &item, const W4Place<BM> &place, auto landed) {
+            const int col0 = item.n0 / 2 + place.wn * 64;
+            // 16 rows at a time: gates and values through the patch's first sixteen rows, H through the last
+            // sixteen (of 128 x 256 tiles, which have sixteen, through the same)
+            constexpr int HPART = W4Place<BM>::UR == 32 && KEEP ? 1 : 0;
+#pragma unroll
+            for (int j = 0; j < W4Place<BM>::TM; ++j) {
+                const int row0 = item.row0 + place.wm * (BM / 2) + j * 16;
+                if constexpr (KEEP) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                        store_f16x4(place.at((i & 1) * 4 + (i >> 1), 0), v);
+                        if (i % 4 == 3) MOE_SB();
+                    }
+                    if (j == 0) landed();
+                    leave_gated<BM, 16, 16>(place, Pre, 2 * h, h, col0, h, row0, item.row1, 0);
+                }
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    float v[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[c] = gate_value<ACT>(acc[2 * p][j][c]) * acc[2 * p + 1][j][c];
+                    store_f16x4(place.at(p, HPART), v);
+                    if (p % 2 == 1) MOE_SB();
+                }
+                if (!KEEP && j == 0) landed();
+                leave_gated<BM, 16, 8>(place, H, h, 0, col0, h, row0, item.row1, HPART);
+            }
+        });
+}
+
+// ---------------------------------------------------------------- first projections, 128 x 128 tiles
+template <int ACT, bool KEEP, bool KTAIL, bool DEEP>
+__global__ __launch_bounds__(256, DEEP ? 1 : 2) void gated_tile_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ H, uint16_t *__restrict__ Pre,
+    const WorkItem *__restrict__ items, int N, int K, int h)
+{
+    constexpr int BM = 128, BN = 128;
+    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false;
+    constexpr int tile_pitch = 0, pair_at = 0, row_div = 1, a_rows = 0;
+    const uint16_t *const tile_in = nullptr;
+    const int32_t *const row_src = nullptr;
+#include "gemm_w4_body.inc"
+
+    // the wavefront's 64 rows of 32 gates and 32 values, or of 32 hidden values: 16 bytes of row padding
+    constexpr int PITCH = 128 + 16;
+    char *const patch = lds + wave * 64 * PITCH;
+    const int rbase = item.row0 + wm * 64, hcol = n0 / 2 + wn * 32;
+#pragma unroll
+    for (int pass = KEEP ? 0 : 1; pass < 2; ++pass) {      // pass 0: G and U, 1: H
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                char *const at = patch + (j * 16 + fr) * PITCH + (p * 16 + 4 * oct) * 2;
+                float v[4], u[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    u[c] = acc[2 * p + 1][j][c];
+                    v[c] = pass == 0 ? acc[2 * p][j][c] : gate_value<ACT>(acc[2 * p][j][c]) * u[c];
+                }
+                store_f16x4(at, v);
+                if (pass == 0) store_f16x4(at + 64, u);
+                if (j == TM / 2 - 1) MOE_SB();
+            }
+            MOE_SB();
+        }
+        MOE_LGKM0();
+        __builtin_amdgcn_wave_barrier();
+        auto leave = [&](auto piecesc, uint16_t *out, int pitch) {
+            constexpr int PIECES = decltype(piecesc)::value, ROWS = 64 / PIECES;
+            const int piece = lane % PIECES, col = hcol + piece % 4 * 8;
+#pragma unroll 8
+            for (int it = 0; it < 64 / ROWS; ++it) {
+                const int rr = it * ROWS + lane / PIECES, r = rbase + rr;
+                const u32x4 q = *reinterpret_cast<const u32x4 *>(patch + rr * PITCH + piece * 16);
+                if (r < item.row1 && col < h)
+                    *reinterpret_cast<u32x4 *>(out + static_cast<size_t>(r) * pitch + col + (piece >= 4 ? h : 0)) = q;
+            }
+        };
+        if (pass == 0) {
+            leave(std::integral_constant<int, 8>{}, Pre, 2 * h);
+            MOE_LGKM0();
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            leave(std::integral_constant<int, 4>{}, H, h);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- first projections, few rows per expert
+// As grouped_gemm_stream_kernel of the expert FFN: a wavefront takes its fragments straight from global memory, here of 32
+// packed columns (sixteen gates and their values) and the rows of a 64-column item, PD stages of 64 on their way.
+template <int ACT, bool KEEP, bool KTAIL>
+__global__ __launch_bounds__(64, 2) void gated_stream_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, _Float16 *__restrict__ H, _Float16 *__restrict__ Pre,
+    const WorkItem *__restrict__ items, int N, int K, int h)
+{
+    // the two blocks of an item are eight apart: one L2's
+    const WorkItem item = items[blockIdx.x / 16 * 8 + blockIdx.x % 8];
+    if (item.expert < 0) return;
+    const int rows = item.row1 - item.row0;
+    const int lane = threadIdx.x, fr = lane & 15, oct = lane >> 4;
+    const int nw = item.n0 + static_cast<int>(blockIdx.x / 8 % 2) * 32;
+    if (nw >= N) return;
+    const int KT = (K + 63) / 64;
+    const uint16_t *wp[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)         // (N is a multiple of 32)
+        wp[t] = W + (static_cast<size_t>(item.expert) * N + nw + t * 16 + fr) * K + oct * 8;
+
+    auto body = [&](auto rt, auto pd) {
+        constexpr int RT = decltype(rt)::value, PD = decltype(pd)::value;
+        const uint16_t *ap[RT];
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+            ap[j] = A + static_cast<size_t>(item.row0 + min(j * 16 + fr, rows - 1)) * K + oct * 8;
+        u32x4 wr[PD][2][2], ar[PD][RT][2];
+        // (no branches around the loads: a piece past K is read from inside the row, and zeroed when multiplied)
+        auto load = [&](auto u, int s) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                int k0 = s * 64 + p * 32;
+                if constexpr (KTAIL) k0 = min(k0, K - 8 - oct * 8);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    wr[decltype(u)::value][t][p] = *reinterpret_cast<const u32x4 *>(wp[t] + k0);
+#pragma unroll
+                for (int j = 0; j < RT; ++j)
+                    ar[decltype(u)::value][j][p] = *reinterpret_cast<const u32x4 *>(ap[j] + k0);
+            }
+        };
+        f32x4 acc[2][RT];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < RT; ++j) acc[t][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+        auto use = [&](auto u, auto tail, int s) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const bool past = KTAIL && decltype(tail)::value && s * 64 + p * 32 + oct * 8 >= K;
+                const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const u32x4 w = past ? zero : wr[decltype(u)::value][t][p];
+#pragma unroll
+                    for (int j = 0; j < RT; ++j) {
+                        const u32x4 a = past ? zero : ar[decltype(u)::value][j][p];
+                        acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, a), acc[t][j], 0, 0, 0);
+                    }
+                }
+            }
+        };
+        static_for<PD>([&](auto u) { load(u, min(decltype(u)::value, KT - 1)); });
+        int s = 0;
+        for (; s + 2 * PD <= KT; s += PD)
+            static_for<PD>([&](auto u) {
+                use(u, std::false_type{}, 0);
+                load(u, s + decltype(u)::value + PD);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        for (; s < KT; s += PD)                      // the last stages: fewer than two rounds
+            static_for<PD>([&](auto u) {
+                if (s + decltype(u)::value < KT) use(u, std::true_type{}, s + decltype(u)::value);
+                if (s + decltype(u)::value + PD < KT) load(u, s + decltype(u)::value + PD);
+            });
+
+        // acc[t][j][c]: gate (t = 0) or value of hidden column nw / 2 + 4 oct + c, row row0 + 16 j + fr
+        const int n = nw / 2 + 4 * oct;
+        if (n >= h) return;
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            if (j * 16 + fr >= rows) continue;
+            const size_t r = static_cast<size_t>(item.row0 + j * 16 + fr);
+            float v[4], g[4], u[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                g[c] = acc[0][j][c];
+                u[c] = acc[1][j][c];
+                v[c] = gate_value<ACT>(g[c]) * u[c];
+            }
+            if constexpr (KEEP) {
+                store_f16x4(reinterpret_cast<char *>(Pre + r * 2 * h + n), g);
+                store_f16x4(reinterpret_cast<char *>(Pre + r * 2 * h + h + n), u);
+            }
+            store_f16x4(reinterpret_cast<char *>(H + r * h + n), v);
+        }
+    };
+    using std::integral_constant;
+    if (rows <= 16)
+        body(integral_constant<int, 1>{}, integral_constant<int, 6>{});
+    else
+        body(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+}
+
+// ---------------------------------------------------------------- fp32 layers
+template <int ACT>
+__device__ __forceinline__ float gate_value_f32(float v)
+{
+    if constexpr (ACT == MOE_ACT_SILU) return v / (1.0f + expf(-v));
+    else if constexpr (ACT == MOE_ACT_GELU_ERF) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    else if constexpr (ACT == MOE_ACT_GELU_TANH) return 0.5f * v * (1.0f + tanhf(0.7978845608028654f * (v + 0.044715f * v * v * v)));
+    else if constexpr (ACT == MOE_ACT_RELU) return fmaxf(v, 0.0f);
+    else return v;
+}
+
+// H = act(A Wg) * (A Wu), W13 canonical [E, K, 2 h]: as grouped_gemm_f32_kernel of the expert FFN, with a second set of
+// weight columns.  Tiles of 32 rows x 32 hidden columns, four wavefronts of 16 x 16, on the fp32 matrix instruction.
+template <int ACT>
+__global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict__ A, const float *__restrict__ B,
+                                                        float *__restrict__ H, const WorkItem *__restrict__ items, int h, int K)
+{
+    const WorkItem tile = items[blockIdx.x];
+    if (tile.expert < 0) return;
+    const int n0 = tile.n0;
+    constexpr int BM = 32, BN = 32, BK = 32, PD = 4, LDA = BK + 4, LDB = BN + 4;
+    __shared__ __attribute__((aligned(16))) float As[2][BM * LDA];
+    __shared__ __attribute__((aligned(16))) float Bs[2][2][BK * LDB];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave & 1, wn = wave >> 1, r16 = lane & 15, kq = lane >> 4;
+    const int KT = (K + BK - 1) / BK;
+    const size_t N = 2 * static_cast<size_t>(h);
+
+    const int a_row = tid / 8, a_k = tid % 8 * 4, b_k = tid / 8, b_n = tid % 8 * 4;
+    const float *a_src = A + static_cast<size_t>(min(tile.row0 + a_row, tile.row1 - 1)) * K;
+    const float *b_src = B + static_cast<size_t>(tile.expert) * K * N + min(n0 + b_n, h - 4);   // (columns past h are not stored)
+    f32x4 ar[PD], br[PD][2];
+    // (no branches around the loads: what lies past K is read from inside and zeroed on its way into LDS)
+    auto load = [&](auto slot, int s) {
+        constexpr int u = decltype(slot)::value;
+        ar[u] = *reinterpret_cast<const f32x4 *>(a_src + min(s * BK + a_k, K - 4));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            br[u][t] = *reinterpret_cast<const f32x4 *>(b_src + static_cast<size_t>(min(s * BK + b_k, K - 1)) * N + t * h);
+    };
+    f32x4 acc[2];
+    acc[0] = acc[1] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    auto stage = [&](auto slot, int s) {
+        constexpr int u = decltype(slot)::value, buf = u & 1;
+        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        *reinterpret_cast<f32x4 *>(&As[buf][a_row * LDA + a_k]) = s * BK + a_k < K ? ar[u] : zero;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            *reinterpret_cast<f32x4 *>(&Bs[buf][t][b_k * LDB + b_n]) = s * BK + b_k < K ? br[u][t] : zero;
+        load(slot, min(s + PD, KT - 1));         // (past the last stage: loaded again, never used)
+        // LDS writes only are waited for: the loads stay in flight across the barrier
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int c = 0; c < BK; c += 16) {
+            const f32x4 af = *reinterpret_cast<const f32x4 *>(&As[buf][(wm * 16 + r16) * LDA + c + 4 * kq]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(Bs[buf][t][(c + 4 * kq + q) * LDB + wn * 16 + r16], af[q],
+                                                                  acc[t], 0, 0, 0);
+        }
+    };
+    static_for<PD>([&](auto u) { load(u, min(decltype(u)::value, KT - 1)); });
+    int s0 = 0;
+    for (; s0 + PD <= KT; s0 += PD) static_for<PD>([&](auto u) { stage(u, s0 + decltype(u)::value); });
+    static_for<PD>([&](auto u) {
+        if (s0 + decltype(u)::value < KT) stage(u, s0 + decltype(u)::value);
+    });
+    // acc[t][c]: column n0 + wn * 16 + 4 kq + c, row row0 + wm * 16 + r16
+    const int n = n0 + wn * 16 + 4 * kq, r = tile.row0 + wm * 16 + r16;
+    if (n >= h || r >= tile.row1) return;
+    f32x4 o;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = gate_value_f32<ACT>(acc[0][c]) * acc[1][c];
+    *reinterpret_cast<f32x4 *>(H + static_cast<size_t>(r) * h + n) = o;
+}
+
+// ---------------------------------------------------------------- backward: dH and through the gate
+// C tile dH = dye W2^T; out = [dG | dU] = [dH U act'(G) | dH act(G)], both bf16, G and U from pre [rows, 2 h].  G and U come
+// into LDS behind the last stages, 32 rows of a wavefront's part at a time, and are turned into dG and dU in their places; of
+// 256 x 256 tiles the rows from 64 on follow while the first ones are computed.
+template <int ACT, bool KTAIL, int BM>
+__global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, const uint16_t *__restrict__ pre, uint16_t *__restrict__ out,
+    const WorkItem *__restrict__ items, int N, int K)
+{
+    constexpr int BN = BM;
+    constexpr bool F16 = false, TILE_IN = true, TILE_PAIR = true, DEEP = false;
+    constexpr int row_div = 1, a_rows = 0;
+    const int32_t *const row_src = nullptr;
+    const uint16_t *const tile_in = pre;
+    const int tile_pitch = 2 * N, pair_at = N;
+#include "gemm_w4_body.inc"
+
+    constexpr int LPR = BN / 16, RPI = 64 / LPR, LINES = 32 / RPI;
+    const int rbase = item.row0 + wm * (BM / 2), ncol = n0 + wn * (BN / 2) + lane % LPR * 8;
+    const int pair[2][2] = {{ua, uw}, {ua1, uw1}};
+    static_for<BM / 64>([&](auto uc) {                // rows 32 u .. of the wavefront's part
+        constexpr int u = decltype(uc)::value;
+        // What may be on its way behind this pair: the pair behind it, and the stores of the pairs before.
+        if constexpr (u == 0) MOE_VMCNT(2 * TILE_LOADS);
+        else if constexpr (BM == 128) MOE_VMCNT(2 * LINES);
+        else if constexpr (u == 1) MOE_VMCNT(2 * TILE_LOADS + 2 * LINES);
+        else if constexpr (u == 2) MOE_VMCNT(2 * TILE_LOADS + 4 * LINES);
+        else MOE_VMCNT(4 * LINES);
+        char *const gp = lds + pair[u & 1][0] + wave * (W_UNIT / 4), *const up = lds + pair[u & 1][1] + wave * (W_UNIT / 4);
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) {
+            const int j = 2 * u + jj, row = jj * 16 + fr;
+            f16x4 g[TN], v[TN];
+            auto place = [&](int i) { return row * BN + (((2 * i + (oct >> 1)) ^ tile_key(row)) << 4) + (oct & 1) * 8; };
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                g[i] = *reinterpret_cast<const f16x4 *>(gp + place(i));
+                v[i] = *reinterpret_cast<const f16x4 *>(up + place(i));
+            }
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                float dg[4], du[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float value, slope;
+                    gate_value_and_slope<ACT>(static_cast<float>(g[i][c]), value, slope);
+                    const float dh = acc[i][j][c];
+                    dg[c] = dh * static_cast<float>(v[i][c]) * slope;
+                    du[c] = dh * value;
+                }
+                store_bf16x4(gp + place(i), dg);
+                store_bf16x4(up + place(i), du);
+                if (i % 2 == 1) MOE_SB();   // a few accumulator registers at a time leave the AGPRs
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        u32x4 line[2][LINES];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int it = 0; it < LINES; ++it) {
+                const int rr = it * RPI + lane / LPR;
+                line[t][it] = *reinterpret_cast<const u32x4 *>((t == 0 ? gp : up) + rr * BN + ((lane % LPR ^ tile_key(rr)) << 4));
+            }
+        if constexpr (BM == 256 && u < 2) {
+            // (the places are free when they have been read)
+            MOE_LGKM0();
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int at = wm * (BM / 2) + (u + 2) * 32, from = t * pair_at, col0 = n0 + wn * (BN / 2);
+                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<uint16_t *>(tile_in) + static_cast<size_t>(item.row0 + min(at, rows - 1)) * tile_pitch + from + min(col0, N - 8), 0,
+                    static_cast<unsigned>(at < rows && col0 < N ? ((rows - at) * tile_pitch - from - col0) * 2 : 0), 0x00020000);
+#pragma unroll
+                for (int q = 0; q < TILE_LOADS; ++q) load_to_lds(rs, t_src[q], w_dest + pair[u & 1][t] + q * 1024, 0);
+            }
+        }
+        MOE_SB();
+        // (stores whose rows or columns lie outside are issued too, past the resource, so that their number is known)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row0 = rbase + u * 32;
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                out + static_cast<size_t>(row0) * tile_pitch + t * pair_at, 0,
+                static_cast<unsigned>(max((item.row1 - row0) * tile_pitch - t * pair_at, 0)) * 2u, 0x00020000);
+#pragma unroll
+            for (int it = 0; it < LINES; ++it) {
+                const int rr = it * RPI + lane / LPR;
+                __builtin_amdgcn_raw_buffer_store_b128(line[t][it], rs, ncol < N ? (rr * tile_pitch + ncol) * 2 : 0x7ff00000, 0, 0);
+            }
+        }
+        MOE_SB();
+    });
+}
+
+// ---------------------------------------------------------------- backward: dxe
+// C [rows, N] bf16 = A W^T
+template <bool KTAIL, int BM>
+__global__ __launch_bounds__(256, 1) void rows_bf16_run_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ C, const WorkItem *__restrict__ items,
+    int entries, int share, int N, int K)
+{
+    struct None {};
+    w4_run<false, KTAIL, BM, 0>(A, W, items, nullptr, entries, share, N, K, nullptr, 1, 0, [](const WorkItem &, int, int) { return None{}; },
+        [&](auto &acc, const None &, const WorkItem &item, const W4Place<BM> &place, auto landed) {
+            constexpr int R = W4Place<BM>::UR;
+#pragma unroll
+            for (int r = 0; r < BM / 2; r += R) {
+#pragma unroll
+                for (int j = r / 16; j < (r + R) / 16; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                        store_bf16x4(place.at(i, j - r / 16), v);
+                        if (i % 4 == 3) MOE_SB();
+                    }
+                }
+                if (r == 0) landed();
+                place.template leave<R>(C, item, r, 0, N);
+            }
+        });
+}
+
+template <bool KTAIL, bool DEEP>
+__global__ __launch_bounds__(256, DEEP ? 1 : 2) void rows_bf16_tile_kernel(
+    const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ C, const WorkItem *__restrict__ items,
+    int N, int K)
+{
+    constexpr int BM = 128, BN = 128;
+    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false;
+    constexpr int tile_pitch = 0, pair_at = 0, row_div = 1, a_rows = 0;
+    const uint16_t *const tile_in = nullptr;
+    const int32_t *const row_src = nullptr;
+#include "gemm_w4_body.inc"
+
+    constexpr int PITCH = BN + 16, LPR = BN / 16, RPI = 64 / LPR;
+    char *const patch = lds + wave * (BM / 2) * PITCH;
+    const int rbase = item.row0 + wm * (BM / 2), ncol = n0 + wn * (BN / 2) + lane % LPR * 8;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+            const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            store_bf16x4(patch + (j * 16 + fr) * PITCH + (i * 16 + 4 * oct) * 2, v);
+        }
+        MOE_SB();
+    }
+    MOE_LGKM0();
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 8
+    for (int it = 0; it < BM / 2 / RPI; ++it) {
+        const int rr = it * RPI + lane / LPR, r = rbase + rr;
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(patch + rr * PITCH + lane % LPR * 16);
+        if (r < item.row1 && ncol < N) *reinterpret_cast<u32x4 *>(C + static_cast<size_t>(r) * N + ncol) = q;
+    }
+}
+
+// ---------------------------------------------------------------- weight packing
+// out[e][column n of in, packed][k] = in[e][k][n], 64 x 64 tiles through LDS.  GATED: n in [0, 2 h), columns n and h + n are
+// sixteen apart (kGatedBlock), padding columns zeros; else out[e][n][k], from bf16 to fp16.
+// Bound by HBM: 16 bytes per lane both ways (a lane turns eight rows of eight columns... through the tile).
+template <bool GATED>
+__global__ __launch_bounds__(256) void gated_pack_kernel(const uint16_t *__restrict__ in, uint16_t *__restrict__ out, int K,
+                                                         int N, int NP)
+{
+    constexpr int PITCH = 66;                      // (33 words: a column's elements fall into different banks)
+    __shared__ uint16_t tile[64 * PITCH];
+    const size_t expert = blockIdx.z;
+    const int k0 = blockIdx.y * 64, p0 = blockIdx.x * 64;
+    // packed column p (of 64 from p0 on) -> column of the matrix, -1: padding
+    auto column = [&](int p) {
+        if constexpr (!GATED) return p < N ? p : -1;
+        const int h = N / 2, b = p / 32, c = b * 16 + p % 16;
+        return c < h ? c + (p % 32 < 16 ? 0 : h) : -1;
+    };
+    const uint16_t *src = in + expert * K * N;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int v = threadIdx.x + 256 * q, kk = v / 8, pp = v % 8 * 8, n = column(p0 + pp);
+        u32x4 w = {0u, 0u, 0u, 0u};                // (eight packed columns are eight of the matrix's)
+        if (n >= 0 && k0 + kk < K) w = *reinterpret_cast<const u32x4 *>(src + static_cast<size_t>(k0 + kk) * N + n);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint32_t *>(&tile[kk * PITCH + pp + 2 * c]) = w[c];
+    }
+    __syncthreads();
+    uint16_t *dst = out + expert * K * NP;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int v = threadIdx.x + 256 * q, pp = v / 8, kk = v % 8 * 8;
+        if (p0 + pp >= NP || k0 + kk >= K) continue;
+        u32x4 w;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint32_t lo = tile[(kk + 2 * c) * PITCH + pp], hi = tile[(kk + 2 * c + 1) * PITCH + pp];
+            if constexpr (!GATED) {
+                lo = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bf16_to_f32(static_cast<uint16_t>(lo))));
+                hi = __builtin_bit_cast(uint16_t, static_cast<_Float16>(bf16_to_f32(static_cast<uint16_t>(hi))));
+            }
+            w[c] = lo | (hi << 16);
+        }
+        *reinterpret_cast<u32x4 *>(dst + static_cast<size_t>(p0 + pp) * K + k0 + kk) = w;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+// Tile of a row-grouped GEMM on these kernels.  few: the kernel for decode steps is there; mid: that of 128 x 256 tiles.
+GemmPlan plan_gated(int64_t rows, int E, int N, int K, bool few, bool mid, int64_t max_rows)
+{
+    GemmPlan gp;
+    if (few && (rows <= 5 * static_cast<int64_t>(E) ||
+                (rows <= 32 * static_cast<int64_t>(E) && rows * ((N + 127) / 128) <= 2000))) {
+        gp.bm = 32;
+        gp.bn = 64;
+        gp.concurrent = 128;
+    } else if (mid && few_long_tiles(rows, E, N, K)) {
+        gp.bm = gp.bn = 128;
+        gp.concurrent = 32;
+        gp.w4 = gp.deep = true;
+    } else {
+        choose_w4_tile(rows, E, N, K, &gp);
+        if (!mid && gp.bm != gp.bn) {
+            gp.bn = 128;
+            gp.concurrent = 64;
+        }
+    }
+    gp.tiles_n = (N + gp.bn - 1) / gp.bn;
+    gp.max_row_tiles = static_cast<int32_t>((max_rows + gp.bm - 1) / gp.bm + E);
+    gp.max_items = work_list_entries(gp);
+    return gp;
+}
+
+struct GatedWorkspace {
+    Workspace lists;           // work lists of the two GEMMs, and the hidden activations
+    size_t bytes;
+};
+void layout_gated(const moe_shape &s, void *base, GatedWorkspace *w)
+{
+    const int64_t R = moe_max_rows(&s);
+    char *p = static_cast<char *>(base);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char *at = p + off;
+        off += align_up(bytes, 256);
+        return at;
+    };
+    w->lists = Workspace{};
+    const bool f32 = s.dtype == MOE_F32;
+    if (f32) {
+        GemmPlan &gp = w->lists.gp[0];
+        gp.bm = gp.bn = 32;
+        gp.concurrent = 256;
+        gp.tiles_n = (s.d_ff + 31) / 32;
+        gp.max_row_tiles = static_cast<int32_t>((R + 31) / 32 + s.E);
+        gp.max_items = work_list_entries(gp);
+    } else {
+        w->lists.gp[0] = plan_gated(R, s.E, gated_packed_columns(s.d_ff), s.d_model, true, true, R);
+    }
+    w->lists.gp[1] = choose_gemm_plan(s, 1, 1, s.T);
+    for (int g = 0; g < 2; ++g)
+        w->lists.items[g] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->lists.gp[g].max_items));
+    w->lists.hidden = take(static_cast<size_t>(R) * s.d_ff * (f32 ? 4 : 2));
+    w->bytes = off;
+}
+
+struct GatedBwdWorkspace {
+    Workspace lists, again;    // of dH and dxe; of the first projections, computed again
+    uint16_t *dGU, *pre, *hid; // [R][2 h], [R][2 h], [R][h]
+    size_t bytes;
+};
+void layout_gated_bwd(const moe_shape &s, void *base, GatedBwdWorkspace *w)
+{
+    const int64_t R = moe_max_rows(&s);
+    char *p = static_cast<char *>(base);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char *at = p + off;
+        off += align_up(bytes, 256);
+        return at;
+    };
+    w->lists = w->again = Workspace{};
+    w->lists.gp[0] = plan_gated(R, s.E, s.d_ff, s.d_model, false, false, R);
+    w->lists.gp[1] = plan_gated(R, s.E, s.d_model, 2 * s.d_ff, false, true, R);
+    w->again.gp[0] = plan_gated(R, s.E, gated_packed_columns(s.d_ff), s.d_model, true, true, R);
+    w->again.gp[1] = w->lists.gp[1];
+    for (int g = 0; g < 2; ++g)
+        w->lists.items[g] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->lists.gp[g].max_items));
+    w->again.items[0] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->again.gp[0].max_items));
+    w->again.items[1] = w->lists.items[1];
+    const size_t Rh = static_cast<size_t>(R) * s.d_ff;
+    w->dGU = reinterpret_cast<uint16_t *>(take(Rh * 4));
+    w->pre = reinterpret_cast<uint16_t *>(take(Rh * 4));
+    w->hid = reinterpret_cast<uint16_t *>(take(Rh * 2));
+    w->bytes = off;
+}
+
+template <typename Kernel, typename... Args>
+void launch_timed(Kernel kern, int grid, int threads, size_t lds, int stage, hipStream_t st, Args... args)
+{
+    hipEvent_t t0, t1;
+    prof_kernel_events(stage, &t0, &t1);
+    hipExtLaunchKernelGGL(kern, dim3(grid), dim3(threads), lds, st, t0, t1, 0, args...);
+}
+
+// f(activation)
+template <typename F>
+void with_activation(int act, F f)
+{
+    using std::integral_constant;
+    switch (act) {
+    case MOE_ACT_GELU_ERF: f(integral_constant<int, MOE_ACT_GELU_ERF>{}); break;
+    case MOE_ACT_GELU_TANH: f(integral_constant<int, MOE_ACT_GELU_TANH>{}); break;
+    case MOE_ACT_RELU: f(integral_constant<int, MOE_ACT_RELU>{}); break;
+    case MOE_ACT_SILU: f(integral_constant<int, MOE_ACT_SILU>{}); break;
+    default: f(integral_constant<int, MOE_ACT_IDENTITY>{});
+    }
+}
+
+// H (and pre) of a bf16 layer
+template <int ACT, bool KEEP>
+void launch_first(const moe_shape &s, const uint16_t *xe, const uint16_t *W13p, uint16_t *H, uint16_t *pre, const GemmPlan &gp,
+                  const WorkItem *items, hipStream_t st)
+{
+    const int N = gated_packed_columns(s.d_ff), K = s.d_model, h = s.d_ff;
+    if (!gp.w4) {
+        auto kern = K % 64 == 0 ? gated_stream_kernel<ACT, KEEP, false> : gated_stream_kernel<ACT, KEEP, true>;
+        launch_timed(kern, gp.max_items * 2, 64, 0, kStageGemm1, st, xe, W13p, reinterpret_cast<_Float16 *>(H),
+                     reinterpret_cast<_Float16 *>(pre), items, N, K, h);
+        return;
+    }
+    auto shape = [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        static PerDeviceOnce once[4];
+        const int share = w4_run_share(gp.bm, K), blocks = w4_run_blocks(gp.max_items, share);
+        auto run = [&](auto kern, PerDeviceOnce &o) {
+            o.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(kW4RunLds));
+            launch_timed(kern, blocks, 256, kW4RunLds, kStageGemm1, st, xe, W13p, H, pre, items, gp.max_items, share, N, K, h);
+        };
+        auto tile = [&](auto kern, PerDeviceOnce &o, size_t lds) {
+            o.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(lds));
+            launch_timed(kern, gp.max_items, 256, lds, kStageGemm1, st, xe, W13p, H, pre, items, N, K, h);
+        };
+        if (gp.bm == 256) run(gated_run_kernel<ACT, KEEP, TAIL, 256>, once[0]);
+        else if (gp.bn == 256) run(gated_run_kernel<ACT, KEEP, TAIL, 128>, once[1]);
+        else if (gp.deep) tile(gated_tile_kernel<ACT, KEEP, TAIL, true>, once[2], kW4Lds);
+        else tile(gated_tile_kernel<ACT, KEEP, TAIL, false>, once[3], w4_lds(128, 128));
+    };
+    if (K % 64 == 0 && (gp.bn != 256 || K >= 256)) shape(std::false_type{});
+    else shape(std::true_type{});
+}
+
+void launch_first_gemm(const moe_shape &s, const void *xe, const void *W13p, void *H, void *pre, const GemmPlan &gp,
+                       const WorkItem *items, hipStream_t st)
+{
+    with_activation(s.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (s.dtype == MOE_F32)
+            launch_timed(gated_f32_kernel<ACT>, gp.max_items, 256, 0, kStageGemm1, st, static_cast<const float *>(xe),
+                         static_cast<const float *>(W13p), static_cast<float *>(H), items, s.d_ff, s.d_model);
+        else if (pre != nullptr)
+            launch_first<ACT, true>(s, static_cast<const uint16_t *>(xe), static_cast<const uint16_t *>(W13p),
+                                    static_cast<uint16_t *>(H), static_cast<uint16_t *>(pre), gp, items, st);
+        else
+            launch_first<ACT, false>(s, static_cast<const uint16_t *>(xe), static_cast<const uint16_t *>(W13p),
+                                     static_cast<uint16_t *>(H), nullptr, gp, items, st);
+    });
+}
+
+void launch_dh(const moe_shape &s, const uint16_t *dye, const uint16_t *W2, const uint16_t *pre, uint16_t *dGU,
+               const GemmPlan &gp, const WorkItem *items, hipStream_t st)
+{
+    const int N = s.d_ff, K = s.d_model;
+    with_activation(s.act, [&](auto act) {
+        auto launch = [&](auto tail, auto bm) {
+            constexpr int BM = decltype(bm)::value;
+            auto kern = gated_dh_kernel<decltype(act)::value, decltype(tail)::value, BM>;
+            constexpr size_t lds = w4_lds(BM, BM);
+            static PerDeviceOnce once;
+            once.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(lds));
+            launch_timed(kern, gp.max_items, 256, lds, kStageBwdDP, st, dye, W2, pre, dGU, items, N, K);
+        };
+        auto shape = [&](auto tail) {
+            if (gp.bm == 256) launch(tail, std::integral_constant<int, 256>{});
+            else launch(tail, std::integral_constant<int, 128>{});
+        };
+        if (K % 64 == 0) shape(std::false_type{});
+        else shape(std::true_type{});
+    });
+}
+
+void launch_dxe(const moe_shape &s, const uint16_t *dGU, const uint16_t *W13, uint16_t *dxe, const GemmPlan &gp,
+                const WorkItem *items, hipStream_t st)
+{
+    const int N = s.d_model, K = 2 * s.d_ff;
+    auto shape = [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        static PerDeviceOnce once[4];
+        const int share = w4_run_share(gp.bm, K), blocks = w4_run_blocks(gp.max_items, share);
+        auto run = [&](auto kern, PerDeviceOnce &o) {
+            o.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(kW4RunLds));
+            launch_timed(kern, blocks, 256, kW4RunLds, kStageBwdDxe, st, dGU, W13, dxe, items, gp.max_items, share, N, K);
+        };
+        auto tile = [&](auto kern, PerDeviceOnce &o, size_t lds) {
+            o.raise_lds(reinterpret_cast<const void *>(kern), static_cast<int>(lds));
+            launch_timed(kern, gp.max_items, 256, lds, kStageBwdDxe, st, dGU, W13, dxe, items, N, K);
+        };
+        if (gp.bm == 256) run(rows_bf16_run_kernel<TAIL, 256>, once[0]);
+        else if (gp.bn == 256) run(rows_bf16_run_kernel<TAIL, 128>, once[1]);
+        else if (gp.deep) tile(rows_bf16_tile_kernel<TAIL, true>, once[2], kW4Lds);
+        else tile(rows_bf16_tile_kernel<TAIL, false>, once[3], w4_lds(128, 128));
+    };
+    if (K % 64 == 0 && (gp.bn != 256 || K >= 256)) shape(std::false_type{});
+    else shape(std::true_type{});
+}
+
+// Everything that the calls below take: a gated row is 2 d_ff values, and the kernels' byte offsets inside a tile's 256 rows
+// are 32 bits.
+moe_status check_gated(const moe_shape *s, bool training)
+{
+    const moe_status rc = check_layer_shape(s);
+    if (rc != MOE_OK) return rc;
+    if (s->d_ff >= 1 << 20 || s->d_model >= 1 << 20) {
+        set_error("gated block: d_model and d_ff below 2^20 (got %d, %d)", s->d_model, s->d_ff);
+        return MOE_EUNSUPPORTED;
+    }
+    if (moe_max_rows(s) >= (1ll << 31) - 256) {
+        set_error("gated block: %lld rows do not fit 31 bits", static_cast<long long>(moe_max_rows(s)));
+        return MOE_EUNSUPPORTED;
+    }
+    if (training && s->dtype != MOE_BF16) {
+        set_error("gated block: its backward pass and what it keeps are for bf16 layers");
+        return MOE_EUNSUPPORTED;
+    }
+    return MOE_OK;
+}
+
+bool bad_pointer(const void *p, const char *name, bool optional)
+{
+    if ((p == nullptr && !optional) || (reinterpret_cast<uintptr_t>(p) & 15u) != 0) {
+        set_error(optional ? "%s is not 16-byte aligned" : "%s is NULL or not 16-byte aligned", name);
+        return true;
+    }
+    return false;
+}
+#define MOE_GATED_PTR(p) \
+    if (bad_pointer(p, #p, false)) return MOE_EINVAL
+#define MOE_GATED_OPTIONAL(p) \
+    if (bad_pointer(p, #p, true)) return MOE_EINVAL
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+size_t moe_gated_packed_bytes(const moe_shape *s)
+{
+    if (check_gated(s, false) != MOE_OK) return 0;
+    const size_t per = static_cast<size_t>(s->E) * s->d_model;
+    return s->dtype == MOE_F32 ? per * s->d_ff * 8 : per * gated_packed_columns(s->d_ff) * 2;
+}
+
+moe_status moe_pack_gated_weights(const moe_shape *s, const void *W13, const void *W2, void *W13p, void *W2p, void *stream)
+{
+    const moe_status rc = check_gated(s, false);
+    if (rc != MOE_OK) return rc;
+    MOE_GATED_PTR(W13);
+    MOE_GATED_PTR(W2);
+    MOE_GATED_PTR(W13p);
+    MOE_GATED_PTR(W2p);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int d = s->d_model, h = s->d_ff;
+    if (s->dtype == MOE_F32) {
+        const size_t one = static_cast<size_t>(s->E) * d * h * 4;
+        MOE_TRY_HIP(hipMemcpyAsync(W13p, W13, 2 * one, hipMemcpyDeviceToDevice, st));
+        MOE_TRY_HIP(hipMemcpyAsync(W2p, W2, one, hipMemcpyDeviceToDevice, st));
+        return MOE_OK;
+    }
+    const int NP = gated_packed_columns(h);
+    hipLaunchKernelGGL(gated_pack_kernel<true>, dim3(ceil_div(NP, 64), ceil_div(d, 64), s->E), dim3(256), 0, st,
+                       static_cast<const uint16_t *>(W13), static_cast<uint16_t *>(W13p), d, 2 * h, NP);
+    hipLaunchKernelGGL(gated_pack_kernel<false>, dim3(ceil_div(d, 64), ceil_div(h, 64), s->E), dim3(256), 0, st,
+                       static_cast<const uint16_t *>(W2), static_cast<uint16_t *>(W2p), h, d, d);
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+size_t moe_gated_workspace_bytes(const moe_shape *s)
+{
+    if (check_gated(s, false) != MOE_OK) return 0;
+    GatedWorkspace w;
+    layout_gated(*s, nullptr, &w);
+    return w.bytes;
+}
+
+moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offsets, const void *W13p, const void *W2p,
+                         void *ye, void *pre, void *hid, void *workspace, void *stream)
+{
+    moe_status rc = check_gated(s, pre != nullptr || hid != nullptr);
+    if (rc != MOE_OK) return rc;
+    MOE_GATED_PTR(xe);
+    MOE_GATED_PTR(offsets);
+    MOE_GATED_PTR(W13p);
+    MOE_GATED_PTR(W2p);
+    MOE_GATED_PTR(ye);
+    MOE_GATED_OPTIONAL(pre);
+    MOE_GATED_OPTIONAL(hid);
+    MOE_GATED_PTR(workspace);
+    if ((pre == nullptr) != (hid == nullptr)) {
+        set_error("moe_gated_ffn: pre and hid come together (both or neither)");
+        return MOE_EINVAL;
+    }
+    GatedWorkspace w;
+    layout_gated(*s, workspace, &w);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    prof_begin(kStageTiles, st);
+    rc = launch_items(*s, 1, 1, offsets, nullptr, w.lists, st);
+    prof_end(kStageTiles, st);
+    if (rc != MOE_OK) return rc;
+    void *H = hid != nullptr ? hid : w.lists.hidden;
+    launch_first_gemm(*s, xe, W13p, H, pre, w.lists.gp[0], w.lists.items[0], st);
+    return launch_second_gemm(*s, H, W2p, ye, w.lists.gp[1], w.lists.items[1], st);
+}
+
+size_t moe_gated_backward_workspace_bytes(const moe_shape *s)
+{
+    if (check_gated(s, true) != MOE_OK) return 0;
+    GatedBwdWorkspace w;
+    layout_gated_bwd(*s, nullptr, &w);
+    return w.bytes;
+}
+
+moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int32_t *offsets, const void *W13, const void *W2,
+                                  const void *W13p, const void *pre, const void *hid, const void *dye, void *dxe, void *dW13,
+                                  void *dW2, void *workspace, void *stream)
+{
+    moe_status rc = check_gated(s, true);
+    if (rc != MOE_OK) return rc;
+    MOE_GATED_PTR(xe);
+    MOE_GATED_PTR(offsets);
+    MOE_GATED_PTR(W13);
+    MOE_GATED_PTR(W2);
+    MOE_GATED_PTR(W13p);
+    MOE_GATED_OPTIONAL(pre);
+    MOE_GATED_OPTIONAL(hid);
+    MOE_GATED_PTR(dye);
+    MOE_GATED_PTR(dxe);
+    MOE_GATED_PTR(dW13);
+    MOE_GATED_PTR(dW2);
+    MOE_GATED_PTR(workspace);
+    if ((pre == nullptr) != (hid == nullptr)) {
+        set_error("moe_gated_ffn_backward: pre and hid come together (both or neither)");
+        return MOE_EINVAL;
+    }
+    GatedBwdWorkspace w;
+    layout_gated_bwd(*s, workspace, &w);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t R = moe_max_rows(s);
+    const int d = s->d_model, h = s->d_ff;
+    rc = launch_items(*s, 1, 1, offsets, nullptr, w.lists, st);
+    if (rc != MOE_OK) return rc;
+    if (pre == nullptr) {
+        // (writes the second list again, as it is)
+        rc = launch_items(*s, 1, 1, offsets, nullptr, w.again, st);
+        if (rc != MOE_OK) return rc;
+        launch_first_gemm(*s, xe, W13p, w.hid, w.pre, w.again.gp[0], w.again.items[0], st);
+        pre = w.pre;
+        hid = w.hid;
+    }
+    const uint16_t *xeb = static_cast<const uint16_t *>(xe), *dyeb = static_cast<const uint16_t *>(dye);
+    launch_dh(*s, dyeb, static_cast<const uint16_t *>(W2), static_cast<const uint16_t *>(pre), w.dGU, w.lists.gp[0],
+              w.lists.items[0], st);
+    launch_dxe(*s, w.dGU, static_cast<const uint16_t *>(W13), static_cast<uint16_t *>(dxe), w.lists.gp[1], w.lists.items[1], st);
+    launch_weight_grad_bf16(true, static_cast<const uint16_t *>(hid), dyeb, static_cast<uint16_t *>(dW2), offsets, s->E, h, d, R,
+                            kStageBwdWgrad2, st);
+    launch_weight_grad_bf16(false, xeb, w.dGU, static_cast<uint16_t *>(dW13), offsets, s->E, d, 2 * h, R, kStageBwdWgrad1, st);
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+}  // extern "C"

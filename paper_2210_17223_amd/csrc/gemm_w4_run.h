@@ -121,7 +121,7 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
     };
     auto weights_of = [&](const WorkItem &t) {
         const uint16_t *at = t.expert < 0 ? W : W + (static_cast<size_t>(t.expert) * N + t.n0) * K;
-        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(N - t.n0);
+        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(min(N - t.n0, 256));     // (a tile's: 256 K values fit)
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(at), 0, n * static_cast<unsigned>(K) * 2u, 0x00020000);
     };
     // load q of this wavefront's TM (TN) of a unit: rows wave * AR (64) + 8 q .. + 7, eight 16-byte pieces

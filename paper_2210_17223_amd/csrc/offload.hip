@@ -51,6 +51,7 @@ moe_status resources(OffloadResources **out)
 bool supported(const moe_shape *s)
 {
     return s != nullptr && s->dtype == MOE_BF16 && s->T >= 1 && s->E >= 1 && s->E <= kMaxExperts &&
+           s->act >= MOE_ACT_GELU_ERF && s->act <= MOE_ACT_IDENTITY &&
            s->k >= 1 && s->k <= kMaxTopK && s->k <= s->E && s->capacity >= 1 && s->d_model >= 8 &&
            s->d_ff >= 8 && s->d_model % 8 == 0 && s->d_ff % 8 == 0;
 }

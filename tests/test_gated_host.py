@@ -1,0 +1,66 @@
+"""CPU-side checks of include/moe_gated.h: sizes, and refusals before anything is enqueued."""
+import ctypes as C
+
+import pytest
+
+import paper_2210_17223_amd as moe
+from paper_2210_17223_amd import gated_binding
+
+
+def shape(**kw):
+    return moe.Shape.make(**{**dict(T=64, d_model=64, E=4, d_ff=128, k=2, capacity=32, act="silu"), **kw})
+
+
+def test_sizes():
+    s = shape()
+    assert moe.moe_gated_packed_bytes(s) == 4 * 64 * 256 * 2
+    assert moe.moe_gated_packed_bytes(shape(d_ff=136)) == 4 * 64 * 288 * 2          # the last sixteen columns are padded
+    assert moe.moe_gated_packed_bytes(shape(d_ff=132, dtype="f32")) == 4 * 64 * 264 * 4
+    assert moe.moe_packed_weight_bytes(s) == 4 * 64 * 128 * 2                        # W2p
+    rows = moe.moe_max_rows(s)
+    assert moe.moe_gated_workspace_bytes(s) >= rows * 128 * 2
+    assert moe.moe_gated_backward_workspace_bytes(s) >= rows * 128 * (4 + 4 + 2)
+    assert moe.moe_gated_workspace_bytes(shape(dtype="f32")) >= rows * 128 * 4
+
+
+@pytest.mark.parametrize("kw,frag", [
+    (dict(E=65), "at most 64"), (dict(k=5, E=4), "exceeds"), (dict(d_model=100), "multiples of 16"), (dict(d_ff=4), "multiples of 16"),
+    (dict(T=0), ">= 1"), (dict(d_ff=1 << 20), "below 2^20"), (dict(T=1 << 30, capacity=1 << 30, k=2), "31 bits"),
+    (dict(T=(1 << 31) - 64, capacity=(1 << 31) - 64, k=1), "31 bits"),
+])
+def test_bad_shapes_are_refused(kw, frag):
+    s = shape(**kw)
+    for size in (moe.moe_gated_packed_bytes, moe.moe_gated_workspace_bytes, moe.moe_gated_backward_workspace_bytes):
+        assert size(s) == 0 and frag in moe.moe_last_error()
+
+
+def test_fp32_blocks_have_no_backward_pass():
+    s, L, ok = shape(dtype="f32"), gated_binding._lib(), C.c_void_p(4096)
+    assert moe.moe_gated_backward_workspace_bytes(s) == 0 and "bf16" in moe.moe_last_error()
+    assert L.moe_gated_ffn_backward(C.byref(s), *[ok] * 12, None) == 2
+    assert L.moe_gated_ffn(C.byref(s), *[ok] * 8, None) == 2 and "bf16" in moe.moe_last_error()
+
+
+def test_null_and_misaligned_pointers_are_refused():
+    L, s, ok, z, odd = gated_binding._lib(), shape(), C.c_void_p(4096), C.c_void_p(0), C.c_void_p(4100)
+    for f, count, optional in ((L.moe_pack_gated_weights, 4, ()), (L.moe_gated_ffn, 8, (5, 6)),
+                               (L.moe_gated_ffn_backward, 12, (5, 6))):
+        for i in range(count):
+            args = [ok] * count
+            args[i] = odd
+            assert f(C.byref(s), *args, z) == 1 and "aligned" in moe.moe_last_error()
+            args[i] = z
+            assert f(C.byref(s), *args, z) == 1
+            assert ("come together" if i in optional else "is NULL") in moe.moe_last_error()
+        assert f(None, *[ok] * count, z) == 1
+
+
+def test_silu_is_the_gated_blocks_only():
+    s, L, ok, z = shape(), moe.lib(), C.c_void_p(4096), C.c_void_p(0)
+    assert L.moe_expert_ffn(C.byref(s), ok, ok, ok, z, ok, z, ok, ok, z) == 2 and "gated" in moe.moe_last_error()
+    assert L.moe_layer_chunked(C.byref(s), 1, ok, ok, z, 0, *[ok] * 16) == 2 and "gated" in moe.moe_last_error()
+    assert moe.moe_padded_workspace_bytes(s, 1) == 0 and moe.moe_offload_workspace_bytes(s) == 0
+    assert moe.moe_workspace_bytes(s, 1) > 0                    # its gate, dispatch and combine are the layer's
+    bad = shape()
+    bad.act = 5
+    assert moe.moe_gated_workspace_bytes(bad) == 0 and "activation" in moe.moe_last_error()
