@@ -69,6 +69,42 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
                                   const void *hid, const void *dye, void *dxe, void *dW13, void *dW2,
                                   void *workspace, void *stream);
 
+/* ---- weights held as 4-bit codes -------------------------------------------------------------
+ *
+ *   w[n, k] = (code[n, k] - zero[n, k / group]) * scale[n, k / group]         y[r, n] = sum_k x[r, k] w[e][n, k]
+ *
+ *   q     uint8 [E, N, K / 2]: the code of k = 2 i in the low four bits of byte i, of 2 i + 1 in the high ones
+ *   scale fp16 [E, N, K / group]
+ *   zero  uint8 [E, N, K / group], or NULL: 8 throughout
+ * group is 32, 64 or 128 and divides K.  Nothing is packed beforehand: the kernels read these as they are.
+ */
+
+/* R rows in all, of E experts (1..64) with matrices [N, K]; x: the rows' type, 1 bf16 or 2 fp16. */
+typedef struct {
+    int32_t R;
+    int32_t E;
+    int32_t N;
+    int32_t K;
+    int32_t group;
+    int32_t x;
+} moe_q4_shape;
+
+/* y fp32 [R, N] = x [R, K] times the rows' expert's matrix; expert e owns rows [offsets[e], offsets[e+1]).
+ * Codes and zeros enter the products exactly, scales and sums are fp32. */
+moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *offsets, const void *q,
+                         const void *scale, const void *zero, float *y, void *stream);
+
+/* Host, pure.  Bytes of workspace of moe_gated_ffn_q4 (0 if unsupported). */
+size_t moe_gated_q4_workspace_bytes(const moe_shape *s);
+
+/* moe_gated_ffn of a MOE_BF16 layer with 4-bit weights: q13 [E, 2 d_ff, d_model / 2] (rows [0, d_ff) are Wg's
+ * columns, [d_ff, 2 d_ff) Wu's), q2 [E, d_model, d_ff / 2], each with its scales and zeros; d_model and d_ff
+ * multiples of group.  xe bf16, ye fp16 [rows, d_model]; the hidden activations are held in fp16. */
+moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, const int32_t *offsets,
+                            const void *q13, const void *scale13, const void *zero13, const void *q2,
+                            const void *scale2, const void *zero2, void *ye, void *workspace,
+                            void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,6 +7,22 @@ import torch
 
 from .binding import Shape, _check, arg, lib, moe_max_rows, moe_packed_weight_bytes, opt, raw_stream
 
+F16, F32, U8 = torch.float16, torch.float32, torch.uint8
+
+
+class Q4Shape(C.Structure):
+    """Mirror of moe_q4_shape in include/moe_gated.h."""
+    _fields_ = [(name, C.c_int32) for name in ("R", "E", "N", "K", "group", "x")]
+
+    @classmethod
+    def make(cls, R, E, N, K, group, x="bf16"):
+        return cls(R, E, N, K, group, {"bf16": 1, "f16": 2}[x])
+
+    @property
+    def x_torch_dtype(self):
+        return torch.bfloat16 if self.x == 1 else F16
+
+
 _ready = False
 
 
@@ -19,6 +35,12 @@ def _lib():
             f = getattr(L, f"moe_gated_{name}_bytes")
             f.restype = C.c_size_t
             f.argtypes = [sp]
+        L.moe_gated_q4_workspace_bytes.restype = C.c_size_t
+        L.moe_gated_q4_workspace_bytes.argtypes = [sp]
+        L.moe_q4_linear.restype = C.c_int
+        L.moe_q4_linear.argtypes = [C.POINTER(Q4Shape)] + [vp] * 7
+        L.moe_gated_ffn_q4.restype = C.c_int
+        L.moe_gated_ffn_q4.argtypes = [sp, C.c_int32] + [vp] * 11
         for name, pointers in (("pack_gated_weights", 5), ("gated_ffn", 9), ("gated_ffn_backward", 13)):
             f = getattr(L, "moe_" + name)
             f.restype = C.c_int
@@ -66,4 +88,29 @@ def moe_gated_ffn_backward(s: Shape, xe, offsets, W13, W2, W13p, pre, hid, dye, 
         opt(pre, torch.float16, rows * 2 * h, "pre"), opt(hid, torch.float16, rows * h, "hid"),
         arg(dye, b, rows * s.d_model, "dye"), arg(dxe, b, rows * s.d_model, "dxe"), arg(dW13, b, 2 * n, "dW13"),
         arg(dW2, b, n, "dW2"), arg(workspace, torch.uint8, moe_gated_backward_workspace_bytes(s), "workspace"),
+        raw_stream(stream, xe)))
+
+
+def moe_gated_q4_workspace_bytes(s: Shape) -> int:
+    return int(_lib().moe_gated_q4_workspace_bytes(C.byref(s)))
+
+
+def _codes(q, scale, zero, values, group, name):
+    g = values // group
+    return (arg(q, U8, values // 2, "q" + name), arg(scale, F16, g, "scale" + name), opt(zero, U8, g, "zero" + name))
+
+
+def moe_q4_linear(s: Q4Shape, x, offsets, q, scale, zero, y, stream=None) -> None:
+    _check(_lib().moe_q4_linear(
+        C.byref(s), arg(x, s.x_torch_dtype, s.R * s.K, "x"), arg(offsets, torch.int32, s.E + 1, "offsets"),
+        *_codes(q, scale, zero, s.E * s.N * s.K, s.group or 1, ""), arg(y, F32, s.R * s.N, "y"), raw_stream(stream, x)))
+
+
+def moe_gated_ffn_q4(s: Shape, group: int, xe, offsets, q13, scale13, zero13, q2, scale2, zero2, ye, workspace,
+                     stream=None) -> None:
+    rows, n = moe_max_rows(s), s.E * s.d_model * s.d_ff
+    _check(_lib().moe_gated_ffn_q4(
+        C.byref(s), group, arg(xe, torch.bfloat16, rows * s.d_model, "xe"), arg(offsets, torch.int32, s.E + 1, "offsets"),
+        *_codes(q13, scale13, zero13, 2 * n, group or 1, "13"), *_codes(q2, scale2, zero2, n, group or 1, "2"),
+        arg(ye, F16, rows * s.d_model, "ye"), arg(workspace, U8, moe_gated_q4_workspace_bytes(s), "workspace"),
         raw_stream(stream, xe)))

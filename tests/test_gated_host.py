@@ -64,3 +64,49 @@ def test_silu_is_the_gated_blocks_only():
     bad = shape()
     bad.act = 5
     assert moe.moe_gated_workspace_bytes(bad) == 0 and "activation" in moe.moe_last_error()
+
+
+def q4(**kw):
+    return moe.Q4Shape.make(**{**dict(R=8, E=2, N=48, K=256, group=64), **kw})
+
+
+@pytest.mark.parametrize("kw,status,frag", [
+    (dict(R=0), 1, ">= 1"), (dict(N=0), 1, ">= 1"), (dict(E=65), 2, "at most 64"), (dict(K=1 << 24), 2, "2^24"),
+    (dict(N=1 << 24), 2, "2^24"), (dict(R=1 << 30), 2, "2^30"), (dict(group=16), 2, "32, 64 or 128"), (dict(group=0), 2, "32, 64 or 128"),
+    (dict(K=96), 2, "divide"), (dict(K=320, group=128), 2, "divide"),
+])
+def test_q4_linear_refuses_bad_shapes(kw, status, frag):
+    L, ok = gated_binding._lib(), C.c_void_p(4096)
+    assert L.moe_q4_linear(C.byref(q4(**kw)), *[ok] * 6, None) == status and frag in moe.moe_last_error()
+
+
+def test_q4_linear_refuses_other_types_and_bad_pointers():
+    L, s, ok, z, odd = gated_binding._lib(), q4(), C.c_void_p(4096), C.c_void_p(0), C.c_void_p(4100)
+    s.x = 0
+    assert L.moe_q4_linear(C.byref(s), *[ok] * 6, None) == 1 and "bf16" in moe.moe_last_error()
+    assert L.moe_q4_linear(None, *[ok] * 6, None) == 1
+    for i in range(6):
+        args = [ok] * 6
+        args[i] = odd
+        assert L.moe_q4_linear(C.byref(q4()), *args, z) == 1 and "aligned" in moe.moe_last_error()
+        args[i] = z
+        if i != 4:
+            assert L.moe_q4_linear(C.byref(q4()), *args, z) == 1 and "is NULL" in moe.moe_last_error()
+
+
+def test_gated_ffn_q4_refusals():
+    L, ok, z, odd = gated_binding._lib(), C.c_void_p(4096), C.c_void_p(0), C.c_void_p(4100)
+    s = shape()
+    assert moe.moe_gated_q4_workspace_bytes(s) >= moe.moe_max_rows(s) * 128 * 2
+    assert moe.moe_gated_q4_workspace_bytes(shape(dtype="f32")) == 0 and "bf16" in moe.moe_last_error()
+    assert L.moe_gated_ffn_q4(C.byref(shape(dtype="f32")), 64, *[ok] * 10, z) == 2
+    for group, kw in ((16, {}), (128, {}), (64, dict(d_ff=136)), (32, dict(d_model=72)), (-32, {})):
+        assert L.moe_gated_ffn_q4(C.byref(shape(**kw)), group, *[ok] * 10, z) == 2 and "group" in moe.moe_last_error()
+    for i in range(10):
+        args = [ok] * 10
+        args[i] = odd
+        assert L.moe_gated_ffn_q4(C.byref(s), 64, *args, z) == 1 and "aligned" in moe.moe_last_error()
+        args[i] = z
+        if i not in (4, 7):
+            assert L.moe_gated_ffn_q4(C.byref(s), 64, *args, z) == 1 and "is NULL" in moe.moe_last_error()
+    assert L.moe_gated_ffn_q4(None, 64, *[ok] * 10, z) == 1
