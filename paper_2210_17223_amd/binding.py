@@ -148,9 +148,15 @@ def opt(t: Optional[torch.Tensor], dtype, numel: int, name: str) -> Optional[int
     return None if t is None else arg(t, dtype, numel, name)
 
 
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def raw_stream(stream, t: torch.Tensor) -> int:
-    """The stream's handle; None: the current one of t's device."""
+    """The stream's handle; None: the current one of t's device (whose Stream object takes 2 us to make, where torch
+    offers no way to the handle alone)."""
     if stream is None:
+        if _current_handle is not None:
+            return _current_handle(t.get_device())
         stream = torch.cuda.current_stream(t.device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

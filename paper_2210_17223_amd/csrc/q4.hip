@@ -41,21 +41,29 @@ __device__ __forceinline__ void unrolled(F f)
     each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
-// Eight codes of a dword, c0 lowest, as eight 16-bit numbers in the order c0 c4 c1 c5 c2 c6 c3 c7.
+// Eight codes of a dword, c0 lowest, as eight 16-bit numbers in the order c0 c4 c1 c5 c2 c6 c3 c7.  exponent: exponent_of<XT>()
+// in a vector register (an instruction takes one constant, and masking and setting the exponent is one instruction then).
 template <int XT>
-__device__ __forceinline__ u32x4 widen(uint32_t w, f16x2 minus, f16x2 minus16)
+__device__ __forceinline__ uint32_t exponent_of()
+{
+    uint32_t e = XT == kXBf16 ? 0x43004300u : 0x64006400u;
+    asm volatile("" : "+v"(e));
+    return e;
+}
+template <int XT>
+__device__ __forceinline__ u32x4 widen(uint32_t w, uint32_t exponent, f16x2 minus, f16x2 minus16)
 {
     if constexpr (XT == kXBf16) {
-        auto part = [](uint32_t v) { return (v & 0x000f000fu) | 0x43004300u; };
+        auto part = [&](uint32_t v) { return (v & 0x000f000fu) | exponent; };
         return (u32x4){part(w), part(w >> 4), part(w >> 8), part(w >> 12)};
     } else {
         // low four bits of a byte: 1024 + q; high: 1024 + 16 q, a sixteenth of which is 64 + q
         const f16x2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
         auto low = [&](uint32_t v) {
-            return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, (v & 0x000f000fu) | 0x64006400u) + minus);
+            return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, (v & 0x000f000fu) | exponent) + minus);
         };
         auto high = [&](uint32_t v) {
-            return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & 0x00f000f0u) | 0x64006400u),
+            return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & 0x00f000f0u) | exponent),
                                                                           sixteenth, minus16));
         };
         return (u32x4){low(w), high(w), low(w >> 8), high(w >> 8)};
@@ -126,6 +134,20 @@ struct Run {                               // BYTES consecutive bytes, from an a
     }
     __device__ __forceinline__ void set16(int i, uint32_t v) { w[i / 2] = i % 2 == 0 ? v : w[i / 2] | (v << 16); }
     __device__ __forceinline__ void set8(int i, uint32_t v) { w[i / 4] = i % 4 == 0 ? v : w[i / 4] | (v << (i % 4 * 8)); }
+    // what the lanes of quarter Q of the wavefront hold, in all of them (of the same place in their quarters)
+    template <int Q>
+    __device__ __forceinline__ Run quarter() const
+    {
+        Run out;
+#pragma unroll
+        for (int i = 0; i < (BYTES + 3) / 4; ++i) {
+            const auto h = __builtin_amdgcn_permlane32_swap(w[i], w[i], false, false);
+            const uint32_t v = h[Q / 2];
+            const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+            out.w[i] = r[Q % 2];
+        }
+        return out;
+    }
     __device__ __forceinline__ float half(int i) const
     {
         return static_cast<float>(__builtin_bit_cast(f16x2, w[i / 2])[i % 2]);
@@ -156,21 +178,31 @@ __device__ __forceinline__ float gated_by(int act, float g, float u)
 
 // ---------------------------------------------------------------- few rows per expert
 // The time is that of streaming the codes once.  A block owns 16 NT columns of one expert, its wavefronts share out the
-// depth in steps of 256 (a 128-byte line of every column's codes), two of them on their way, and add up through LDS in a fixed
-// order; rows are taken 16 at a time, of which those past the expert's last one are zeros that no load fetches.  x comes
-// straight from memory, too, half a step ahead, and feeds NT column groups: with one its reads, not the codes', would fill
-// the address unit (1 KiB of x for 256 bytes of codes).
+// depth in steps of 256 (a 128-byte line of every column's codes) and add up through LDS in a fixed order; rows are taken XR at
+// a time.
+// What bounded it first was the address unit, which takes a cycle for every 64 bytes that four neighbouring lanes do not
+// share, and neighbouring lanes hold neighbouring columns (or rows of x): 64 cycles for each KiB, and x is four loads beside
+// one of codes, the scales and zeros two more (64 rows, 8 experts of 4096 x 14336, group 64: busy for 81 % of 180 us).  So
+// x and the codes are loaded line by line, pass through the wavefront's own LDS, x in the codes' order, and are read from there
+// as the instruction wants them; and of scales and zeros a lane loads one of four steps, which the quarters of the wavefront
+// then hand round.
+// Loads are waited for in the order of their issue: x of the next step goes out before the codes of the one behind it.
 // KTAIL: K is not a multiple of 256.
-template <int XT, int G, bool ZEROS, int NT, bool KTAIL>
+template <int XT, int G, bool ZEROS, int NT, int XR, bool KTAIL>
 __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
 {
-    constexpr int PD = 2, GROUPS = 256 / G, PER = 4 / (128 / G);      // groups of a step; dwords of 128 k and one group
+    constexpr int GROUPS = 256 / G, PER = 4 / (128 / G);     // groups of a step; dwords of 128 k and one group
+    constexpr int XP = XR / 2, PITCH = 528, CODES = 144;     // pieces of x per lane; bytes of a row of x, of codes in LDS
     const int expert = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
     const int r0 = a.offsets[expert], r1 = a.offsets[expert + 1];
     if (r0 >= r1) return;
     const int lane = lane_id(), fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    extern __shared__ __attribute__((aligned(16))) float sums[];      // [waves][NT][4][64]
+    // [waves] of a step's x and codes, and then of the sums [NT][4][64]
+    constexpr int XS = XR * PITCH, OWN = XS + NT * 16 * CODES;
+    static_assert(OWN >= NT * 1024, "the sums lie there, too");
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    char *const own = shared + wave * OWN;
     const bool gated = a.kind == kOutGated;
     const int half = gated ? NT / 2 : NT, width = gated ? a.N / 2 : a.N, col0 = tile * half * 16;
     const int KG = a.K / G, KB = a.K / 2;
@@ -179,23 +211,37 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
         return static_cast<size_t>(expert) * a.N + min(col0 + t % half * 16, width - 1) + (t >= half ? width : 0);
     };
     auto rows_of = [&](int t) { return min(max(width - col0 - t % half * 16, 1), 16); };
-    const int q_at = fr * KB + oct * 16;
-    unsigned g_at[NT];                                   // the lane's row of groups
+    const uint32_t exponent = exponent_of<XT>();
+    // codes: lane l loads 16 bytes of row l / 8 of each eight
+    const int q_at = (lane >> 3) * KB + (lane & 7) * 16;
+    char *const q_to = own + XS + (lane >> 3) * CODES + (lane & 7) * 16;
+    const char *const q_from = own + XS + fr * CODES + oct * 16;
+    unsigned g_at[NT];                                       // the lane's row of groups
 #pragma unroll
     for (int t = 0; t < NT; ++t) g_at[t] = static_cast<unsigned>(min(fr, rows_of(t) - 1)) * KG;
     const int steps = a.K / 256;
     const int s0 = steps * wave / waves, s1 = steps * (wave + 1) / waves;
+    // x: lane l loads 16 bytes of row l / 32 of each two
+    const int x_at = (lane >> 5) * a.K * 2 + (lane & 31) * 16;
+    char *const x_to = own + (lane >> 5) * PITCH + (lane & 31) * 16;
+    const char *const x_from = own + fr % XR * PITCH;
 
-    for (int row0 = r0; row0 < r1; row0 += 16) {
+    for (int row0 = r0; row0 < r1; row0 += XR) {
+        // (rows past the expert's last one: zeros that no load fetches)
         const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(min(r1 - row0, 16)) * a.K * 2u, 0x00020000);
+            const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(min(r1 - row0, XR)) * a.K * 2u, 0x00020000);
         f32x4 total[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) total[t] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-        u32x4 code[PD][NT][2], xr[2][4];
-        Run<GROUPS * 2> sc[PD][NT];
-        Run<GROUPS> zr[PD][NT];
-        auto load = [&](auto uc, int s) {
+        u32x4 code[2][NT][2], xr[XP];
+        Run<GROUPS * 2> sc[2][NT];                           // of the step s0 + 4 c + oct, for two c
+        Run<GROUPS> zr[2][NT];
+        auto load_x = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < XP; ++i)
+                xr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, x_at + i * 4 * a.K, s * 512, 0));
+        };
+        auto load_codes = [&](auto uc, int s) {
             constexpr int u = decltype(uc)::value;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -203,119 +249,138 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
                     const_cast<uint8_t *>(a.q) + first_row(t) * KB + s * 128, 0, static_cast<unsigned>(max(rows_of(t) * KB - s * 128, 0)), 0x00020000);
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
-                    code[u][t][b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, q_at + b * 64, 0, 0));
-                const uint16_t *sp = a.scale + first_row(t) * KG;
-                const uint8_t *zp = a.zero + first_row(t) * KG;
-                sc[u][t].load(reinterpret_cast<const char *>(sp + s * GROUPS) + g_at[t] * 2u);
-                if constexpr (ZEROS) zr[u][t].load(zp + s * GROUPS + g_at[t]);
+                    code[u][t][b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, q_at + b * 8 * KB, 0, 0));
             }
         };
-        // (what lies past K reads as zeros: x alone decides there)
-        auto load_x = [&](auto bc, auto tail, int s) {
-            constexpr int b = decltype(bc)::value;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = s * 256 + b * 128 + k_of<G>(j, oct);
-                int at = (fr * a.K + k) * 2;
-                if constexpr (decltype(tail)::value) at = k < a.K ? at : 0x7ffffff0;
-                xr[b][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, at, 0, 0));
-            }
-        };
-        auto use = [&](auto uc, auto bc) {
-            constexpr int u = decltype(uc)::value, b = decltype(bc)::value;
-            const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-            const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-            f32x4 xsum[GROUPS / 2];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) xr[b][j] = reorder(xr[b][j]);
-            if constexpr (XT == kXBf16) {
-#pragma unroll
-                for (int g = 0; g < GROUPS / 2; ++g) {
-                    xsum[g] = none;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) xsum[g] = multiply<XT>(xr[b][g * PER + j], ones, xsum[g]);
-                }
-            }
+        auto load_scales = [&](auto cc, int s) {             // of the steps s .. s + 3
+            constexpr int c = decltype(cc)::value;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                regroup<G>(code[u][t][b]);
-#pragma unroll
-                for (int g = 0; g < GROUPS / 2; ++g) {
-                    const float sv = sc[u][t].half(b * (GROUPS / 2) + g);
-                    const float z = ZEROS ? static_cast<float>(zr[u][t].byte(b * (GROUPS / 2) + g)) : 8.0f;
-                    const _Float16 m1 = static_cast<_Float16>(-1024.0f - z), m16 = static_cast<_Float16>(-64.0f - z);
-                    f32x4 part = none;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        part = multiply<XT>(xr[b][g * PER + j],
-                                            widen<XT>(code[u][t][b][g * PER + j], (f16x2){m1, m1}, (f16x2){m16, m16}), part);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v = part[c];
-                        if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - z, xsum[g][c], v);
-                        total[t][c] = __builtin_fmaf(sv, v, total[t][c]);
-                    }
-                }
-                if (t % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (two column groups' numbers at a time)
+                const unsigned at = g_at[t] + static_cast<unsigned>(min(s + oct, s1 - 1)) * GROUPS;
+                sc[c][t].load(reinterpret_cast<const char *>(a.scale + first_row(t) * KG) + at * 2u);
+                if constexpr (ZEROS) zr[c][t].load(a.zero + first_row(t) * KG + at);
             }
         };
-        using B0 = std::integral_constant<int, 0>;
-        using B1 = std::integral_constant<int, 1>;
+        auto codes_into_lds = [&](auto uc) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) *reinterpret_cast<u32x4 *>(q_to + (t * 2 + b) * 8 * CODES) = code[decltype(uc)::value][t][b];
+        };
+        auto x_into_lds = [&]() {
+#pragma unroll
+            for (int i = 0; i < XP; ++i) *reinterpret_cast<u32x4 *>(x_to + i * 2 * PITCH) = reorder(xr[i]);
+        };
+        // the step's sums, with scales s and zeros z (every lane's own)
+        auto use = [&](auto &s, auto &z) {
+            const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+            const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                u32x4 xf[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xf[j] = *reinterpret_cast<const u32x4 *>(x_from + (b * 128 + k_of<G>(j, oct)) * 2);
+                f32x4 xsum[GROUPS / 2];
+                if constexpr (XT == kXBf16) {
+#pragma unroll
+                    for (int g = 0; g < GROUPS / 2; ++g) {
+                        xsum[g] = none;
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) xsum[g] = multiply<XT>(xf[g * PER + j], ones, xsum[g]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    u32x4 w = *reinterpret_cast<const u32x4 *>(q_from + t * 16 * CODES + b * 64);
+                    regroup<G>(w);
+#pragma unroll
+                    for (int g = 0; g < GROUPS / 2; ++g) {
+                        const float sv = s[t].half(b * (GROUPS / 2) + g);
+                        const float zv = ZEROS ? static_cast<float>(z[t].byte(b * (GROUPS / 2) + g)) : 8.0f;
+                        const _Float16 m1 = static_cast<_Float16>(-1024.0f - zv), m16 = static_cast<_Float16>(-64.0f - zv);
+                        f32x4 part = none;
+#pragma unroll
+                        for (int j = 0; j < PER; ++j)
+                            part = multiply<XT>(xf[g * PER + j],
+                                                widen<XT>(w[g * PER + j], exponent, (f16x2){m1, m1}, (f16x2){m16, m16}), part);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float v = part[c];
+                            if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - zv, xsum[g][c], v);
+                            total[t][c] = __builtin_fmaf(sv, v, total[t][c]);
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);           // (half a step's numbers at a time)
+            }
+        };
+        using std::integral_constant;
         if (s0 < s1) {
             // (past the last step: the last one again, never used)
-            unrolled<PD>([&](auto u) { load(u, min(s0 + decltype(u)::value, s1 - 1)); });
-            using Whole = std::false_type;
-            load_x(B0{}, Whole{}, s0);
-            auto one = [&](auto u, int s) {
-                load_x(B1{}, Whole{}, s);
-                use(u, B0{});
-                load_x(B0{}, Whole{}, min(s + 1, s1 - 1));
-                use(u, B1{});
-                load(u, min(s + PD, s1 - 1));
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            int s = s0;
-            for (; s + PD <= s1; s += PD) unrolled<PD>([&](auto u) { one(u, s + decltype(u)::value); });
-            if (s < s1) one(B0{}, s);
+            load_scales(integral_constant<int, 0>{}, s0);
+            load_codes(integral_constant<int, 0>{}, s0);
+            load_x(s0);
+            load_codes(integral_constant<int, 1>{}, min(s0 + 1, s1 - 1));
+            for (int s = s0; s < s1; s += 8) {
+                unrolled<8>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value, c = i / 4;
+                    if (s + i >= s1) return;
+                    x_into_lds();
+                    codes_into_lds(integral_constant<int, i % 2>{});
+                    load_x(min(s + i + 1, s1 - 1));
+                    load_codes(integral_constant<int, i % 2>{}, min(s + i + 2, s1 - 1));
+                    if constexpr (i % 4 == 0) load_scales(integral_constant<int, 1 - c>{}, min(s + i + 4, s1 - 1));
+                    Run<GROUPS * 2> mine[NT];
+                    Run<GROUPS> zeros[NT];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        mine[t] = sc[c][t].template quarter<i % 4>();
+                        if constexpr (ZEROS) zeros[t] = zr[c][t].template quarter<i % 4>();
+                    }
+                    use(mine, zeros);
+                });
+            }
         }
         if constexpr (KTAIL) {
             // what is left of K, in the last wavefront: groups past it have no scale, codes and x past it read as zeros
             // or the next row's codes against zeros
             if (wave == waves - 1) {
+                Run<GROUPS * 2> mine[NT];
+                Run<GROUPS> zeros[NT];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-                        const_cast<uint8_t *>(a.q) + first_row(t) * KB + steps * 128, 0, static_cast<unsigned>(rows_of(t) * KB - steps * 128), 0x00020000);
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        code[0][t][b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, q_at + b * 64, 0, 0));
 #pragma unroll
                     for (int g = 0; g < GROUPS; ++g) {
                         const bool there = steps * GROUPS + g < KG;
                         const unsigned at = g_at[t] + min(steps * GROUPS + g, KG - 1);
-                        sc[0][t].set16(g, there ? (a.scale + first_row(t) * KG)[at] : 0u);
-                        if constexpr (ZEROS) zr[0][t].set8(g, (a.zero + first_row(t) * KG)[at]);
+                        mine[t].set16(g, there ? (a.scale + first_row(t) * KG)[at] : 0u);
+                        if constexpr (ZEROS) zeros[t].set8(g, (a.zero + first_row(t) * KG)[at]);
                     }
                 }
-                load_x(B0{}, std::true_type{}, steps);
-                load_x(B1{}, std::true_type{}, steps);
-                use(B0{}, B0{});
-                use(B0{}, B1{});
+                load_codes(integral_constant<int, 0>{}, steps);
+#pragma unroll
+                for (int i = 0; i < XP; ++i)
+                    xr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                        rsx, steps * 256 + (lane & 31) * 8 < a.K ? x_at + i * 4 * a.K + steps * 512 : 0x7ffffff0, 0, 0));
+                x_into_lds();
+                codes_into_lds(integral_constant<int, 0>{});
+                use(mine, zeros);
             }
         }
 
         // total[t][c]: row row0 + 4 oct + c, column fr of group t
-        float *own = sums + wave * (NT * 256);
+        // (over x, whose reads are through: a wavefront's accesses are taken in order)
+        float *mine = reinterpret_cast<float *>(own);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) own[(t * 4 + c) * 64 + lane] = total[t][c];
+            for (int c = 0; c < 4; ++c) mine[(t * 4 + c) * 64 + lane] = total[t][c];
         __syncthreads();
-        const int rows = min(r1 - row0, 16), cols = half * 16;
+        const int rows = min(r1 - row0, XR), cols = half * 16;
         auto add_up = [&](int row, int t, int n) {
             const int at = (t * 4 + row % 4) * 64 + row / 4 * 16 + n;
             float v = 0.0f;
-            for (int w = 0; w < waves; ++w) v += sums[w * (NT * 256) + at];
+            for (int w = 0; w < waves; ++w) v += reinterpret_cast<const float *>(shared + w * OWN)[at];
             return v;
         };
         for (int i = threadIdx.x; i < rows * cols; i += blockDim.x) {
@@ -331,46 +396,299 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
     }
 }
 
+// ---------------------------------------------------------------- many rows per expert
+// BM x 128 tiles (128 rows of codes: columns, or 64 gates and their values), four wavefronts of 64 x 64 (BM = 128), 64 x 32
+// or 32 x 32, two blocks a compute unit.  Stages of 128: x (in the codes' order), codes, scales and zeros of the next one are on
+// their way in registers while this one, in LDS, is multiplied; one block multiplies while the other moves them there.  A group's sums have accumulators of their own; behind the
+// group they are scaled into the totals, four instructions for each tile of 16 x 16 and group beside its G / 32 matrix
+// instructions (and in bf16 four more for the zeros): bound by the issue of both.  Each wavefront widens its own columns'
+// codes, seven instructions for eight of them, which feed BM / 32 matrix instructions.
+template <int XT, int G, bool ZEROS, int BM>
+__global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
+{
+    constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
+    constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
+    constexpr int XPITCH = 272, QPITCH = 80;                 // bytes of a row in LDS
+    constexpr int XV = BM / 16;                              // 16-byte pieces of x per thread and stage
+    constexpr int Q_AT = BM * XPITCH, S_AT = Q_AT + 128 * QPITCH;
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
+    const bool gated = a.kind == kOutGated;
+    const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
+
+    // The block's tile: an expert's tiles row by row inside a column, experts one after the other, an eighth of all per XCD.
+    int expert, row0, row1, col0;
+    {
+        const int e = min(lane, a.E - 1), first = a.offsets[e], end = lane < a.E ? a.offsets[e + 1] : first;
+        const int mt = end > first ? (end - first + BM - 1) / BM : 0;
+        int sum = mt * a.tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        const int total = __builtin_amdgcn_readlane(sum, 63), per_xcd = (total + 7) / 8;
+        const int slot = blockIdx.x / 8, index = blockIdx.x % 8 * per_xcd + slot;
+        if (slot >= per_xcd || index >= total) return;
+        expert = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
+        const int rows_mt = __builtin_amdgcn_readlane(mt, expert);
+        const int within = index - (__builtin_amdgcn_readlane(sum, expert) - rows_mt * a.tiles);
+        const int r0 = __builtin_amdgcn_readlane(first, expert);
+        row0 = r0 + within % rows_mt * BM;
+        row1 = min(row0 + BM, __builtin_amdgcn_readlane(end, expert));
+        col0 = within / rows_mt * (gated ? 64 : 128);
+    }
+
+    // staging: piece p = tid + 256 q; x: row p / 16 of the tile, codes: row p / 4
+    const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(row1 - row0) * a.K * 2u, 0x00020000);
+    auto code_row = [&](int i) {                             // row of the expert's codes that lies in row i of the tile
+        if (!gated) return min(col0 + i, width - 1);
+        const int w = i / (16 * TN), t = i / 16 % TN;
+        return min(col0 + w * (8 * TN) + t % (TN / 2) * 16 + i % 16, width - 1) + (t >= TN / 2 ? width : 0);
+    };
+    const uint8_t *q_src[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int p = tid + 256 * q;
+        q_src[q] = a.q + (static_cast<size_t>(expert) * a.N + code_row(p / 4)) * KB;
+    }
+    const size_t g_row = (static_cast<size_t>(expert) * a.N + code_row(tid & 127)) * KG;   // threads < 128: scales, others: zeros
+    u32x4 xr[XV], qr[2];
+    Run<GS * 2> gr;
+    auto load = [&](int s) {
+#pragma unroll
+        for (int q = 0; q < XV; ++q) {
+            const int p = tid + 256 * q, k = s * 128 + p % 16 * 8;
+            xr[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, k < a.K ? (p / 16 * a.K + k) * 2 : 0x7ffffff0, 0, 0));
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + 256 * q) % 4 * 16, KB - 16));
+        if (tid < 128) {
+            if (s * GS + GS <= KG) {
+                gr.load(a.scale + g_row + s * GS);
+            } else {
+#pragma unroll
+                for (int g = 0; g < GS; ++g) gr.set16(g, s * GS + g < KG ? a.scale[g_row + min(s * GS + g, KG - 1)] : 0u);
+            }
+        } else if (ZEROS) {
+#pragma unroll
+            for (int g = 0; g < GS; ++g) gr.set16(g, a.zero[g_row + min(s * GS + g, KG - 1)]);
+        }
+    };
+    auto place = [&]() {
+#pragma unroll
+        for (int q = 0; q < XV; ++q) {
+            const int p = tid + 256 * q;
+            *reinterpret_cast<u32x4 *>(shared + p / 16 * XPITCH + p % 16 * 16) = reorder(xr[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int p = tid + 256 * q;
+            *reinterpret_cast<u32x4 *>(shared + Q_AT + p / 4 * QPITCH + p % 4 * 16) = qr[q];
+        }
+        // [group][128] pairs of scale and zero
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            float *to = reinterpret_cast<float *>(shared + S_AT) + (g * 128 + (tid & 127)) * 2;
+            if (tid < 128) to[0] = gr.half(g);
+            else to[1] = ZEROS ? static_cast<float>((gr.w[g / 2] >> (g % 2 * 16)) & 0xffu) : 8.0f;
+        }
+    };
+    f32x4 total[TN][TM];
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int r = 0; r < TM; ++r) total[t][r] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t exponent = exponent_of<XT>();
+    auto multiply_stage = [&]() {
+        const char *const xb = shared + (wm * (BM / WM) + fr) * XPITCH, *const qb = shared + Q_AT + (wn * TN * 16 + fr) * QPITCH + oct * 16;
+        const float *const sb = reinterpret_cast<const float *>(shared + S_AT) + (wn * TN * 16 + fr) * 2;
+        const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        u32x4 code[TN];
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+            code[t] = *reinterpret_cast<const u32x4 *>(qb + t * 16 * QPITCH);
+            regroup<G>(code[t]);
+        }
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            f32x4 part[TN][TM], xsum[TM];
+            float sv[TN], zv[TN];
+            f16x2 m1[TN], m16[TN];
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                const float2 v = *reinterpret_cast<const float2 *>(sb + (g * 128 + t * 16) * 2);
+                sv[t] = v.x;
+                zv[t] = v.y;
+                const _Float16 one = static_cast<_Float16>(-1024.0f - v.y), sixteen = static_cast<_Float16>(-64.0f - v.y);
+                m1[t] = (f16x2){one, one};
+                m16[t] = (f16x2){sixteen, sixteen};
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                u32x4 xf[TM];
+#pragma unroll
+                for (int r = 0; r < TM; ++r) xf[r] = *reinterpret_cast<const u32x4 *>(xb + r * 16 * XPITCH + k_of<G>(g * PER + j, oct) * 2);
+                if constexpr (XT == kXBf16) {
+#pragma unroll
+                    for (int r = 0; r < TM; ++r) xsum[r] = multiply<XT>(xf[r], ones, j == 0 ? none : xsum[r]);
+                }
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    const u32x4 w = widen<XT>(code[t][g * PER + j], exponent, m1[t], m16[t]);
+#pragma unroll
+                    for (int r = 0; r < TM; ++r) part[t][r] = multiply<XT>(xf[r], w, j == 0 ? none : part[t][r]);
+                }
+                __builtin_amdgcn_sched_barrier(0);           // (32 k's numbers at a time)
+            }
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int r = 0; r < TM; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float v = part[t][r][c];
+                        if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - zv[t], xsum[r][c], v);
+                        total[t][r][c] = __builtin_fmaf(sv[t], v, total[t][r][c]);
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const int stages = (a.K + 127) / 128;
+    load(0);
+    for (int s = 0; s < stages; ++s) {
+        place();
+        __syncthreads();
+        load(min(s + 1, stages - 1));                        // (the last one again, never used)
+        multiply_stage();
+        __syncthreads();
+    }
+
+    // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, its code row (wn * TN + t) * 16 + fr.  Out through
+    // LDS, as whole lines.
+    const int rows = row1 - row0;
+    if (gated || a.kind == kOutF16) {
+        _Float16 *const tile = reinterpret_cast<_Float16 *>(shared);
+        const int cols = gated ? 64 : 128, pitch = cols + 8;
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+            if (gated && t >= TN / 2) break;
+            const int col = gated ? wn * (8 * TN) + t * 16 + fr : (wn * TN + t) * 16 + fr;
+#pragma unroll
+            for (int r = 0; r < TM; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float v = total[t][r][c];
+                    if (gated) v = gated_by(a.act, v, total[(t + TN / 2) % TN][r][c]);
+                    tile[(wm * (BM / WM) + r * 16 + oct * 4 + c) * pitch + col] = static_cast<_Float16>(v);
+                }
+        }
+        __syncthreads();
+        // (width is a multiple of 32 here)
+        for (int p = tid; p < BM * cols / 8; p += 256) {
+            const int row = p / (cols / 8), col = p % (cols / 8) * 8;
+            if (row < rows && col0 + col < width)
+                *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + static_cast<size_t>(row0 + row) * width + col0 + col) =
+                    *reinterpret_cast<const u32x4 *>(tile + row * pitch + col);
+        }
+    } else {
+        // (sixteen columns of four rows per instruction: 64 bytes each)
+#pragma unroll
+        for (int r = 0; r < TM; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int row = wm * (BM / WM) + r * 16 + oct * 4 + c;
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    const int col = col0 + (wn * TN + t) * 16 + fr;
+                    if (row < rows && col < width)
+                        static_cast<float *>(a.out)[static_cast<size_t>(row0 + row) * width + col] = total[t][r][c];
+                }
+            }
+    }
+}
+
 // ---------------------------------------------------------------- host side
-void launch_q4(Q4Args a, int R, int E, int group, int x, int stage, hipStream_t st)
+// f(group, zeros or not) as constants
+template <typename F>
+void with_codes(const Q4Args &a, int group, F f)
+{
+    using std::integral_constant;
+    auto with_group = [&](auto zeros) {
+        if (group == 32) f(integral_constant<int, 32>{}, zeros);
+        else if (group == 64) f(integral_constant<int, 64>{}, zeros);
+        else f(integral_constant<int, 128>{}, zeros);
+    };
+    if (a.zero != nullptr) with_group(std::true_type{});
+    else with_group(std::false_type{});
+}
+
+template <int XT>
+void launch_q4_tiles(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
 {
     const bool gated = a.kind == kOutGated;
+    a.E = E;
+    a.tiles = ceil_div(gated ? a.N / 2 : a.N, gated ? 64 : 128);
+    with_codes(a, group, [&](auto g, auto zeros) {
+        auto launch = [&](auto bmc) {
+            constexpr int BM = decltype(bmc)::value, G = decltype(g)::value;
+            auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM>;
+            constexpr int lds = BM * 272 + 128 * 80 + 128 / G * 128 * 8;
+            static PerDeviceOnce once;
+            once.raise_lds(reinterpret_cast<const void *>(kern), lds);
+            const int64_t blocks = align_up(static_cast<size_t>(R / BM + std::min(R, E)) * a.tiles, 8);
+            hipEvent_t t0 = nullptr, t1 = nullptr;
+            if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
+            hipExtLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, st, t0, t1, 0, a);
+        };
+        if (R > 64 * E) launch(std::integral_constant<int, 128>{});
+        else if (R > 32 * E) launch(std::integral_constant<int, 64>{});
+        else launch(std::integral_constant<int, 32>{});
+    });
+}
+
+void launch_q4(Q4Args a, int R, int E, int group, int x, int stage, hipStream_t st)
+{
+    if (R > 16 * E) {
+        if (x == kXBf16) launch_q4_tiles<kXBf16>(a, R, E, group, stage, st);
+        else launch_q4_tiles<kXF16>(a, R, E, group, stage, st);
+        return;
+    }
+    const bool gated = a.kind == kOutGated;
     const int width = gated ? a.N / 2 : a.N, used = std::min(R, E), steps = ceil_div(a.K, 256);
-    // Column groups per block: the more of them the fewer reads of x, as long as the blocks occupy the compute units.
-    int nt = a.K % 256 == 0 ? 4 : 2;              // (with a part of a step left, four take more than 256 registers)
-    while (nt > (gated ? 2 : 1) && used * ceil_div(width, gated ? nt * 8 : nt * 16) < 256) nt /= 2;
+    // One or two column groups per block, and the depth shared out over as many wavefronts as occupy the compute units.
+    int nt = R > 2 || gated || used * ceil_div(width, 32) >= 256 ? 2 : 1;
     a.tiles = ceil_div(width, gated ? nt * 8 : nt * 16);
     a.E = E;
     int waves = 1;
-    while (waves < 8 && 2 * waves <= steps && used * a.tiles * waves < 4096) waves *= 2;
-    auto launch = [&](auto xt, auto g, auto zeros, auto ntc, auto tail) {
-        constexpr int NT = decltype(ntc)::value;
-        auto kern = q4_stream_kernel<decltype(xt)::value, decltype(g)::value, decltype(zeros)::value, NT, decltype(tail)::value>;
+    while (waves < 8 && 2 * waves <= steps && (used * a.tiles * waves < 1536 || (used * a.tiles * waves < 4096 && steps >= 24 * waves))) waves *= 2;
+    auto launch = [&](auto xt, auto g, auto zeros, auto ntc, auto xrc, auto tail) {
+        constexpr int NT = decltype(ntc)::value, XR = decltype(xrc)::value, OWN = XR * 528 + NT * 16 * 144;
+        auto kern = q4_stream_kernel<decltype(xt)::value, decltype(g)::value, decltype(zeros)::value, NT, XR, decltype(tail)::value>;
+        static PerDeviceOnce once;
+        once.raise_lds(reinterpret_cast<const void *>(kern), 8 * OWN);
         hipEvent_t t0 = nullptr, t1 = nullptr;
         if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
-        hipExtLaunchKernelGGL(kern, dim3(E * a.tiles), dim3(64 * waves), static_cast<size_t>(waves) * NT * 1024, st, t0, t1, 0, a);
+        hipExtLaunchKernelGGL(kern, dim3(E * a.tiles), dim3(64 * waves), static_cast<size_t>(waves) * OWN, st, t0, t1, 0, a);
     };
     using std::integral_constant;
-    auto with_tail = [&](auto xt, auto g, auto zeros, auto ntc) {
-        if (a.K % 256 == 0) launch(xt, g, zeros, ntc, std::false_type{});
-        else launch(xt, g, zeros, ntc, std::true_type{});
+    auto with_tail = [&](auto xt, auto g, auto zeros, auto ntc, auto xrc) {
+        if (a.K % 256 == 0) launch(xt, g, zeros, ntc, xrc, std::false_type{});
+        else launch(xt, g, zeros, ntc, xrc, std::true_type{});
     };
     auto with_nt = [&](auto xt, auto g, auto zeros) {
-        if (nt == 4) launch(xt, g, zeros, integral_constant<int, 4>{}, std::false_type{});
-        else if (nt == 2) with_tail(xt, g, zeros, integral_constant<int, 2>{});
-        else with_tail(xt, g, zeros, integral_constant<int, 1>{});
+        if (R > 2) with_tail(xt, g, zeros, integral_constant<int, 2>{}, integral_constant<int, 16>{});
+        else if (nt == 2) with_tail(xt, g, zeros, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+        else with_tail(xt, g, zeros, integral_constant<int, 1>{}, integral_constant<int, 2>{});
     };
-    auto with_zeros = [&](auto xt, auto g) {
-        if (a.zero != nullptr) with_nt(xt, g, std::true_type{});
-        else with_nt(xt, g, std::false_type{});
-    };
-    auto with_group = [&](auto xt) {
-        if (group == 32) with_zeros(xt, integral_constant<int, 32>{});
-        else if (group == 64) with_zeros(xt, integral_constant<int, 64>{});
-        else with_zeros(xt, integral_constant<int, 128>{});
-    };
-    if (x == kXBf16) with_group(integral_constant<int, kXBf16>{});
-    else with_group(integral_constant<int, kXF16>{});
+    with_codes(a, group, [&](auto g, auto zeros) {
+        if (x == kXBf16) with_nt(integral_constant<int, kXBf16>{}, g, zeros);
+        else with_nt(integral_constant<int, kXF16>{}, g, zeros);
+    });
 }
 
 bool bad_pointer(const void *p, const char *name, bool optional)
