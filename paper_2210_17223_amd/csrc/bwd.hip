@@ -1349,16 +1349,11 @@ moe_status bwd_resources(BwdResources **out)
     return MOE_OK;
 }
 
-// A side stream and its events for the weight gradients of an unchunked backward pass.  None of the above:
+// Side streams for the weight gradients of an unchunked backward pass.  None of the above:
 // a chunked pass that is being captured holds those in its capture until the capture ends, and a call
 // from outside may neither wait for them nor record on them; these are used outside capture only.  One per
 // caller's stream, so that a call does not queue behind another stream's work; a fifth takes over the one
 // used longest ago.
-struct SideStream {
-    hipStream_t caller = nullptr, stream = nullptr;
-    hipEvent_t dispatched = nullptr, hidden = nullptr, joined = nullptr;
-    uint64_t used = 0;                  // 0: not created yet
-};
 struct SideStreams {
     std::mutex enqueue;                 // held while a call enqueues on one of them
     uint64_t calls = 0;
@@ -1419,6 +1414,21 @@ bool overlaps_weight_grads(double work, hipStream_t st)
     }
     return status == hipStreamCaptureStatusNone;
 }
+
+}  // namespace
+
+SideStream *lend_side_stream(double work, hipStream_t st, std::unique_lock<std::mutex> &enqueue)
+{
+    int dev = 0;
+    if (!overlaps_weight_grads(work, st) || hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 16) return nullptr;
+    enqueue = std::unique_lock<std::mutex>(g_side[dev].enqueue);
+    SideStream *side = side_stream(g_side[dev], st);
+    if (side == nullptr) enqueue.unlock();
+    else count_path_call(kPathSideWeightGrads);
+    return side;
+}
+
+namespace {
 
 // The backward pass, cut like the forward: tokens in n_chunks contiguous parts, the row-grouped
 // GEMMs once per group of consecutive chunks (ffn_groups).  Gradient rows are dispatched to the
@@ -1514,14 +1524,8 @@ moe_status backward_t(const moe_shape &s, int n_chunks, const uint16_t *x, const
     if (n_chunks == 1) {
         SideStream *side = nullptr;
         std::unique_lock<std::mutex> enqueue;
-        int dev = 0;
-        if (overlaps_weight_grads(static_cast<double>(R) * d * h, st) && hipGetDevice(&dev) == hipSuccess &&
-            dev >= 0 && dev < 16) {
-            enqueue = std::unique_lock<std::mutex>(g_side[dev].enqueue);
-            side = side_stream(g_side[dev], st);
-        }
+        side = lend_side_stream(static_cast<double>(R) * d * h, st, enqueue);
         if (side == nullptr) {
-            if (enqueue.owns_lock()) enqueue.unlock();
             grad_dispatch(0, T, st);
             hidden_grads(0);
             input_grads(0);
@@ -1532,7 +1536,6 @@ moe_status backward_t(const moe_shape &s, int n_chunks, const uint16_t *x, const
             MOE_TRY_HIP(hipGetLastError());
             return combine_rc;
         }
-        count_path_call(kPathSideWeightGrads);
         // The two weight gradients on a side stream: dW2 beside dP from dye on, dW1 beside dxe and the
         // gate's gradients from dP on.
         auto enqueue_both = [&]() -> moe_status {

@@ -160,6 +160,15 @@ void prof_end(int stage, hipStream_t st);
 // timestamps without the launch gaps around it.  Both null when the stage is not timed.
 void prof_kernel_events(int stage, hipEvent_t *start, hipEvent_t *stop);
 
+// A side stream and its events for the weight gradients of an unchunked backward pass (bwd.hip).
+struct SideStream {
+    hipStream_t caller = nullptr, stream = nullptr;
+    hipEvent_t dispatched = nullptr, hidden = nullptr, joined = nullptr;
+    uint64_t used = 0;                  // 0: not created yet
+};
+// The one of `st`, held by `enqueue` while the caller enqueues on it; NULL where weight gradients are to run in order on `st`.
+SideStream *lend_side_stream(double work, hipStream_t st, std::unique_lock<std::mutex> &enqueue);
+
 // ---- kernel launchers (each only enqueues on `st`) ---------------------------
 // when seg_cnt is not NULL the per-segment expert histogram of the dispatch plan is
 // produced in the same pass

@@ -933,12 +933,48 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
         hid = w.hid;
     }
     const uint16_t *xeb = static_cast<const uint16_t *>(xe), *dyeb = static_cast<const uint16_t *>(dye);
-    launch_dh(*s, dyeb, static_cast<const uint16_t *>(W2), static_cast<const uint16_t *>(pre), w.dGU, w.lists.gp[0],
-              w.lists.items[0], st);
-    launch_dxe(*s, w.dGU, static_cast<const uint16_t *>(W13), static_cast<uint16_t *>(dxe), w.lists.gp[1], w.lists.items[1], st);
-    launch_weight_grad_bf16(true, static_cast<const uint16_t *>(hid), dyeb, static_cast<uint16_t *>(dW2), offsets, s->E, h, d, R,
-                            kStageBwdWgrad2, st);
-    launch_weight_grad_bf16(false, xeb, w.dGU, static_cast<uint16_t *>(dW13), offsets, s->E, d, 2 * h, R, kStageBwdWgrad1, st);
+    auto hidden_grads = [&]() {
+        launch_dh(*s, dyeb, static_cast<const uint16_t *>(W2), static_cast<const uint16_t *>(pre), w.dGU, w.lists.gp[0],
+                  w.lists.items[0], st);
+    };
+    auto input_grads = [&]() {
+        launch_dxe(*s, w.dGU, static_cast<const uint16_t *>(W13), static_cast<uint16_t *>(dxe), w.lists.gp[1], w.lists.items[1], st);
+    };
+    auto weight_grad2 = [&](hipStream_t q) {
+        launch_weight_grad_bf16(true, static_cast<const uint16_t *>(hid), dyeb, static_cast<uint16_t *>(dW2), offsets, s->E, h, d,
+                                R, kStageBwdWgrad2, q);
+    };
+    auto weight_grad1 = [&](hipStream_t q) {
+        launch_weight_grad_bf16(false, xeb, w.dGU, static_cast<uint16_t *>(dW13), offsets, s->E, d, 2 * h, R, kStageBwdWgrad1, q);
+    };
+    std::unique_lock<std::mutex> enqueue;
+    SideStream *side = lend_side_stream(static_cast<double>(R) * d * h, st, enqueue);
+    if (side == nullptr) {
+        hidden_grads();
+        input_grads();
+        weight_grad2(st);
+        weight_grad1(st);
+        MOE_TRY_HIP(hipGetLastError());
+        return MOE_OK;
+    }
+    // dW2 beside dH, dW13 beside dxe
+    auto enqueue_both = [&]() -> moe_status {
+        MOE_TRY_HIP(hipEventRecord(side->dispatched, st));
+        MOE_TRY_HIP(hipStreamWaitEvent(side->stream, side->dispatched, 0));
+        hidden_grads();
+        weight_grad2(side->stream);
+        MOE_TRY_HIP(hipEventRecord(side->hidden, st));
+        MOE_TRY_HIP(hipStreamWaitEvent(side->stream, side->hidden, 0));
+        input_grads();
+        weight_grad1(side->stream);
+        return MOE_OK;
+    };
+    rc = enqueue_both();
+    // (joined also after a failure part-way)
+    hipError_t je = hipEventRecord(side->joined, side->stream);
+    if (je == hipSuccess) je = hipStreamWaitEvent(st, side->joined, 0);
+    if (rc != MOE_OK) return rc;
+    if (je != hipSuccess) return hip_fail(je, "joining the side stream");
     MOE_TRY_HIP(hipGetLastError());
     return MOE_OK;
 }

@@ -61,6 +61,19 @@ def moe_gated_backward_workspace_bytes(s: Shape) -> int:
     return int(_lib().moe_gated_backward_workspace_bytes(C.byref(s)))
 
 
+_sizes = {}
+
+
+def _sizes_of(s: Shape):
+    """Rows and bytes that depend on the shape's values alone: (rows, W13p, W2p, workspace)."""
+    key = bytes(s)
+    if key not in _sizes:
+        if len(_sizes) >= 1024:
+            _sizes.clear()
+        _sizes[key] = (moe_max_rows(s), moe_gated_packed_bytes(s), moe_packed_weight_bytes(s), moe_gated_workspace_bytes(s))
+    return _sizes[key]
+
+
 def moe_pack_gated_weights(s: Shape, W13, W2, W13p, W2p, stream=None) -> None:
     n, dt = s.E * s.d_model * s.d_ff, s.torch_dtype
     _check(_lib().moe_pack_gated_weights(
@@ -70,13 +83,12 @@ def moe_pack_gated_weights(s: Shape, W13, W2, W13p, W2p, stream=None) -> None:
 
 
 def moe_gated_ffn(s: Shape, xe, offsets, W13p, W2p, ye, pre, hid, workspace, stream=None) -> None:
-    rows, h = moe_max_rows(s), s.d_ff
+    (rows, n13, n2, nw), d, h = _sizes_of(s), s.d_model, s.d_ff
     _check(_lib().moe_gated_ffn(
-        C.byref(s), arg(xe, s.torch_dtype, rows * s.d_model, "xe"), arg(offsets, torch.int32, s.E + 1, "offsets"),
-        arg(W13p, torch.uint8, moe_gated_packed_bytes(s), "W13p"),
-        arg(W2p, torch.uint8, moe_packed_weight_bytes(s), "W2p"), arg(ye, s.ye_dtype, rows * s.d_model, "ye"),
-        opt(pre, torch.float16, rows * 2 * h, "pre"), opt(hid, torch.float16, rows * h, "hid"),
-        arg(workspace, torch.uint8, moe_gated_workspace_bytes(s), "workspace"), raw_stream(stream, xe)))
+        C.byref(s), arg(xe, s.torch_dtype, rows * d, "xe"), arg(offsets, torch.int32, s.E + 1, "offsets"),
+        arg(W13p, U8, n13, "W13p"), arg(W2p, U8, n2, "W2p"), arg(ye, s.ye_dtype, rows * d, "ye"),
+        opt(pre, F16, rows * 2 * h, "pre"), opt(hid, F16, rows * h, "hid"), arg(workspace, U8, nw, "workspace"),
+        raw_stream(stream, xe)))
 
 
 def moe_gated_ffn_backward(s: Shape, xe, offsets, W13, W2, W13p, pre, hid, dye, dxe, dW13, dW2, workspace,
