@@ -3,10 +3,13 @@
 //
 // All of it is bound by HBM: a row is read once, stays in registers through both norms, and is written once.  TPR threads
 // (a wavefront, or a block) own a row, EPT of its columns each; a run of consecutive rows is one group of TPR threads' work,
-// which keeps the vectors (weights, biases, gates) in registers and has the next row's loads on their way while it reduces
-// this one's.  Statistics are fp32: the mean first, then the sum of squares around it, from the registers.
+// which keeps the vectors (weights, biases, gates) in registers; the forward pass has the next row's loads on their way
+// while it reduces this one's.  Statistics are fp32: the mean first, then the sum of squares around it, from the registers.
 // Backward: the vector gradients of a run are summed in registers and leave as one row of partial sums per run, which a
 // second kernel adds up in a fixed order (no atomics: the same bits every time).
+// Measured: forward, 32768 x 2048, fp32 x and z, bf16 next (0.94 GB) 188 us, 5.0 TB/s; 16384 x 4096, bf16 throughout, layer
+// (0.54 GB) 106 us, 5.1 TB/s, its backward pass (0.81 GB, and 42 MB of partial sums both ways) 195 + 9 us, 4.3 TB/s.  A plain
+// copy reaches 4.5 to 4.6 TB/s on these cards.
 #include "common.h"
 #include "moe_norm.h"
 
@@ -277,8 +280,9 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
 // of a gate whose rows begin in an earlier run, and of one whose rows begin here and go on in the next.
 enum { kDwNext = 0, kDbNext, kDw, kDb, kGateFrom, kGateOn, kAfterSlots, kBeforeSlots = 2 };
 
-template <int RES, int Z, int TPR, int EPT>
-__global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel(NormArgs a)
+// BIAS: the sums of dnext and D themselves are wanted (a norm has a bias, or its gradient was asked for).
+template <int RES, int Z, int TPR, int EPT, bool BIAS>
+__global__ __launch_bounds__(TPR == kWave ? 256 : TPR, TPR == kWave ? 3 : TPR <= 512 ? 4 : 1) void norm_backward_kernel(NormArgs a)
 {
     constexpr bool AFTER = Z >= 0;
     constexpr int ZT = AFTER ? Z : kF32, VEC = row_vec(RES, Z), NV = EPT / VEC;
@@ -302,8 +306,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
     }
     Piece<RES, VEC> rr[NV], drr[NV];
     Piece<ZT, VEC> zr[NV];
-    Piece<kF32, VEC> dnf[NV];
-    Piece<kB16, VEC> dnb[NV];
+    Piece<kF32, VEC> dnr[NV];                      // (of bf16: the first half)
     auto fetch = [&](int i) {
         const size_t at = static_cast<size_t>(i) * d;
         const char *r = static_cast<const char *>(a.r) + at * RB, *dr = static_cast<const char *>(a.dr) + at * RB;
@@ -317,15 +320,19 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
         const char *dn = static_cast<const char *>(a.dnext) + at * (a.next_f32 ? 4 : 2);
         if (a.next_f32) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) dnf[v].load(dn, col[v]);
+            for (int v = 0; v < NV; ++v) dnr[v].load(dn, col[v]);
         } else {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) dnb[v].load(dn, col[v]);
+            for (int v = 0; v < NV; ++v) {
+                Piece<kB16, VEC> p;
+                p.load(dn, col[v]);
+#pragma unroll
+                for (int c = 0; c < VEC / 2; ++c) dnr[v].w[c] = p.w[c];
+            }
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v) drr[v].load(dr, col[v]);
     };
-    fetch(i0);
     auto vector = [&](const float *p, float other, float (&out)[NV][VEC]) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -419,16 +426,16 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
     bool left = false;                             // dw and db hold something already
     for (int i = i0; i < i1; ++i) {
         float r[NV][VEC], z[NV][VEC], D[NV][VEC], u[NV][VEC], f[2];
+        fetch(i);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 r[v][e] = in[v] ? rr[v].at(e) : 0.0f;
                 if constexpr (AFTER) z[v][e] = in[v] ? zr[v].at(e) : 0.0f;
-                u[v][e] = in[v] ? (a.next_f32 ? dnf[v].at(e) : dnb[v].at(e)) : 0.0f;
+                u[v][e] = in[v] ? (a.next_f32 ? dnr[v].at(e) : __uint_as_float(e & 1 ? dnr[v].w[e / 2] & 0xffff0000u : dnr[v].w[e / 2] << 16)) : 0.0f;
                 D[v][e] = in[v] ? drr[v].at(e) : 0.0f;
             }
-        if (i + 1 < i1) fetch(i + 1);
         if constexpr (AFTER) {
             if (i >= group_end) {
                 group = a.gate_tokens != 0 ? i / a.gate_tokens : 0;
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 dwn[v][e] = __builtin_fmaf(u[v][e], r[v][e], dwn[v][e]);
-                dbn[v][e] += u[v][e];
+                if constexpr (BIAS) dbn[v][e] += u[v][e];
                 u[v][e] *= wn[v][e];
             }
         through(u, r, f[0]);
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     dz_sum[v][e] = __builtin_fmaf(D[v][e], z[v][e], dz_sum[v][e]);
-                    d_sum[v][e] += D[v][e];
+                    if constexpr (BIAS) d_sum[v][e] += D[v][e];
                     D[v][e] *= wa[v][e];
                 }
             through(D, z, f[1]);
@@ -490,7 +497,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
                         d_sum[v][e] = g[v][e] * s0;
                     }
                 leave(own + kDw * d, dz_sum, left);
-                leave(own + kDb * d, d_sum, left);
+                if constexpr (BIAS) leave(own + kDb * d, d_sum, left);
                 left = true;
                 if (a.dgate != nullptr) {
                     if (group_begin < i0) leave(own + kGateFrom * d, w, false);
@@ -503,7 +510,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_backward_kernel
         }
     }
     leave(own + kDwNext * d, dwn, false);
-    leave(own + kDbNext * d, dbn, false);
+    if constexpr (BIAS) leave(own + kDbNext * d, dbn, false);
 }
 
 // Sums over the runs, 64 columns a block, 16 runs at a time: blockIdx.y < 4 the vectors, behind them the gates whose
@@ -660,14 +667,29 @@ moe_status launch_norm_backward(const moe_norm_shape &n, NormArgs a, bool after,
     with_types(n, after, [&](auto res, auto z) {
         auto launch = [&](auto tpr, auto ept) {
             constexpr int TPR = decltype(tpr)::value;
-            hipLaunchKernelGGL((norm_backward_kernel<decltype(res)::value, decltype(z)::value, TPR, decltype(ept)::value>),
-                               dim3(TPR == kWave ? ceil_div(runs, 4) : runs), dim3(TPR == kWave ? 256 : TPR), 0, st, a);
+            auto run = [&](auto bias) {
+                hipLaunchKernelGGL((norm_backward_kernel<decltype(res)::value, decltype(z)::value, TPR, decltype(ept)::value, decltype(bias)::value>),
+                                   dim3(TPR == kWave ? ceil_div(runs, 4) : runs), dim3(TPR == kWave ? 256 : TPR), 0, st, a);
+            };
+            if (a.b != nullptr || out[kDbNext] != nullptr || out[kDb] != nullptr) run(std::true_type{});
+            else run(std::false_type{});
         };
         using std::integral_constant;
-        if (n.d <= 512) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-        else if (n.d <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 8>{});
-        else if (n.d <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 16>{});
-        else if (n.d <= 8192) launch(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+        // As few columns per thread as a block of 1024 allows: without the next row's loads on their way in registers
+        // and with at most 128 of these, other wavefronts' rows cover a row's latency (16384 rows of 4096, bf16 throughout,
+        // layer, with sixteen columns per thread and a row ahead 296 us, with eight 313, without the row ahead 195; fp32
+        // throughout with eight columns 425, with four 358).
+        if constexpr (row_vec(decltype(res)::value, decltype(z)::value) == 4) {
+            if (n.d <= 256) return launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+            if (n.d <= 1024) return launch(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+            if (n.d <= 2048) return launch(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+            if (n.d <= 4096) return launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+        } else {
+            if (n.d <= 512) return launch(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+            if (n.d <= 2048) return launch(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+            if (n.d <= 4096) return launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+        }
+        if (n.d <= 8192) launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
         else launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
     });
     NormReduceArgs q = {};
