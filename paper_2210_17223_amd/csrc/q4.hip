@@ -27,6 +27,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
+#include "gemm_w4.h"
+
 enum { kXBf16 = 1, kXF16 = 2 };
 enum { kOutF32 = 0, kOutF16, kOutGated };
 
@@ -163,6 +165,8 @@ struct Q4Args {
     void *out;
     int E, N, K, kind, act;                // kind kOut...; kOutGated: N = 2 h rows of codes, out [rows, h]
     int tiles;                             // column tiles of an expert
+    const float *row_scale;                // of the block's first product on many rows: what x was divided by
+    bool reorder_out;                      // kOutGated: out in the codes' order, for the second product
 };
 
 __device__ __forceinline__ float gated_by(int act, float g, float u)
@@ -397,8 +401,43 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
 }
 
 // ---------------------------------------------------------------- many rows per expert
-// BM x 128 tiles (128 rows of codes: columns, or 64 gates and their values), four wavefronts of 64 x 64 (BM = 128), 64 x 32
-// or 32 x 32, two blocks a compute unit.  Stages of 128: x (in the codes' order), codes, scales and zeros of the next one are on
+// The block's tile of BM rows by a column tile: an expert's tiles row by row inside a column, experts one after the other, an
+// eighth of all per XCD.  False: none.
+template <int BM>
+__device__ __forceinline__ bool own_tile(const Q4Args &a, int lane, int &expert, int &row0, int &row1, int &column)
+{
+    const int e = min(lane, a.E - 1), first = a.offsets[e], end = lane < a.E ? a.offsets[e + 1] : first;
+    const int mt = end > first ? (end - first + BM - 1) / BM : 0;
+    int sum = mt * a.tiles;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int v = __shfl_up(sum, d);
+        if (lane >= d) sum += v;
+    }
+    const int total = __builtin_amdgcn_readlane(sum, 63), per_xcd = (total + 7) / 8;
+    const int slot = blockIdx.x / 8, index = blockIdx.x % 8 * per_xcd + slot;
+    if (slot >= per_xcd || index >= total) return false;
+    expert = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
+    const int tiles = __builtin_amdgcn_readlane(mt, expert);
+    const int within = index - (__builtin_amdgcn_readlane(sum, expert) - tiles * a.tiles);
+    row0 = __builtin_amdgcn_readlane(first, expert) + within % tiles * BM;
+    row1 = min(row0 + BM, __builtin_amdgcn_readlane(end, expert));
+    column = within / tiles;
+    return true;
+}
+// Row of the expert's codes that lies in row i of a tile's 128, of wavefronts of TN column groups each: of a gated tile half of
+// a wavefront's groups are gates, half the values of the same columns.
+template <int TN>
+__device__ __forceinline__ int tile_code_row(bool gated, int i, int col0, int width)
+{
+    if (!gated) return min(col0 + i, width - 1);
+    const int w = i / (16 * TN), t = i / 16 % TN;
+    return min(col0 + w * (8 * TN) + t % (TN / 2) * 16 + i % 16, width - 1) + (t >= TN / 2 ? width : 0);
+}
+// Where element e of eight lies in the codes' order
+__device__ __forceinline__ int widened_place(int e) { return (e & ~7) | (e & 3) << 1 | (e >> 2 & 1); }
+
+// The linear map on BM x 128 tiles, four wavefronts of 64 x 64 (BM = 128), 64 x 32 or 32 x 32, two blocks a compute unit.  Stages of 128: x (in the codes' order), codes, scales and zeros of the next one are on
 // their way in registers while this one, in LDS, is multiplied; one block multiplies while the other moves them there.  A group's sums have accumulators of their own; behind the
 // group they are scaled into the totals, four instructions for each tile of 16 x 16 and group beside its G / 32 matrix
 // instructions (and in bf16 four more for the zeros): bound by the issue of both.  Each wavefront widens its own columns'
@@ -414,40 +453,16 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
-    const bool gated = a.kind == kOutGated;
-    const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
+    const int width = a.N, KG = a.K / G, KB = a.K / 2;
 
-    // The block's tile: an expert's tiles row by row inside a column, experts one after the other, an eighth of all per XCD.
     int expert, row0, row1, col0;
-    {
-        const int e = min(lane, a.E - 1), first = a.offsets[e], end = lane < a.E ? a.offsets[e + 1] : first;
-        const int mt = end > first ? (end - first + BM - 1) / BM : 0;
-        int sum = mt * a.tiles;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int v = __shfl_up(sum, d);
-            if (lane >= d) sum += v;
-        }
-        const int total = __builtin_amdgcn_readlane(sum, 63), per_xcd = (total + 7) / 8;
-        const int slot = blockIdx.x / 8, index = blockIdx.x % 8 * per_xcd + slot;
-        if (slot >= per_xcd || index >= total) return;
-        expert = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
-        const int rows_mt = __builtin_amdgcn_readlane(mt, expert);
-        const int within = index - (__builtin_amdgcn_readlane(sum, expert) - rows_mt * a.tiles);
-        const int r0 = __builtin_amdgcn_readlane(first, expert);
-        row0 = r0 + within % rows_mt * BM;
-        row1 = min(row0 + BM, __builtin_amdgcn_readlane(end, expert));
-        col0 = within / rows_mt * (gated ? 64 : 128);
-    }
+    if (!own_tile<BM>(a, lane, expert, row0, row1, col0)) return;
+    col0 *= 128;
 
     // staging: piece p = tid + 256 q; x: row p / 16 of the tile, codes: row p / 4
     const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(row1 - row0) * a.K * 2u, 0x00020000);
-    auto code_row = [&](int i) {                             // row of the expert's codes that lies in row i of the tile
-        if (!gated) return min(col0 + i, width - 1);
-        const int w = i / (16 * TN), t = i / 16 % TN;
-        return min(col0 + w * (8 * TN) + t % (TN / 2) * 16 + i % 16, width - 1) + (t >= TN / 2 ? width : 0);
-    };
+    auto code_row = [&](int i) { return min(col0 + i, width - 1); };
     const uint8_t *q_src[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -515,13 +530,14 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
             regroup<G>(code[t]);
         }
 #pragma unroll
-        for (int g = 0; g < GS; ++g) {
-            f32x4 part[TN][TM], xsum[TM];
-            float sv[TN], zv[TN];
-            f16x2 m1[TN], m16[TN];
+        for (int gt = 0; gt < GS * (TN / 2); ++gt) {             // two column groups at a time
+            const int g = gt / (TN / 2), t0 = gt % (TN / 2) * 2;
+            f32x4 part[2][TM], xsum[TM];
+            float sv[2], zv[2];
+            f16x2 m1[2], m16[2];
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                const float2 v = *reinterpret_cast<const float2 *>(sb + (g * 128 + t * 16) * 2);
+            for (int t = 0; t < 2; ++t) {
+                const float2 v = *reinterpret_cast<const float2 *>(sb + (g * 128 + (t0 + t) * 16) * 2);
                 sv[t] = v.x;
                 zv[t] = v.y;
                 const _Float16 one = static_cast<_Float16>(-1024.0f - v.y), sixteen = static_cast<_Float16>(-64.0f - v.y);
@@ -538,22 +554,22 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
                     for (int r = 0; r < TM; ++r) xsum[r] = multiply<XT>(xf[r], ones, j == 0 ? none : xsum[r]);
                 }
 #pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                    const u32x4 w = widen<XT>(code[t][g * PER + j], exponent, m1[t], m16[t]);
+                for (int t = 0; t < 2; ++t) {
+                    const u32x4 w = widen<XT>(code[t0 + t][g * PER + j], exponent, m1[t], m16[t]);
 #pragma unroll
                     for (int r = 0; r < TM; ++r) part[t][r] = multiply<XT>(xf[r], w, j == 0 ? none : part[t][r]);
                 }
                 __builtin_amdgcn_sched_barrier(0);           // (32 k's numbers at a time)
             }
 #pragma unroll
-            for (int t = 0; t < TN; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < TM; ++r)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         float v = part[t][r][c];
                         if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - zv[t], xsum[r][c], v);
-                        total[t][r][c] = __builtin_fmaf(sv[t], v, total[t][r][c]);
+                        total[t0 + t][r][c] = __builtin_fmaf(sv[t], v, total[t0 + t][r][c]);
                     }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -568,51 +584,244 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
         __syncthreads();
     }
 
+    // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, column (wn * TN + t) * 16 + fr: sixteen columns of four
+    // rows per instruction, 64 bytes each
+    const int rows = row1 - row0;
+#pragma unroll
+    for (int r = 0; r < TM; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int row = wm * (BM / WM) + r * 16 + oct * 4 + c;
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                const int col = col0 + (wn * TN + t) * 16 + fr;
+                if (row < rows && col < width)
+                    static_cast<float *>(a.out)[static_cast<size_t>(row0 + row) * width + col] = total[t][r][c];
+            }
+        }
+}
+
+// The rows of a block's first product, ready for the kernel below: fp16, in the codes' order, each row divided by a power of two
+// such that its largest value is at most 2^15 (bf16's eight digits are then exact down to 2^-29 of it, and below that off by
+// less than fp32 sums of such rows round).  A wavefront per row.
+__global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict__ x, const int32_t *__restrict__ offsets, int E,
+                                                      _Float16 *__restrict__ out, float *__restrict__ row_scale, int K)
+{
+    const int lane = lane_id(), row = blockIdx.x * 4 + threadIdx.x / kWave;
+    if (row >= offsets[E]) return;
+    const uint16_t *src = x + static_cast<size_t>(row) * K;
+    float most = 0.0f;
+    for (int k = lane * 8; k < K; k += kWave * 8) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(src + k);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(v[c] << 16)), fabsf(__uint_as_float(v[c] & 0xffff0000u))));
+    }
+#pragma unroll
+    for (int m = kWave / 2; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+    // 2^15 / 2^ceil(log2 most), within fp32's range of normal numbers; a row of zeros or without a largest value as it is
+    const int e = static_cast<int>(__float_as_uint(most) >> 23 & 0xff) - 127;
+    const bool plain = most == 0.0f || e == 128;
+    const int shift = plain ? 0 : min(max(14 - e, -126), 126);
+    const float by = __uint_as_float(static_cast<uint32_t>(shift + 127) << 23);
+    if (lane == 0) row_scale[row] = __uint_as_float(static_cast<uint32_t>(127 - shift) << 23);
+    for (int k = lane * 8; k < K; k += kWave * 8) {
+        const u32x4 v = reorder(*reinterpret_cast<const u32x4 *>(src + k));
+        u32x4 o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const f16x2 h = {static_cast<_Float16>(__uint_as_float(v[c] << 16) * by), static_cast<_Float16>(__uint_as_float(v[c] & 0xffff0000u) * by)};
+            o[c] = __builtin_bit_cast(uint32_t, h);
+        }
+        *reinterpret_cast<u32x4 *>(out + static_cast<size_t>(row) * K + k) = o;
+    }
+}
+
+// The tile kernel for rows that are ready: fp16 in the codes' order.  They go from memory straight into LDS, one stage ahead,
+// two places in turn; a row's sixteen 16-byte pieces are XOR-swizzled with the row on the global side, so that fragment reads
+// are free of bank conflicts.  Codes, scales and zeros of the next stage are on their way in registers, requested behind x, so that
+// the wait for them covers it.
+template <int G, bool ZEROS, int BM>
+__global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
+{
+    constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
+    constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
+    constexpr int X_BUF = BM * 256, Q_AT = 2 * X_BUF, S_AT = Q_AT + 128 * 64;
+    constexpr int XV = BM / 16;                              // loads of x per wavefront and stage, four rows each
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
+    const bool gated = a.kind == kOutGated;
+    const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
+    int expert, row0, row1, col0;
+    if (!own_tile<BM>(a, lane, expert, row0, row1, col0)) return;
+    expert = __builtin_amdgcn_readfirstlane(expert);
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    row1 = __builtin_amdgcn_readfirstlane(row1);
+    col0 = __builtin_amdgcn_readfirstlane(col0) * (gated ? 64 : 128);
+
+    // (rows past the expert's end: zeros that no load fetches)
+    const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(row1 - row0) * a.K * 2u, 0x00020000);
+    int x_src[XV], x_col[4];                                 // (a lane's piece repeats every four loads)
+#pragma unroll
+    for (int q = 0; q < XV; ++q) {
+        const int row = wave * (BM / 4) + q * 4 + (lane >> 4), piece = (lane & 15) ^ (row & 15);
+        x_src[q] = (row * a.K + piece * 8) * 2;
+        if (q < 4) x_col[q] = piece * 8;
+    }
+    const uint32_t x_dest = lds_address(shared) + wave * (X_BUF / 4);
+    auto load_x = [&](int s) {
+#pragma unroll
+        for (int q = 0; q < XV; ++q)
+            load_to_lds(rsx, s * 128 + x_col[q % 4] < a.K ? x_src[q] : 0x7ffffff0, x_dest + (s & 1) * X_BUF + q * 1024, s * 256);
+    };
+    const uint8_t *q_src[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        q_src[q] = a.q + (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, (tid + 256 * q) / 4, col0, width)) * KB;
+    const size_t g_row = (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, tid & 127, col0, width)) * KG;
+    u32x4 qr[2];
+    Run<GS * 2> gr;                                          // threads < 128: scales, others: zeros
+    auto load_codes = [&](int s) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + 256 * q) % 4 * 16, KB - 16));
+        if (tid < 128) {
+            if (s * GS + GS <= KG) {
+                gr.load(a.scale + g_row + s * GS);
+            } else {
+#pragma unroll
+                for (int g = 0; g < GS; ++g) gr.set16(g, s * GS + g < KG ? a.scale[g_row + min(s * GS + g, KG - 1)] : 0u);
+            }
+        } else if (ZEROS) {
+#pragma unroll
+            for (int g = 0; g < GS; ++g) gr.set16(g, a.zero[g_row + min(s * GS + g, KG - 1)]);
+        }
+    };
+    auto place = [&]() {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int p = tid + 256 * q, row = p / 4;
+            *reinterpret_cast<u32x4 *>(shared + Q_AT + row * 64 + ((p % 4) ^ (row >> 2 & 3)) * 16) = qr[q];
+        }
+        // [group][128] pairs of scale and -1024 - zero (twice, in fp16)
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(shared + S_AT) + (g * 128 + (tid & 127)) * 2;
+            if (tid < 128) {
+                to[0] = __float_as_uint(gr.half(g));
+            } else {
+                const _Float16 m = static_cast<_Float16>(-1024.0f - (ZEROS ? static_cast<float>((gr.w[g / 2] >> (g % 2 * 16)) & 0xffu) : 8.0f));
+                to[1] = __builtin_bit_cast(uint32_t, (f16x2){m, m});
+            }
+        }
+    };
+    f32x4 total[TN][TM];
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int r = 0; r < TM; ++r) total[t][r] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t exponent = exponent_of<kXF16>();
+    int x_off[4];                                            // the lane's four fragments of a row
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x_off[j] = (wm * (BM / WM) + fr) * 256 + (((k_of<G>(j, oct) >> 3) ^ fr) << 4);
+    const char *const qb = shared + Q_AT + (wn * TN * 16 + fr) * 64 + ((oct ^ (fr >> 2 & 3)) << 4);
+    const u32x2 *const sb = reinterpret_cast<const u32x2 *>(shared + S_AT) + wn * TN * 16 + fr;
+    auto multiply_stage = [&](int at) {
+        const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+        const f16x2 up = {static_cast<_Float16>(960.0f), static_cast<_Float16>(960.0f)};
+        u32x4 code[TN];
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+            code[t] = *reinterpret_cast<const u32x4 *>(qb + t * 16 * 64);
+            regroup<G>(code[t]);
+        }
+#pragma unroll
+        for (int g = 0; g < GS; ++g) {
+            f32x4 part[TN][TM];
+            u32x2 sz[TN];
+#pragma unroll
+            for (int t = 0; t < TN; ++t) sz[t] = sb[g * 128 + t * 16];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                u32x4 xf[TM];
+#pragma unroll
+                for (int r = 0; r < TM; ++r) xf[r] = *reinterpret_cast<const u32x4 *>(shared + at + x_off[g * PER + j] + r * 4096);
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    // (a scalar first: a bit cast of a vector's element is compiled as one of its first)
+                    const uint32_t bits = sz[t][1];
+                    const f16x2 m1 = __builtin_bit_cast(f16x2, bits);       // (m1 + 960, -64 - zero, is exact)
+                    const u32x4 w = widen<kXF16>(code[t][g * PER + j], exponent, m1, m1 + up);
+#pragma unroll
+                    for (int r = 0; r < TM; ++r) part[t][r] = multiply<kXF16>(xf[r], w, j == 0 ? none : part[t][r]);
+                }
+                __builtin_amdgcn_sched_barrier(0);           // (32 k's numbers at a time)
+            }
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int r = 0; r < TM; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) total[t][r][c] = __builtin_fmaf(__uint_as_float(sz[t][0]), part[t][r][c], total[t][r][c]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const int stages = (a.K + 127) / 128;
+    load_x(0);
+    load_codes(0);
+    for (int s = 0; s < stages; ++s) {
+        place();
+        MOE_VMCNT(0);                                        // (x of this stage is older than what place() has waited for)
+        __syncthreads();
+        if (s + 1 < stages) {
+            load_x(s + 1);
+            load_codes(s + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply_stage((s & 1) * X_BUF);
+        __syncthreads();
+    }
+
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, its code row (wn * TN + t) * 16 + fr.  Out through
     // LDS, as whole lines.
     const int rows = row1 - row0;
-    if (gated || a.kind == kOutF16) {
-        _Float16 *const tile = reinterpret_cast<_Float16 *>(shared);
-        const int cols = gated ? 64 : 128, pitch = cols + 8;
+    _Float16 *const tile = reinterpret_cast<_Float16 *>(shared);
+    const int cols = gated ? 64 : 128, pitch = cols + 8;
+    float by[TM][4];
 #pragma unroll
-        for (int t = 0; t < TN; ++t) {
-            if (gated && t >= TN / 2) break;
-            const int col = gated ? wn * (8 * TN) + t * 16 + fr : (wn * TN + t) * 16 + fr;
+    for (int r = 0; r < TM; ++r)
 #pragma unroll
-            for (int r = 0; r < TM; ++r)
+        for (int c = 0; c < 4; ++c)
+            by[r][c] = a.row_scale != nullptr ? a.row_scale[row0 + min(wm * (BM / WM) + r * 16 + oct * 4 + c, rows - 1)] : 1.0f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float v = total[t][r][c];
-                    if (gated) v = gated_by(a.act, v, total[(t + TN / 2) % TN][r][c]);
-                    tile[(wm * (BM / WM) + r * 16 + oct * 4 + c) * pitch + col] = static_cast<_Float16>(v);
-                }
-        }
-        __syncthreads();
-        // (width is a multiple of 32 here)
-        for (int p = tid; p < BM * cols / 8; p += 256) {
-            const int row = p / (cols / 8), col = p % (cols / 8) * 8;
-            if (row < rows && col0 + col < width)
-                *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + static_cast<size_t>(row0 + row) * width + col0 + col) =
-                    *reinterpret_cast<const u32x4 *>(tile + row * pitch + col);
-        }
-    } else {
-        // (sixteen columns of four rows per instruction: 64 bytes each)
+    for (int t = 0; t < TN; ++t) {
+        if (gated && t >= TN / 2) break;
+        int col = gated ? wn * (8 * TN) + t * 16 + fr : (wn * TN + t) * 16 + fr;
+        if (a.reorder_out) col = widened_place(col);
 #pragma unroll
         for (int r = 0; r < TM; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int row = wm * (BM / WM) + r * 16 + oct * 4 + c;
-#pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                    const int col = col0 + (wn * TN + t) * 16 + fr;
-                    if (row < rows && col < width)
-                        static_cast<float *>(a.out)[static_cast<size_t>(row0 + row) * width + col] = total[t][r][c];
-                }
+                float v = total[t][r][c] * by[r][c];
+                if (gated) v = gated_by(a.act, v, total[(t + TN / 2) % TN][r][c] * by[r][c]);
+                tile[(wm * (BM / WM) + r * 16 + oct * 4 + c) * pitch + col] = static_cast<_Float16>(v);
             }
+    }
+    __syncthreads();
+    // (width is a multiple of 32)
+    for (int p = tid; p < BM * cols / 8; p += 256) {
+        const int row = p / (cols / 8), col = p % (cols / 8) * 8;
+        if (row < rows && col0 + col < width)
+            *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + static_cast<size_t>(row0 + row) * width + col0 + col) =
+                *reinterpret_cast<const u32x4 *>(tile + row * pitch + col);
     }
 }
 
 // ---------------------------------------------------------------- host side
+unsigned parts_of(int n, int size) { return static_cast<unsigned>((n - 1) / size + 1); }
+
 // f(group, zeros or not) as constants
 template <typename F>
 void with_codes(const Q4Args &a, int group, F f)
@@ -627,37 +836,58 @@ void with_codes(const Q4Args &a, int group, F f)
     else with_group(std::false_type{});
 }
 
-template <int XT>
-void launch_q4_tiles(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
+// f(rows of a tile) as a constant: by the rows that an expert has on average
+template <typename F>
+void with_rows(int R, int E, F f)
+{
+    if (R > 64 * E) f(std::integral_constant<int, 128>{});
+    else if (R > 32 * E) f(std::integral_constant<int, 64>{});
+    else f(std::integral_constant<int, 32>{});
+}
+unsigned tile_blocks(int R, int E, int BM, int tiles)
+{
+    return static_cast<unsigned>(align_up((static_cast<size_t>(R) / BM + std::min(R, E)) * tiles, 8));
+}
+
+// rows that are ready
+void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
 {
     const bool gated = a.kind == kOutGated;
     a.E = E;
     a.tiles = ceil_div(gated ? a.N / 2 : a.N, gated ? 64 : 128);
     with_codes(a, group, [&](auto g, auto zeros) {
-        auto launch = [&](auto bmc) {
+        with_rows(R, E, [&](auto bmc) {
+            constexpr int BM = decltype(bmc)::value, G = decltype(g)::value;
+            auto kern = q4_ready_kernel<G, decltype(zeros)::value, BM>;
+            constexpr int lds = std::max(2 * BM * 256 + 128 * 64 + 128 / G * 128 * 8, BM * 136 * 2);
+            static PerDeviceOnce once;
+            once.raise_lds(reinterpret_cast<const void *>(kern), lds);
+            hipEvent_t t0, t1;
+            prof_kernel_events(stage, &t0, &t1);
+            hipExtLaunchKernelGGL(kern, dim3(tile_blocks(R, E, BM, a.tiles)), dim3(256), lds, st, t0, t1, 0, a);
+        });
+    });
+}
+
+template <int XT>
+void launch_q4_tiles(Q4Args a, int R, int E, int group, hipStream_t st)
+{
+    a.E = E;
+    a.tiles = ceil_div(a.N, 128);
+    with_codes(a, group, [&](auto g, auto zeros) {
+        with_rows(R, E, [&](auto bmc) {
             constexpr int BM = decltype(bmc)::value, G = decltype(g)::value;
             auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM>;
             constexpr int lds = BM * 272 + 128 * 80 + 128 / G * 128 * 8;
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
-            const int64_t blocks = align_up(static_cast<size_t>(R / BM + std::min(R, E)) * a.tiles, 8);
-            hipEvent_t t0 = nullptr, t1 = nullptr;
-            if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
-            hipExtLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, st, t0, t1, 0, a);
-        };
-        if (R > 64 * E) launch(std::integral_constant<int, 128>{});
-        else if (R > 32 * E) launch(std::integral_constant<int, 64>{});
-        else launch(std::integral_constant<int, 32>{});
+            hipLaunchKernelGGL(kern, dim3(tile_blocks(R, E, BM, a.tiles)), dim3(256), lds, st, a);
+        });
     });
 }
 
-void launch_q4(Q4Args a, int R, int E, int group, int x, int stage, hipStream_t st)
+void launch_q4_stream(Q4Args a, int R, int E, int group, int x, int stage, hipStream_t st)
 {
-    if (R > 16 * E) {
-        if (x == kXBf16) launch_q4_tiles<kXBf16>(a, R, E, group, stage, st);
-        else launch_q4_tiles<kXF16>(a, R, E, group, stage, st);
-        return;
-    }
     const bool gated = a.kind == kOutGated;
     const int width = gated ? a.N / 2 : a.N, used = std::min(R, E), steps = ceil_div(a.K, 256);
     // One or two column groups per block, and the depth shared out over as many wavefronts as occupy the compute units.
@@ -721,6 +951,9 @@ moe_status check_q4_block(const moe_shape *s)
     return MOE_OK;
 }
 
+// Whether a block's rows are made ready and its products run on tiles.
+bool many_rows(const moe_shape &s) { return moe_max_rows(&s) > 16 * static_cast<int64_t>(s.E); }
+
 }  // namespace
 }  // namespace moe
 
@@ -763,7 +996,10 @@ moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *of
     a.N = s->N;
     a.K = s->K;
     a.kind = kOutF32;
-    launch_q4(a, s->R, s->E, s->group, s->x, -1, static_cast<hipStream_t>(stream));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (s->R <= 16 * s->E) launch_q4_stream(a, s->R, s->E, s->group, s->x, -1, st);
+    else if (s->x == kXBf16) launch_q4_tiles<kXBf16>(a, s->R, s->E, s->group, st);
+    else launch_q4_tiles<kXF16>(a, s->R, s->E, s->group, st);
     MOE_TRY_HIP(hipGetLastError());
     return MOE_OK;
 }
@@ -771,7 +1007,10 @@ moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *of
 size_t moe_gated_q4_workspace_bytes(const moe_shape *s)
 {
     if (check_q4_block(s) != MOE_OK) return 0;
-    return align_up(static_cast<size_t>(moe_max_rows(s)) * s->d_ff * 2, 256);
+    const size_t R = static_cast<size_t>(moe_max_rows(s));
+    size_t bytes = align_up(R * s->d_ff * 2, 256);
+    if (many_rows(*s)) bytes += align_up(R * s->d_model * 2, 256) + align_up(R * 4, 256);
+    return bytes;
 }
 
 moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, const int32_t *offsets, const void *q13,
@@ -807,7 +1046,21 @@ moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, c
     a.K = s->d_model;
     a.kind = kOutGated;
     a.act = s->act;
-    launch_q4(a, R, s->E, group, kXBf16, kStageGemm1, st);
+    const bool many = many_rows(*s);
+    if (many) {
+        char *at = static_cast<char *>(workspace) + align_up(static_cast<size_t>(R) * s->d_ff * 2, 256);
+        float *row_scale = reinterpret_cast<float *>(at + align_up(static_cast<size_t>(R) * s->d_model * 2, 256));
+        hipLaunchKernelGGL(q4_rows_kernel, dim3(parts_of(R, 4)), dim3(256), 0, st, a.x, offsets, s->E, reinterpret_cast<_Float16 *>(at),
+                           row_scale, s->d_model);
+        a.x = reinterpret_cast<const uint16_t *>(at);
+        a.row_scale = row_scale;
+        a.reorder_out = true;
+        launch_q4_ready(a, R, s->E, group, kStageGemm1, st);
+    } else {
+        launch_q4_stream(a, R, s->E, group, kXBf16, kStageGemm1, st);
+    }
+    a.row_scale = nullptr;
+    a.reorder_out = false;
     a.x = static_cast<const uint16_t *>(workspace);
     a.q = static_cast<const uint8_t *>(q2);
     a.scale = static_cast<const uint16_t *>(scale2);
@@ -816,7 +1069,8 @@ moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, c
     a.N = s->d_model;
     a.K = s->d_ff;
     a.kind = kOutF16;
-    launch_q4(a, R, s->E, group, kXF16, kStageGemm2, st);
+    if (many) launch_q4_ready(a, R, s->E, group, kStageGemm2, st);
+    else launch_q4_stream(a, R, s->E, group, kXF16, kStageGemm2, st);
     MOE_TRY_HIP(hipGetLastError());
     return MOE_OK;
 }
