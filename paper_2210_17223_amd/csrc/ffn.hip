@@ -15,6 +15,7 @@
 // ye are kept in fp16.
 // fp32 layers: grouped_gemm_f32_kernel, on the fp32 matrix instruction.
 #include "activation.h"
+#include "block_tile.h"
 #include "common.h"
 #include "gated.h"
 #include <cstdio>
@@ -59,16 +60,23 @@ __device__ __forceinline__ float activate(float v)
 // the 32 x 32 tile (TM = TN = 1) where 64 x 64 leaves compute units without one.
 // Layer of 512 tokens, 128 x 256, 4 experts: the two GEMMs 4.5 and 4.8 us (10.2 and 15.5 with a 4 x 4
 // register block of v_fmac per thread).
+// items NULL: the tiles are found from `offsets` (block_tile.h).
 template <int ACT, int TM, int TN>
 __global__ __launch_bounds__(256) void grouped_gemm_f32_kernel(
     const float *__restrict__ A, const float *__restrict__ B, const float *__restrict__ bias,
-    float *__restrict__ C, const WorkItem *__restrict__ items, int N, int K)
+    float *__restrict__ C, const WorkItem *__restrict__ items, const int32_t *__restrict__ offsets, int E, int N, int K)
 {
-    const WorkItem tile = items[blockIdx.x];
-    if (tile.expert < 0) return;
+    constexpr int BM = 32 * TM, BN = 32 * TN, BK = 32, PD = 4;
+    WorkItem tile;
+    if (items != nullptr) {
+        tile = items[blockIdx.x];
+        if (tile.expert < 0) return;
+    } else {
+        if (!block_tile<BM>(offsets, E, (N + BN - 1) / BN, blockIdx.x, tile.expert, tile.row0, tile.row1, tile.n0)) return;
+        tile.n0 *= BN;
+    }
     const int n0 = tile.n0;
 
-    constexpr int BM = 32 * TM, BN = 32 * TN, BK = 32, PD = 4;
     constexpr int LDA = BK + 4, LDB = BN + 4;
     __shared__ __attribute__((aligned(16))) float As[2][BM * LDA];
     __shared__ __attribute__((aligned(16))) float Bs[2][BK * LDB];
@@ -418,21 +426,29 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grouped_gemm_staged_kernel(
 // first GEMM's 3072 are one round.  Items hold at most 32 rows: with 64 a
 // popular expert's wavefronts had three stages in flight instead of five and ended last.
 // The contraction order is that of the other 16-bit kernels (same bits).
+// items NULL: the tiles, of 16 columns each, are found from `offsets` (block_tile.h).
 // 16 tokens, 16 experts, k = 2, 768 x 3072, the two GEMMs: 16.3 and 14.5 us (17.0 and 18.4 with four
 // wavefronts a block; 17.2 and 25.7 with 128 x 128 and 64 x 256 tiles).
 template <bool F16, int ACT, bool KEEP, bool KTAIL>
 __global__ __launch_bounds__(64, 3) void grouped_gemm_stream_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, const float *__restrict__ bias,
     _Float16 *__restrict__ C, _Float16 *__restrict__ Pre, const WorkItem *__restrict__ items,
-    int N, int K, const int32_t *__restrict__ row_src, int row_div)
+    int N, int K, const int32_t *__restrict__ row_src, int row_div, const int32_t *__restrict__ offsets, int E)
 {
-    // the four blocks of an item are eight apart: one L2's
-    const WorkItem item = items[blockIdx.x / 32 * 8 + blockIdx.x % 8];
-    if (item.expert < 0) return;
+    WorkItem item;
+    int nw;
+    if (items != nullptr) {
+        // the four blocks of an item are eight apart: one L2's
+        item = items[blockIdx.x / 32 * 8 + blockIdx.x % 8];
+        if (item.expert < 0) return;
+        nw = item.n0 + static_cast<int>(blockIdx.x / 8 % 4) * 16;
+        if (nw >= N) return;
+    } else {
+        if (!block_tile<32>(offsets, E, (N + 15) / 16, blockIdx.x, item.expert, item.row0, item.row1, nw)) return;
+        nw *= 16;
+    }
     const int rows = item.row1 - item.row0;
     const int lane = threadIdx.x, fr = lane & 15, oct = lane >> 4;
-    const int nw = item.n0 + static_cast<int>(blockIdx.x / 8 % 4) * 16;
-    if (nw >= N) return;
     const int KT = (K + 63) / 64;
     const uint16_t *wp = W + (static_cast<size_t>(item.expert) * N + min(nw + fr, N - 1)) * K + oct * 8;
 
@@ -725,7 +741,7 @@ void launch_f32_pair(const moe_shape &s, const float *xe, const float *W1, const
         constexpr int A_ = decltype(act)::value;
         const GemmPlan &gp = w.gp[g];
         auto kern = gp.bm == 64 ? grouped_gemm_f32_kernel<A_, 2, 2> : grouped_gemm_f32_kernel<A_, 1, 1>;
-        hipLaunchKernelGGL(kern, dim3(gp.max_items), dim3(256), 0, st, A, B, bias, C, items, N, K);
+        hipLaunchKernelGGL(kern, dim3(gp.max_items), dim3(256), 0, st, A, B, bias, C, items, nullptr, 0, N, K);
     };
     prof_begin(kStageGemm1, st);
     launch(std::integral_constant<int, ACT>{}, 0, xe, W1, b1, H, it1, s.d_ff, s.d_model);
@@ -780,7 +796,7 @@ template <bool F16, typename TOut, int ACT, bool KEEP>
 void launch_mfma(const GemmPlan &gp, const uint16_t *A, const uint16_t *W, const float *bias,
                  TOut *C, _Float16 *pre, const WorkItem *items, int N, int K,
                  int stage, hipStream_t st, const int32_t *row_src = nullptr, int row_div = 1,
-                 uint64_t row_limit = 0)
+                 uint64_t row_limit = 0, const DirectTiles &direct = {})
 {
 #define MOE_MFMA_SHAPE(WM_, WN_, TM_, TN_)                                                        \
     launch_mfma_cfg<F16, TOut, ACT, KEEP, WM_, WN_, TM_, TN_>(A, W, bias, C, pre, items,            \
@@ -819,11 +835,11 @@ void launch_mfma(const GemmPlan &gp, const uint16_t *A, const uint16_t *W, const
     else if (gp.bn == 64) {
         auto kern = K % 64 == 0 ? grouped_gemm_stream_kernel<F16, ACT, KEEP, false>
                                 : grouped_gemm_stream_kernel<F16, ACT, KEEP, true>;
-        const int grid = gp.max_items * 4;
+        const unsigned grid = items != nullptr ? gp.max_items * 4 : block_tile_grid(direct.rows, direct.E, 32, (N + 15) / 16);
         hipEvent_t t0, t1;
         prof_kernel_events(stage, &t0, &t1);
         hipExtLaunchKernelGGL(kern, dim3(grid), dim3(64), 0, st, t0, t1, 0, A, W, bias, C, pre, items, N, K,
-                              row_src, row_div);
+                              row_src, row_div, direct.offsets, direct.E);
     }
     else if (gp.bm == 64)
         MOE_MFMA_SHAPE(1, 8, 2, 1);
@@ -1013,18 +1029,20 @@ moe_status launch_ffn(const moe_shape &s, const void *xe, const void *W1p, const
 
 // The second GEMM of a gated block
 moe_status launch_second_gemm(const moe_shape &s, const void *hidden, const void *W2p, void *ye, const GemmPlan &gp,
-                              const WorkItem *items, hipStream_t st)
+                              const WorkItem *items, const DirectTiles &direct, hipStream_t st)
 {
     if (s.dtype == MOE_BF16) {
         launch_mfma<true, _Float16, MOE_ACT_IDENTITY, false>(gp, static_cast<const uint16_t *>(hidden),
                                                              static_cast<const uint16_t *>(W2p), nullptr,
                                                              static_cast<_Float16 *>(ye), nullptr, items, s.d_model, s.d_ff,
-                                                             kStageGemm2, st);
+                                                             kStageGemm2, st, nullptr, 1, 0, direct);
     } else {
         auto kern = gp.bm == 64 ? grouped_gemm_f32_kernel<MOE_ACT_IDENTITY, 2, 2> : grouped_gemm_f32_kernel<MOE_ACT_IDENTITY, 1, 1>;
+        const unsigned grid = items != nullptr ? gp.max_items : block_tile_grid(direct.rows, direct.E, gp.bm, (s.d_model + gp.bn - 1) / gp.bn);
         prof_begin(kStageGemm2, st);
-        hipLaunchKernelGGL(kern, dim3(gp.max_items), dim3(256), 0, st, static_cast<const float *>(hidden),
-                           static_cast<const float *>(W2p), nullptr, static_cast<float *>(ye), items, s.d_model, s.d_ff);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, static_cast<const float *>(hidden),
+                           static_cast<const float *>(W2p), nullptr, static_cast<float *>(ye), items, direct.offsets, direct.E,
+                           s.d_model, s.d_ff);
         prof_end(kStageGemm2, st);
     }
     MOE_TRY_HIP(hipGetLastError());

@@ -9,6 +9,7 @@
 // The loops are the expert FFN's: tiles of 256 columns on gemm_w4_run.h's, 128 x 128 on gemm_w4_body.inc's, decode steps
 // straight from global memory.
 #include "activation.h"
+#include "block_tile.h"
 #include "gated.h"
 #include "moe_gated.h"
 
@@ -177,19 +178,18 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void gated_tile_kernel(
 
 // ---------------------------------------------------------------- first projections, few rows per expert
 // As grouped_gemm_stream_kernel of the expert FFN: a wavefront takes its fragments straight from global memory, here of 32
-// packed columns (sixteen gates and their values) and the rows of a 64-column item, PD stages of 64 on their way.
+// packed columns (sixteen gates and their values) and at most 32 rows, PD stages of 64 on their way; the block finds its tile
+// from the offsets.  32 rows, 16 experts, 768 x 2048: 15.8 us, 6.4 TB/s of weights (a list of tiles made first: 3 us and a launch
+// more).
 template <int ACT, bool KEEP, bool KTAIL>
 __global__ __launch_bounds__(64, 2) void gated_stream_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, _Float16 *__restrict__ H, _Float16 *__restrict__ Pre,
-    const WorkItem *__restrict__ items, int N, int K, int h)
+    const int32_t *__restrict__ offsets, int E, int N, int K, int h)
 {
-    // the two blocks of an item are eight apart: one L2's
-    const WorkItem item = items[blockIdx.x / 16 * 8 + blockIdx.x % 8];
-    if (item.expert < 0) return;
-    const int rows = item.row1 - item.row0;
+    WorkItem item;
+    if (!block_tile<32>(offsets, E, N / 32, blockIdx.x, item.expert, item.row0, item.row1, item.n0)) return;
+    const int rows = item.row1 - item.row0, nw = item.n0 * 32;
     const int lane = threadIdx.x, fr = lane & 15, oct = lane >> 4;
-    const int nw = item.n0 + static_cast<int>(blockIdx.x / 8 % 2) * 32;
-    if (nw >= N) return;
     const int KT = (K + 63) / 64;
     const uint16_t *wp[2];
 #pragma unroll
@@ -296,11 +296,11 @@ __device__ __forceinline__ float gate_value_f32(float v)
 // weight columns.  Tiles of 32 rows x 32 hidden columns, four wavefronts of 16 x 16, on the fp32 matrix instruction.
 template <int ACT>
 __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict__ A, const float *__restrict__ B,
-                                                        float *__restrict__ H, const WorkItem *__restrict__ items, int h, int K)
+                                                        float *__restrict__ H, const int32_t *__restrict__ offsets, int E, int h, int K)
 {
-    const WorkItem tile = items[blockIdx.x];
-    if (tile.expert < 0) return;
-    const int n0 = tile.n0;
+    WorkItem tile;
+    if (!block_tile<32>(offsets, E, (h + 31) / 32, blockIdx.x, tile.expert, tile.row0, tile.row1, tile.n0)) return;
+    const int n0 = tile.n0 * 32;
     constexpr int BM = 32, BN = 32, BK = 32, PD = 4, LDA = BK + 4, LDB = BN + 4;
     __shared__ __attribute__((aligned(16))) float As[2][BM * LDA];
     __shared__ __attribute__((aligned(16))) float Bs[2][2][BK * LDB];
@@ -611,12 +611,7 @@ void layout_gated(const moe_shape &s, void *base, GatedWorkspace *w)
     w->lists = Workspace{};
     const bool f32 = s.dtype == MOE_F32;
     if (f32) {
-        GemmPlan &gp = w->lists.gp[0];
-        gp.bm = gp.bn = 32;
-        gp.concurrent = 256;
-        gp.tiles_n = (s.d_ff + 31) / 32;
-        gp.max_row_tiles = static_cast<int32_t>((R + 31) / 32 + s.E);
-        gp.max_items = work_list_entries(gp);
+        w->lists.gp[0].max_items = 0;          // (both GEMMs find their tiles from the offsets)
     } else {
         w->lists.gp[0] = plan_gated(R, s.E, gated_packed_columns(s.d_ff), s.d_model, true, true, R);
     }
@@ -683,13 +678,13 @@ void with_activation(int act, F f)
 // H (and pre) of a bf16 layer
 template <int ACT, bool KEEP>
 void launch_first(const moe_shape &s, const uint16_t *xe, const uint16_t *W13p, uint16_t *H, uint16_t *pre, const GemmPlan &gp,
-                  const WorkItem *items, hipStream_t st)
+                  const WorkItem *items, const DirectTiles &direct, hipStream_t st)
 {
     const int N = gated_packed_columns(s.d_ff), K = s.d_model, h = s.d_ff;
     if (!gp.w4) {
         auto kern = K % 64 == 0 ? gated_stream_kernel<ACT, KEEP, false> : gated_stream_kernel<ACT, KEEP, true>;
-        launch_timed(kern, gp.max_items * 2, 64, 0, kStageGemm1, st, xe, W13p, reinterpret_cast<_Float16 *>(H),
-                     reinterpret_cast<_Float16 *>(pre), items, N, K, h);
+        launch_timed(kern, block_tile_grid(direct.rows, direct.E, 32, N / 32), 64, 0, kStageGemm1, st, xe, W13p,
+                     reinterpret_cast<_Float16 *>(H), reinterpret_cast<_Float16 *>(pre), direct.offsets, direct.E, N, K, h);
         return;
     }
     auto shape = [&](auto tail) {
@@ -714,19 +709,20 @@ void launch_first(const moe_shape &s, const uint16_t *xe, const uint16_t *W13p, 
 }
 
 void launch_first_gemm(const moe_shape &s, const void *xe, const void *W13p, void *H, void *pre, const GemmPlan &gp,
-                       const WorkItem *items, hipStream_t st)
+                       const WorkItem *items, const DirectTiles &direct, hipStream_t st)
 {
     with_activation(s.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
         if (s.dtype == MOE_F32)
-            launch_timed(gated_f32_kernel<ACT>, gp.max_items, 256, 0, kStageGemm1, st, static_cast<const float *>(xe),
-                         static_cast<const float *>(W13p), static_cast<float *>(H), items, s.d_ff, s.d_model);
+            launch_timed(gated_f32_kernel<ACT>, block_tile_grid(direct.rows, direct.E, 32, (s.d_ff + 31) / 32), 256, 0, kStageGemm1, st,
+                         static_cast<const float *>(xe), static_cast<const float *>(W13p), static_cast<float *>(H), direct.offsets,
+                         direct.E, s.d_ff, s.d_model);
         else if (pre != nullptr)
             launch_first<ACT, true>(s, static_cast<const uint16_t *>(xe), static_cast<const uint16_t *>(W13p),
-                                    static_cast<uint16_t *>(H), static_cast<uint16_t *>(pre), gp, items, st);
+                                    static_cast<uint16_t *>(H), static_cast<uint16_t *>(pre), gp, items, direct, st);
         else
             launch_first<ACT, false>(s, static_cast<const uint16_t *>(xe), static_cast<const uint16_t *>(W13p),
-                                     static_cast<uint16_t *>(H), nullptr, gp, items, st);
+                                     static_cast<uint16_t *>(H), nullptr, gp, items, direct, st);
     });
 }
 
@@ -878,13 +874,17 @@ moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offs
     GatedWorkspace w;
     layout_gated(*s, workspace, &w);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    prof_begin(kStageTiles, st);
-    rc = launch_items(*s, 1, 1, offsets, nullptr, w.lists, st);
-    prof_end(kStageTiles, st);
-    if (rc != MOE_OK) return rc;
+    const DirectTiles direct{offsets, s->E, moe_max_rows(s)};
+    const bool direct1 = takes_direct_tiles(*s, w.lists.gp[1]);
+    if (!takes_direct_tiles(*s, w.lists.gp[0]) || !direct1) {
+        prof_begin(kStageTiles, st);
+        rc = launch_items(*s, 1, 1, offsets, nullptr, w.lists, st);
+        prof_end(kStageTiles, st);
+        if (rc != MOE_OK) return rc;
+    }
     void *H = hid != nullptr ? hid : w.lists.hidden;
-    launch_first_gemm(*s, xe, W13p, H, pre, w.lists.gp[0], w.lists.items[0], st);
-    return launch_second_gemm(*s, H, W2p, ye, w.lists.gp[1], w.lists.items[1], st);
+    launch_first_gemm(*s, xe, W13p, H, pre, w.lists.gp[0], w.lists.items[0], direct, st);
+    return launch_second_gemm(*s, H, W2p, ye, w.lists.gp[1], direct1 ? nullptr : w.lists.items[1], direct, st);
 }
 
 size_t moe_gated_backward_workspace_bytes(const moe_shape *s)
@@ -928,7 +928,7 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
         // (writes the second list again, as it is)
         rc = launch_items(*s, 1, 1, offsets, nullptr, w.again, st);
         if (rc != MOE_OK) return rc;
-        launch_first_gemm(*s, xe, W13p, w.hid, w.pre, w.again.gp[0], w.again.items[0], st);
+        launch_first_gemm(*s, xe, W13p, w.hid, w.pre, w.again.gp[0], w.again.items[0], DirectTiles{offsets, s->E, R}, st);
         pre = w.pre;
         hid = w.hid;
     }

@@ -8,6 +8,7 @@
 //          (shared by all of a wavefront's columns)
 //   fp16   q - z by one packed subtraction (exact), no correction
 #include "activation.h"
+#include "block_tile.h"
 #include "gated.h"
 #include "moe_gated.h"
 
@@ -401,30 +402,6 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
 }
 
 // ---------------------------------------------------------------- many rows per expert
-// The block's tile of BM rows by a column tile: an expert's tiles row by row inside a column, experts one after the other, an
-// eighth of all per XCD.  False: none.
-template <int BM>
-__device__ __forceinline__ bool own_tile(const Q4Args &a, int lane, int &expert, int &row0, int &row1, int &column)
-{
-    const int e = min(lane, a.E - 1), first = a.offsets[e], end = lane < a.E ? a.offsets[e + 1] : first;
-    const int mt = end > first ? (end - first + BM - 1) / BM : 0;
-    int sum = mt * a.tiles;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int v = __shfl_up(sum, d);
-        if (lane >= d) sum += v;
-    }
-    const int total = __builtin_amdgcn_readlane(sum, 63), per_xcd = (total + 7) / 8;
-    const int slot = blockIdx.x / 8, index = blockIdx.x % 8 * per_xcd + slot;
-    if (slot >= per_xcd || index >= total) return false;
-    expert = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
-    const int tiles = __builtin_amdgcn_readlane(mt, expert);
-    const int within = index - (__builtin_amdgcn_readlane(sum, expert) - tiles * a.tiles);
-    row0 = __builtin_amdgcn_readlane(first, expert) + within % tiles * BM;
-    row1 = min(row0 + BM, __builtin_amdgcn_readlane(end, expert));
-    column = within / tiles;
-    return true;
-}
 // Row of the expert's codes that lies in row i of a tile's 128, of wavefronts of TN column groups each: of a gated tile half of
 // a wavefront's groups are gates, half the values of the same columns.
 template <int TN>
@@ -456,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
     const int width = a.N, KG = a.K / G, KB = a.K / 2;
 
     int expert, row0, row1, col0;
-    if (!own_tile<BM>(a, lane, expert, row0, row1, col0)) return;
+    if (!block_tile<BM>(a.offsets, a.E, a.tiles, blockIdx.x, expert, row0, row1, col0)) return;
     col0 *= 128;
 
     // staging: piece p = tid + 256 q; x: row p / 16 of the tile, codes: row p / 4
@@ -654,7 +631,7 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
     const bool gated = a.kind == kOutGated;
     const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
     int expert, row0, row1, col0;
-    if (!own_tile<BM>(a, lane, expert, row0, row1, col0)) return;
+    if (!block_tile<BM>(a.offsets, a.E, a.tiles, blockIdx.x, expert, row0, row1, col0)) return;
     expert = __builtin_amdgcn_readfirstlane(expert);
     row0 = __builtin_amdgcn_readfirstlane(row0);
     row1 = __builtin_amdgcn_readfirstlane(row1);
@@ -844,10 +821,6 @@ void with_rows(int R, int E, F f)
     else if (R > 32 * E) f(std::integral_constant<int, 64>{});
     else f(std::integral_constant<int, 32>{});
 }
-unsigned tile_blocks(int R, int E, int BM, int tiles)
-{
-    return static_cast<unsigned>(align_up((static_cast<size_t>(R) / BM + std::min(R, E)) * tiles, 8));
-}
 
 // rows that are ready
 void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
@@ -864,7 +837,7 @@ void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t s
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
             hipEvent_t t0, t1;
             prof_kernel_events(stage, &t0, &t1);
-            hipExtLaunchKernelGGL(kern, dim3(tile_blocks(R, E, BM, a.tiles)), dim3(256), lds, st, t0, t1, 0, a);
+            hipExtLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256), lds, st, t0, t1, 0, a);
         });
     });
 }
@@ -881,7 +854,7 @@ void launch_q4_tiles(Q4Args a, int R, int E, int group, hipStream_t st)
             constexpr int lds = BM * 272 + 128 * 80 + 128 / G * 128 * 8;
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
-            hipLaunchKernelGGL(kern, dim3(tile_blocks(R, E, BM, a.tiles)), dim3(256), lds, st, a);
+            hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256), lds, st, a);
         });
     });
 }
