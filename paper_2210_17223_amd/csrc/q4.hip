@@ -414,21 +414,64 @@ __device__ __forceinline__ int tile_code_row(bool gated, int i, int col0, int wi
 // Where element e of eight lies in the codes' order
 __device__ __forceinline__ int widened_place(int e) { return (e & ~7) | (e & 3) << 1 | (e >> 2 & 1); }
 
-// The linear map on BM x 128 tiles, four wavefronts of 64 x 64 (BM = 128), 64 x 32 or 32 x 32, two blocks a compute unit.  Stages of 128: x (in the codes' order), codes, scales and zeros of the next one are on
-// their way in registers while this one, in LDS, is multiplied; one block multiplies while the other moves them there.  A group's sums have accumulators of their own; behind the
-// group they are scaled into the totals, four instructions for each tile of 16 x 16 and group beside its G / 32 matrix
-// instructions (and in bf16 four more for the zeros): bound by the issue of both.  Each wavefront widens its own columns'
-// codes, seven instructions for eight of them, which feed BM / 32 matrix instructions.
-template <int XT, int G, bool ZEROS, int BM>
-__global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
+// LDS of the tile kernels' four wavefronts that work on a stage together
+constexpr int tile_lds(int bm, int group)
+{
+    return bm * 272 + 128 * 80 + 128 / group * 128 * 8;
+}
+constexpr int ready_lds(int bm, int group)
+{
+    const int stages = 2 * bm * 256 + 128 * 64 + 128 / group * 128 * 8, tile = bm * 136 * 2;
+    return stages > tile ? stages : tile;
+}
+// Where KS times four wavefronts share out a tile's depth, stage by stage in turn: the first four add up all sums, in a fixed
+// order (through LDS, behind a barrier after its last use).  False: not one of them.
+template <int KS, int TN, int TM>
+__device__ __forceinline__ bool join(f32x4 (&total)[TN][TM], char *shared, int pitch, int part_of, int tid)
+{
+    if constexpr (KS > 1) {
+        if (part_of > 0) {
+            f32x4 *const out = reinterpret_cast<f32x4 *>(shared + part_of * pitch) + tid;
+#pragma unroll
+            for (int i = 0; i < TN * TM; ++i) out[i * 256] = total[i / TM][i % TM];
+        }
+        __syncthreads();
+        if (part_of > 0) return false;
+#pragma unroll
+        for (int p = 1; p < KS; ++p) {
+            const f32x4 *const in = reinterpret_cast<const f32x4 *>(shared + p * pitch) + tid;
+#pragma unroll
+            for (int i = 0; i < TN * TM; ++i) {
+                const f32x4 v = in[i * 256];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) total[i / TM][i % TM][c] += v[c];
+            }
+        }
+    }
+    return true;
+}
+
+// The linear map on BM x 128 tiles, four wavefronts of 64 x 64 (BM = 128), 64 x 32 or 32 x 32.  Stages of 128: x (in the codes'
+// order), codes, scales and zeros of the next one are on their way in registers while this one, in LDS, is multiplied; KS times
+// four wavefronts, or several blocks, of a compute unit take turns at that.  A group's sums have accumulators of their own;
+// behind the group they are scaled into the totals, four instructions for each tile of 16 x 16 and group beside its G / 32 matrix
+// instructions (and in bf16 four more for the zeros).  Each wavefront widens its own columns' codes, seven instructions for eight
+// of them, which feed BM / 32 matrix instructions: bound by the issue of vector instructions, and with few tiles by the compute
+// units that have none.  4096 x 4096, group 128: 160 rows 19 us, 1000 rows 55 us (605 TFLOP/s); 8192 x 8192 from fp16, 6000
+// rows 1132 us (712 TFLOP/s).
+template <int XT, int G, bool ZEROS, int BM, int KS>
+__global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_tile_kernel(Q4Args a)
 {
     constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
     constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
     constexpr int XPITCH = 272, QPITCH = 80;                 // bytes of a row in LDS
     constexpr int XV = BM / 16;                              // 16-byte pieces of x per thread and stage
     constexpr int Q_AT = BM * XPITCH, S_AT = Q_AT + 128 * QPITCH;
-    extern __shared__ __attribute__((aligned(16))) char shared[];
-    const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    static_assert(KS == 1 || tile_lds(BM, G) >= BM * 128 * 4, "the sums lie there, too");
+    extern __shared__ __attribute__((aligned(16))) char all_shared[];
+    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    char *const shared = all_shared + part_of * tile_lds(BM, G);
+    const int tid = threadIdx.x & 255, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
     const int width = a.N, KG = a.K / G, KB = a.K / 2;
 
@@ -551,15 +594,16 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(Q4Args a)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    const int stages = (a.K + 127) / 128;
-    load(0);
-    for (int s = 0; s < stages; ++s) {
+    const int stages = (a.K + 127) / 128, turns = (stages + KS - 1) / KS;
+    load(part_of);
+    for (int i = 0; i < turns; ++i) {
         place();
         __syncthreads();
-        load(min(s + 1, stages - 1));                        // (the last one again, never used)
+        load(min(i + 1, turns - 1) * KS + part_of);          // (the last one again, never used; past K: zeros)
         multiply_stage();
         __syncthreads();
     }
+    if (!join<KS>(total, all_shared, tile_lds(BM, G), part_of, tid)) return;
 
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, column (wn * TN + t) * 16 + fr: sixteen columns of four
     // rows per instruction, 64 bytes each
@@ -615,18 +659,28 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
 }
 
 // The tile kernel for rows that are ready: fp16 in the codes' order.  They go from memory straight into LDS, one stage ahead,
-// two places in turn; a row's sixteen 16-byte pieces are XOR-swizzled with the row on the global side, so that fragment reads
-// are free of bank conflicts.  Codes, scales and zeros of the next stage are on their way in registers, requested behind x, so that
-// the wait for them covers it.
-template <int G, bool ZEROS, int BM>
-__global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
+// two places in turn; of a row's sixteen 16-byte pieces the one that quarter o of a wavefront reads with dword j lies at
+// 4 j + o, XOR-swizzled with the row, both done by the choice of the loads' addresses: fragment reads are free of bank conflicts
+// (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).  Codes, scales and zeros of the next stage
+// are on their way in registers, requested behind x, so that the wait for them covers it.
+// Bound by issue: beside 64 matrix instructions of a wavefront and stage stand 300 vector instructions (widening, scaling), and
+// a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, the two products, tiles of 64 rows: 380 + 215
+// us, 720 and 640 TFLOP/s; of 128 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector
+// instructions placed by hand between the matrix instructions 375 + 225; weights scaled before the product (no sums per group,
+// rounded to fp16) on four wavefronts and 128 x 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its
+// loads and numbers with nobody to step in.
+template <int G, bool ZEROS, int BM, int KS>
+__global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Args a)
 {
     constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
     constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
     constexpr int X_BUF = BM * 256, Q_AT = 2 * X_BUF, S_AT = Q_AT + 128 * 64;
     constexpr int XV = BM / 16;                              // loads of x per wavefront and stage, four rows each
-    extern __shared__ __attribute__((aligned(16))) char shared[];
-    const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    static_assert(KS == 1 || ready_lds(BM, G) >= BM * 128 * 4, "the sums lie there, too");
+    extern __shared__ __attribute__((aligned(16))) char all_shared[];
+    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    char *const shared = all_shared + part_of * ready_lds(BM, G);
+    const int tid = threadIdx.x & 255, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
     const bool gated = a.kind == kOutGated;
     const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
@@ -643,15 +697,15 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
     int x_src[XV], x_col[4];                                 // (a lane's piece repeats every four loads)
 #pragma unroll
     for (int q = 0; q < XV; ++q) {
-        const int row = wave * (BM / 4) + q * 4 + (lane >> 4), piece = (lane & 15) ^ (row & 15);
+        const int row = wave * (BM / 4) + q * 4 + (lane >> 4), at = (lane & 15) ^ (row & 15), piece = k_of<G>(at >> 2, at & 3) >> 3;
         x_src[q] = (row * a.K + piece * 8) * 2;
         if (q < 4) x_col[q] = piece * 8;
     }
     const uint32_t x_dest = lds_address(shared) + wave * (X_BUF / 4);
-    auto load_x = [&](int s) {
+    auto load_x = [&](int s, int place) {
 #pragma unroll
         for (int q = 0; q < XV; ++q)
-            load_to_lds(rsx, s * 128 + x_col[q % 4] < a.K ? x_src[q] : 0x7ffffff0, x_dest + (s & 1) * X_BUF + q * 1024, s * 256);
+            load_to_lds(rsx, s * 128 + x_col[q % 4] < a.K ? x_src[q] : 0x7ffffff0, x_dest + place * X_BUF + q * 1024, s * 256);
     };
     const uint8_t *q_src[2];
 #pragma unroll
@@ -702,7 +756,7 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
     const uint32_t exponent = exponent_of<kXF16>();
     int x_off[4];                                            // the lane's four fragments of a row
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x_off[j] = (wm * (BM / WM) + fr) * 256 + (((k_of<G>(j, oct) >> 3) ^ fr) << 4);
+    for (int j = 0; j < 4; ++j) x_off[j] = (wm * (BM / WM) + fr) * 256 + ((4 * j + oct) ^ fr) * 16;
     const char *const qb = shared + Q_AT + (wn * TN * 16 + fr) * 64 + ((oct ^ (fr >> 2 & 3)) << 4);
     const u32x2 *const sb = reinterpret_cast<const u32x2 *>(shared + S_AT) + wn * TN * 16 + fr;
     auto multiply_stage = [&](int at) {
@@ -745,26 +799,27 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    const int stages = (a.K + 127) / 128;
-    load_x(0);
-    load_codes(0);
-    for (int s = 0; s < stages; ++s) {
+    const int stages = (a.K + 127) / 128, turns = (stages + KS - 1) / KS;
+    load_x(part_of, 0);
+    load_codes(part_of);
+    for (int i = 0; i < turns; ++i) {
         place();
         MOE_VMCNT(0);                                        // (x of this stage is older than what place() has waited for)
         __syncthreads();
-        if (s + 1 < stages) {
-            load_x(s + 1);
-            load_codes(s + 1);
+        if (i + 1 < turns) {
+            load_x((i + 1) * KS + part_of, (i + 1) & 1);     // (past K: zeros)
+            load_codes((i + 1) * KS + part_of);
         }
         __builtin_amdgcn_sched_barrier(0);
-        multiply_stage((s & 1) * X_BUF);
+        multiply_stage((i & 1) * X_BUF);
         __syncthreads();
     }
+    const bool joined = join<KS>(total, all_shared, ready_lds(BM, G), part_of, tid);
 
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, its code row (wn * TN + t) * 16 + fr.  Out through
     // LDS, as whole lines.
     const int rows = row1 - row0;
-    _Float16 *const tile = reinterpret_cast<_Float16 *>(shared);
+    _Float16 *const tile = reinterpret_cast<_Float16 *>(all_shared);
     const int cols = gated ? 64 : 128, pitch = cols + 8;
     float by[TM][4];
 #pragma unroll
@@ -774,7 +829,7 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
             by[r][c] = a.row_scale != nullptr ? a.row_scale[row0 + min(wm * (BM / WM) + r * 16 + oct * 4 + c, rows - 1)] : 1.0f;
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
-        if (gated && t >= TN / 2) break;
+        if (!joined || (gated && t >= TN / 2)) break;
         int col = gated ? wn * (8 * TN) + t * 16 + fr : (wn * TN + t) * 16 + fr;
         if (a.reorder_out) col = widened_place(col);
 #pragma unroll
@@ -788,7 +843,7 @@ __global__ __launch_bounds__(256, 2) void q4_ready_kernel(Q4Args a)
     }
     __syncthreads();
     // (width is a multiple of 32)
-    for (int p = tid; p < BM * cols / 8; p += 256) {
+    for (int p = threadIdx.x; p < BM * cols / 8; p += 256 * KS) {
         const int row = p / (cols / 8), col = p % (cols / 8) * 8;
         if (row < rows && col0 + col < width)
             *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + static_cast<size_t>(row0 + row) * width + col0 + col) =
@@ -813,13 +868,32 @@ void with_codes(const Q4Args &a, int group, F f)
     else with_group(std::false_type{});
 }
 
-// f(rows of a tile) as a constant: by the rows that an expert has on average
+// f(rows of a tile, parts that its depth is shared out in) as constants.  Measured on either side of the lines, us:
+//  * Tiles of 32 rows leave the fewest compute units idle; widening the codes once for every 32 rows costs most where
+//    there are enough of larger tiles, too.  Block of 8 experts, 2048 x 8192, 32 / 64 rows a tile: 48 rows per expert 98 / 100,
+//    96 153 / 133; of 4, 1024 x 2048, where tiles are few: 300 46 / 48, 512 64 / 66.  Linear map 4096 x 4096 of 640 rows 48 / 51,
+//    of 1000 63 / 55; 2048 x 12000 of 160 35 / 43, of 320 52 / 45.
+//  * 64 / 128 rows, 8 experts, 2048 x 8192: 512 per expert 525 / 540, 1024 1017 / 985, 2048 2139 / 1958; 4096 x 4096 654 / 684,
+//    1247 / 1227, 2557 / 2297; linear map 2048 x 12000: 1000 rows 115 / 123, 2000 241 / 218.
+//  * Few blocks of 32 rows, depth in 1 / 2 / 4 parts: 192 blocks 25 / 20 / 19, 352 36 / 32 / 36, 470 35 / 32 / 37, 640 48 / 49 / 57.
 template <typename F>
-void with_rows(int R, int E, F f)
+void with_tile(int R, int E, int tiles, F f)
 {
-    if (R > 64 * E) f(std::integral_constant<int, 128>{});
-    else if (R > 32 * E) f(std::integral_constant<int, 64>{});
-    else f(std::integral_constant<int, 32>{});
+    using std::integral_constant;
+    const int64_t blocks = (R / 32 + (std::min(R, E) + 1) / 2) * static_cast<int64_t>(tiles);   // of 32 rows
+    if (R / 1024 >= E) f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+    else if (R / 64 >= E && blocks > 900) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (blocks > 512) f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (blocks > 256) f(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+    else f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+}
+// Whether rows go through the kernel for few of them: with tiles 128 columns wide on no more than a quarter of the compute units,
+// up to 32 per expert, else up to 16.  Stream / tiles, us: 20 and 40 rows of 4096 x 4096 12 / 18 and 17 / 18, of 8192 x 8192 22 / 37 and
+// 32 / 37, of 2048 x 12000 21 / 18 and 31 / 19.  The gated block (always 16): 8 experts of 2048 x 8192, 10, 14 and 18 rows each 51 / 72,
+// 78 / 72, 84 / 73; 4096 x 4096 63 / 97, 91 / 97, 98 / 97.
+bool few_rows(int R, int E, int tiles)
+{
+    return R <= 16 * E || (R <= 32 * E && std::min(R, E) * static_cast<int64_t>(tiles) <= 64);
 }
 
 // rows that are ready
@@ -829,15 +903,15 @@ void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t s
     a.E = E;
     a.tiles = ceil_div(gated ? a.N / 2 : a.N, gated ? 64 : 128);
     with_codes(a, group, [&](auto g, auto zeros) {
-        with_rows(R, E, [&](auto bmc) {
-            constexpr int BM = decltype(bmc)::value, G = decltype(g)::value;
-            auto kern = q4_ready_kernel<G, decltype(zeros)::value, BM>;
-            constexpr int lds = std::max(2 * BM * 256 + 128 * 64 + 128 / G * 128 * 8, BM * 136 * 2);
+        with_tile(R, E, a.tiles, [&](auto bmc, auto ksc) {
+            constexpr int BM = decltype(bmc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
+            auto kern = q4_ready_kernel<G, decltype(zeros)::value, BM, KS>;
+            constexpr int lds = KS * ready_lds(BM, G);
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
             hipEvent_t t0, t1;
             prof_kernel_events(stage, &t0, &t1);
-            hipExtLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256), lds, st, t0, t1, 0, a);
+            hipExtLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256 * KS), lds, st, t0, t1, 0, a);
         });
     });
 }
@@ -848,13 +922,13 @@ void launch_q4_tiles(Q4Args a, int R, int E, int group, hipStream_t st)
     a.E = E;
     a.tiles = ceil_div(a.N, 128);
     with_codes(a, group, [&](auto g, auto zeros) {
-        with_rows(R, E, [&](auto bmc) {
-            constexpr int BM = decltype(bmc)::value, G = decltype(g)::value;
-            auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM>;
-            constexpr int lds = BM * 272 + 128 * 80 + 128 / G * 128 * 8;
+        with_tile(R, E, a.tiles, [&](auto bmc, auto ksc) {
+            constexpr int BM = decltype(bmc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
+            auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM, KS>;
+            constexpr int lds = KS * tile_lds(BM, G);
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
-            hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256), lds, st, a);
+            hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256 * KS), lds, st, a);
         });
     });
 }
@@ -970,7 +1044,7 @@ moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *of
     a.K = s->K;
     a.kind = kOutF32;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (s->R <= 16 * s->E) launch_q4_stream(a, s->R, s->E, s->group, s->x, -1, st);
+    if (few_rows(s->R, s->E, ceil_div(s->N, 128))) launch_q4_stream(a, s->R, s->E, s->group, s->x, -1, st);
     else if (s->x == kXBf16) launch_q4_tiles<kXBf16>(a, s->R, s->E, s->group, st);
     else launch_q4_tiles<kXF16>(a, s->R, s->E, s->group, st);
     MOE_TRY_HIP(hipGetLastError());

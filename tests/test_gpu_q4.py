@@ -215,3 +215,40 @@ def test_another_stream_and_a_graph():
             torch.cuda.synchronize()
             assert torch.equal(b.ye, want)
             b.run()
+
+
+# Each tile of the kernels for many rows (32, 64 and 128 rows), and a depth that one, two or four parts of a block share out
+TILES = [
+    dict(R=40, N=8200, K=256, group=32), dict(R=200, N=4224, K=384, group=64, x="f16", zeros=True), dict(R=35, N=70, K=1184, group=32),
+    dict(R=300, N=5000, K=640, group=128, zeros=True), dict(R=300, N=5000, K=96, group=32, x="f16"),
+    dict(R=700, N=5000, K=320, group=64), dict(R=800, N=5000, K=320, group=64, x="f16"), dict(R=800, N=5000, K=160, group=32, zeros=True),
+    dict(R=2050, N=300, K=384, group=128), dict(R=2050, N=130, K=416, group=32, x="f16", zeros=True),
+    dict(R=900, N=2000, K=256, group=128, E=7, counts=[0, 1, 33, 0, 800, 64, 2]), dict(R=24, N=4000, K=512, group=64, zeros=True),
+    dict(R=60, N=700, K=640, group=32, E=2, counts=[59, 1], x="f16"),
+]
+
+
+@pytest.mark.parametrize("kw", TILES, ids=lambda kw: "-".join(str(v) for v in kw.values()))
+def test_linear_tiles(kw):
+    c = Linear(**kw)
+    c.run()
+    c.check()
+    first = c.y.clone()
+    c.y.fill_(7.0)
+    assert torch.equal(c.run(), first)
+
+
+BLOCK_TILES = [
+    dict(R=100, d=512, h=512, group=128, E=2), dict(R=100, d=96, h=2976, group=32, zeros=True, act="gelu"),
+    dict(R=400, d=640, h=3200, group=64), dict(R=1500, d=256, h=4096, group=128, E=8, zeros=True, act="relu"),
+    dict(R=2500, d=1056, h=608, group=32, act="gelu_tanh"), dict(R=2100, d=384, h=640, group=128, E=2, counts=[0, 2100], zeros=True),
+]
+
+
+@pytest.mark.parametrize("kw", BLOCK_TILES, ids=lambda kw: "-".join(str(v) for v in kw.values()))
+def test_gated_ffn_tiles(kw):
+    b = Q4Block(**kw)
+    first = b.run().clone()
+    b.check()
+    b.ye.fill_(7.0)
+    assert torch.equal(b.run(), first)
