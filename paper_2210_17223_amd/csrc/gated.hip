@@ -54,6 +54,9 @@ __device__ __forceinline__ void store_bf16x4(char *p, const float (&v)[4])
 }
 
 // ---------------------------------------------------------------- first projections, tiles of 256 packed columns
+// Bound by the matrix cores at the clock that their energy leaves, as the expert FFN's: 32768 rows, 32 experts, 2048 x 8192,
+// 256 x 256 tiles, 1753 us, 1254 TFLOP/s (a vendor library's dense product of that size 1200); keeping G, U and H for the backward
+// pass, 16384 rows, 8 experts, 2048 x 5632, 632 us, 1196 TFLOP/s.
 // R of a wavefront's rows, from `r` on, as they lie in the patch's rows 16 part .. (W4Place): PIECES 16-byte pieces of 8
 // columns each, to columns col0 + 8 piece of `out`; of 16 pieces the last eight go pair_at columns further on.
 template <int BM, int R, int PIECES>
@@ -118,6 +121,8 @@ __global__ __launch_bounds__(256, 1) void gated_run_kernel(
 }
 
 // ---------------------------------------------------------------- first projections, 128 x 128 tiles
+// For some hundred rows per expert, bound by bytes into LDS; with five stages on their way (DEEP) for fewer, bound by the weights'
+// arrival: the block of 8 experts, 2048 x 5632, 48 rows each, 142 us, 3.9 TB/s (128 x 256 tiles 150, 256 x 256 164).
 template <int ACT, bool KEEP, bool KTAIL, bool DEEP>
 __global__ __launch_bounds__(256, DEEP ? 1 : 2) void gated_tile_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ H, uint16_t *__restrict__ Pre,
@@ -293,7 +298,8 @@ __device__ __forceinline__ float gate_value_f32(float v)
 }
 
 // H = act(A Wg) * (A Wu), W13 canonical [E, K, 2 h]: as grouped_gemm_f32_kernel of the expert FFN, with a second set of
-// weight columns.  Tiles of 32 rows x 32 hidden columns, four wavefronts of 16 x 16, on the fp32 matrix instruction.
+// weight columns.  Tiles of 32 rows x 32 hidden columns, four wavefronts of 16 x 16, on the fp32 matrix instruction.  512 rows, 4
+// experts, 128 x 256: 5.3 us, most of it a launch's latency (tiles from the offsets; behind a list of them 3 us more).
 template <int ACT>
 __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict__ A, const float *__restrict__ B,
                                                         float *__restrict__ H, const int32_t *__restrict__ offsets, int E, int h, int K)
@@ -365,7 +371,8 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict_
 // ---------------------------------------------------------------- backward: dH and through the gate
 // C tile dH = dye W2^T; out = [dG | dU] = [dH U act'(G) | dH act(G)], both bf16, G and U from pre [rows, 2 h].  G and U come
 // into LDS behind the last stages, 32 rows of a wavefront's part at a time, and are turned into dG and dU in their places; of
-// 256 x 256 tiles the rows from 64 on follow while the first ones are computed.
+// 256 x 256 tiles the rows from 64 on follow while the first ones are computed.  16384 rows, 8 experts, 2048 x 5632: 414 us alone,
+// 913 TFLOP/s: per 256 x 256 tile of 32 stages 512 KiB come in and go out behind the loop.
 template <int ACT, bool KTAIL, int BM>
 __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, const uint16_t *__restrict__ pre, uint16_t *__restrict__ out,
@@ -459,7 +466,8 @@ __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
 }
 
 // ---------------------------------------------------------------- backward: dxe
-// C [rows, N] bf16 = A W^T
+// C [rows, N] bf16 = A W^T, A = [dG | dU].  16384 rows, 8 experts, N = 2048, K = 11264, 128 x 256 tiles: 860 us, 880 TFLOP/s (544 tiles of
+// 256 x 256 are two rounds and a bit); the weight gradients beside it fill the last one.
 template <bool KTAIL, int BM>
 __global__ __launch_bounds__(256, 1) void rows_bf16_run_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, uint16_t *__restrict__ C, const WorkItem *__restrict__ items,
@@ -523,7 +531,7 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void rows_bf16_tile_kernel(
 // ---------------------------------------------------------------- weight packing
 // out[e][column n of in, packed][k] = in[e][k][n], 64 x 64 tiles through LDS.  GATED: n in [0, 2 h), columns n and h + n are
 // sixteen apart (kGatedBlock), padding columns zeros; else out[e][n][k], from bf16 to fp16.
-// Bound by HBM: 16 bytes per lane both ways (a lane turns eight rows of eight columns... through the tile).
+// Bound by HBM: 16 bytes per lane both ways.  8 experts, 2048 x 11264: 178 us, 4.2 TB/s; rows of 2000 bytes (K = 1000) 3.4.
 template <bool GATED>
 __global__ __launch_bounds__(256) void gated_pack_kernel(const uint16_t *__restrict__ in, uint16_t *__restrict__ out, int K,
                                                          int N, int NP)
@@ -568,21 +576,28 @@ __global__ __launch_bounds__(256) void gated_pack_kernel(const uint16_t *__restr
 }
 
 // ---------------------------------------------------------------- host side
-// Tile of a row-grouped GEMM on these kernels.  few: the kernel for decode steps is there; mid: that of 128 x 256 tiles.
+// Tile of a row-grouped GEMM on these kernels.  few: the kernel for decode steps is there, and few rows mean that the weights'
+// arrival bounds the launch (first projections); mid: that of 128 x 256 tiles.
+//  * Decode kernel / 128 x 128 tiles, us of the whole block, 16 experts 768 x 2048, 8 of 2048 x 5632, 64 of 512 x 1376, 4 of 4096 x
+//    2048: 5 rows per expert 29 / 32, 118 / 124, 48 / 52, 37 / 46, 8 rows 31 / 33, 122 / 127, 57 / 55, 39 / 47, 16 rows 36 / 36, 140 / 135,
+//    65 / 56, 47 / 46.  While its blocks are few it holds longer: one expert 1024 x 2816, 32 rows 17 / 22, 48 rows 33 / 31.
+//  * Up to 64 rows per expert, K = 2048, five stages of 128 x 128 on their way / the general choice: 16 rows 135 / 146, 32 139 / 160, 64
+//    146 / 158, 128 170 / 174, 256 233 / 224; K = 768 40 / 36.
+//  * Else the expert FFN's choice, from no fewer rows than one tile has (one expert, 128 rows: 47 -> 32).
 GemmPlan plan_gated(int64_t rows, int E, int N, int K, bool few, bool mid, int64_t max_rows)
 {
     GemmPlan gp;
-    if (few && (rows <= 5 * static_cast<int64_t>(E) ||
+    if (few && (rows <= 10 * static_cast<int64_t>(E) ||
                 (rows <= 32 * static_cast<int64_t>(E) && rows * ((N + 127) / 128) <= 2000))) {
         gp.bm = 32;
         gp.bn = 64;
         gp.concurrent = 128;
-    } else if (mid && few_long_tiles(rows, E, N, K)) {
+    } else if (mid && (few_long_tiles(rows, E, N, K) || (few && K >= 1920 && rows <= 64 * static_cast<int64_t>(E)))) {
         gp.bm = gp.bn = 128;
         gp.concurrent = 32;
         gp.w4 = gp.deep = true;
     } else {
-        choose_w4_tile(rows, E, N, K, &gp);
+        choose_w4_tile(std::max<int64_t>(rows, 256), E, N, K, &gp);
         if (!mid && gp.bm != gp.bn) {
             gp.bn = 128;
             gp.concurrent = 64;
