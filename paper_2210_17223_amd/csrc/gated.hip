@@ -580,14 +580,16 @@ __global__ __launch_bounds__(256) void gated_pack_kernel(const uint16_t *__restr
 // arrival bounds the launch (first projections); mid: that of 128 x 256 tiles.
 //  * Decode kernel / 128 x 128 tiles, us of the whole block, 16 experts 768 x 2048, 8 of 2048 x 5632, 64 of 512 x 1376, 4 of 4096 x
 //    2048: 5 rows per expert 29 / 32, 118 / 124, 48 / 52, 37 / 46, 8 rows 31 / 33, 122 / 127, 57 / 55, 39 / 47, 16 rows 36 / 36, 140 / 135,
-//    65 / 56, 47 / 46.  While its blocks are few it holds longer: one expert 1024 x 2816, 32 rows 17 / 22, 48 rows 33 / 31.
+//    65 / 56, 47 / 46.  Of experts whose rows are uneven (popularity by 1 / rank) the line lies lower: 6 rows 33 / 34 and 121 / 125, 8 rows
+//    42 / 38 and 132 / 131, 10 rows 42 / 38 and 140 / 136.  While its blocks are few it holds longer: one expert 1024 x 2816, 32 rows 17 /
+//    22, 48 rows 33 / 31.
 //  * Up to 64 rows per expert, K = 2048, five stages of 128 x 128 on their way / the general choice: 16 rows 135 / 146, 32 139 / 160, 64
-//    146 / 158, 128 170 / 174, 256 233 / 224; K = 768 40 / 36.
+//    146 / 158, 128 170 / 174, 256 233 / 224; uneven rows, 20 133 / 143, 64 137 / 148; K = 768 40 / 36, K = 1024 119 / 112.
 //  * Else the expert FFN's choice, from no fewer rows than one tile has (one expert, 128 rows: 47 -> 32).
 GemmPlan plan_gated(int64_t rows, int E, int N, int K, bool few, bool mid, int64_t max_rows)
 {
     GemmPlan gp;
-    if (few && (rows <= 10 * static_cast<int64_t>(E) ||
+    if (few && (rows <= 7 * static_cast<int64_t>(E) ||
                 (rows <= 32 * static_cast<int64_t>(E) && rows * ((N + 127) / 128) <= 2000))) {
         gp.bm = 32;
         gp.bn = 64;
