@@ -415,25 +415,25 @@ __device__ __forceinline__ int tile_code_row(bool gated, int i, int col0, int wi
 __device__ __forceinline__ int widened_place(int e) { return (e & ~7) | (e & 3) << 1 | (e >> 2 & 1); }
 
 // LDS of the tile kernels' four wavefronts that work on a stage together
-constexpr int tile_lds(int bm, int group)
+constexpr int tile_lds(int bm, int bn, int group)
 {
-    return bm * 272 + 128 * 80 + 128 / group * 128 * 8;
+    return bm * 272 + bn * 80 + 128 / group * bn * 8;
 }
 constexpr int ready_lds(int bm, int group)
 {
     const int stages = 2 * bm * 256 + 128 * 64 + 128 / group * 128 * 8, tile = bm * 136 * 2;
     return stages > tile ? stages : tile;
 }
-// Where KS times four wavefronts share out a tile's depth, stage by stage in turn: the first four add up all sums, in a fixed
+// Where KS times NT threads share out a tile's depth, stage by stage in turn: the first NT add up all sums, in a fixed
 // order (through LDS, behind a barrier after its last use).  False: not one of them.
-template <int KS, int TN, int TM>
+template <int KS, int NT, int TN, int TM>
 __device__ __forceinline__ bool join(f32x4 (&total)[TN][TM], char *shared, int pitch, int part_of, int tid)
 {
     if constexpr (KS > 1) {
         if (part_of > 0) {
             f32x4 *const out = reinterpret_cast<f32x4 *>(shared + part_of * pitch) + tid;
 #pragma unroll
-            for (int i = 0; i < TN * TM; ++i) out[i * 256] = total[i / TM][i % TM];
+            for (int i = 0; i < TN * TM; ++i) out[i * NT] = total[i / TM][i % TM];
         }
         __syncthreads();
         if (part_of > 0) return false;
@@ -442,7 +442,7 @@ __device__ __forceinline__ bool join(f32x4 (&total)[TN][TM], char *shared, int p
             const f32x4 *const in = reinterpret_cast<const f32x4 *>(shared + p * pitch) + tid;
 #pragma unroll
             for (int i = 0; i < TN * TM; ++i) {
-                const f32x4 v = in[i * 256];
+                const f32x4 v = in[i * NT];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) total[i / TM][i % TM][c] += v[c];
             }
@@ -451,57 +451,57 @@ __device__ __forceinline__ bool join(f32x4 (&total)[TN][TM], char *shared, int p
     return true;
 }
 
-// The linear map on BM x 128 tiles, four wavefronts of 64 x 64 (BM = 128), 64 x 32 or 32 x 32.  Stages of 128: x (in the codes'
-// order), codes, scales and zeros of the next one are on their way in registers while this one, in LDS, is multiplied; KS times
-// four wavefronts, or several blocks, of a compute unit take turns at that.  A group's sums have accumulators of their own;
-// behind the group they are scaled into the totals, four instructions for each tile of 16 x 16 and group beside its G / 32 matrix
-// instructions (and in bf16 four more for the zeros).  Each wavefront widens its own columns' codes, seven instructions for eight
-// of them, which feed BM / 32 matrix instructions: bound by the issue of vector instructions, and with few tiles by the compute
-// units that have none.  4096 x 4096, group 128: 160 rows 19 us, 1000 rows 55 us (605 TFLOP/s); 8192 x 8192 from fp16, 6000
-// rows 1132 us (712 TFLOP/s).
-template <int XT, int G, bool ZEROS, int BM, int KS>
-__global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_tile_kernel(Q4Args a)
+// The linear map on tiles of BM rows x BN columns: of 128 columns four wavefronts of 64 x 64 (BM = 128), 64 x 32 or 32 x 32, of
+// 32 columns one.  Stages of 128: x (in the codes' order), codes, scales and zeros of the next one are on their way in registers
+// while this one, in LDS, is multiplied; KS times as many wavefronts, or several blocks, of a compute unit take turns at that.  A
+// group's sums have accumulators of their own; behind the group they are scaled into the totals, four instructions for each tile
+// of 16 x 16 and group beside its G / 32 matrix instructions (and in bf16 four more for the zeros).  Each wavefront widens its own
+// columns' codes, seven instructions for eight of them, which feed BM / 32 matrix instructions: bound by the issue of vector
+// instructions, and with few tiles by the compute units that have none.  4096 x 4096, group 128: 64 rows 11 us, 160 rows 19 us,
+// 1000 rows 56 us (600 TFLOP/s); 8192 x 8192 from fp16, 6000 rows 1132 us (712 TFLOP/s).
+template <int XT, int G, bool ZEROS, int BM, int BN, int KS>
+__global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_tile_kernel(Q4Args a)
 {
-    constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
+    constexpr int NT = 2 * BN, WM = BM / 64 > 1 ? 2 : 1, WN = NT / kWave / WM, TM = BM / WM / 16, TN = BN / 16 / WN;
     constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
     constexpr int XPITCH = 272, QPITCH = 80;                 // bytes of a row in LDS
-    constexpr int XV = BM / 16;                              // 16-byte pieces of x per thread and stage
-    constexpr int Q_AT = BM * XPITCH, S_AT = Q_AT + 128 * QPITCH;
-    static_assert(KS == 1 || tile_lds(BM, G) >= BM * 128 * 4, "the sums lie there, too");
+    constexpr int XV = BM * 16 / NT;                         // 16-byte pieces of x per thread and stage
+    constexpr int Q_AT = BM * XPITCH, S_AT = Q_AT + BN * QPITCH;
+    static_assert(KS == 1 || tile_lds(BM, BN, G) >= BM * BN * 4, "the sums lie there, too");
     extern __shared__ __attribute__((aligned(16))) char all_shared[];
-    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-    char *const shared = all_shared + part_of * tile_lds(BM, G);
-    const int tid = threadIdx.x & 255, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+    char *const shared = all_shared + part_of * tile_lds(BM, BN, G);
+    const int tid = threadIdx.x % NT, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
     const int width = a.N, KG = a.K / G, KB = a.K / 2;
 
     int expert, row0, row1, col0;
     if (!block_tile<BM>(a.offsets, a.E, a.tiles, blockIdx.x, expert, row0, row1, col0)) return;
-    col0 *= 128;
+    col0 *= BN;
 
-    // staging: piece p = tid + 256 q; x: row p / 16 of the tile, codes: row p / 4
+    // staging: piece p = tid + NT q; x: row p / 16 of the tile, codes: row p / 4
     const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(a.x) + static_cast<size_t>(row0) * a.K, 0, static_cast<unsigned>(row1 - row0) * a.K * 2u, 0x00020000);
     auto code_row = [&](int i) { return min(col0 + i, width - 1); };
     const uint8_t *q_src[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const int p = tid + 256 * q;
+        const int p = tid + NT * q;
         q_src[q] = a.q + (static_cast<size_t>(expert) * a.N + code_row(p / 4)) * KB;
     }
-    const size_t g_row = (static_cast<size_t>(expert) * a.N + code_row(tid & 127)) * KG;   // threads < 128: scales, others: zeros
+    const size_t g_row = (static_cast<size_t>(expert) * a.N + code_row(tid % BN)) * KG;   // threads < BN: scales, others: zeros
     u32x4 xr[XV], qr[2];
     Run<GS * 2> gr;
     auto load = [&](int s) {
 #pragma unroll
         for (int q = 0; q < XV; ++q) {
-            const int p = tid + 256 * q, k = s * 128 + p % 16 * 8;
+            const int p = tid + NT * q, k = s * 128 + p % 16 * 8;
             xr[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, k < a.K ? (p / 16 * a.K + k) * 2 : 0x7ffffff0, 0, 0));
         }
 #pragma unroll
         for (int q = 0; q < 2; ++q)
-            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + 256 * q) % 4 * 16, KB - 16));
-        if (tid < 128) {
+            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + NT * q) % 4 * 16, KB - 16));
+        if (tid < BN) {
             if (s * GS + GS <= KG) {
                 gr.load(a.scale + g_row + s * GS);
             } else {
@@ -516,19 +516,19 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_tile_kernel(Q4Arg
     auto place = [&]() {
 #pragma unroll
         for (int q = 0; q < XV; ++q) {
-            const int p = tid + 256 * q;
+            const int p = tid + NT * q;
             *reinterpret_cast<u32x4 *>(shared + p / 16 * XPITCH + p % 16 * 16) = reorder(xr[q]);
         }
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const int p = tid + 256 * q;
+            const int p = tid + NT * q;
             *reinterpret_cast<u32x4 *>(shared + Q_AT + p / 4 * QPITCH + p % 4 * 16) = qr[q];
         }
-        // [group][128] pairs of scale and zero
+        // [group][BN] pairs of scale and zero
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
-            float *to = reinterpret_cast<float *>(shared + S_AT) + (g * 128 + (tid & 127)) * 2;
-            if (tid < 128) to[0] = gr.half(g);
+            float *to = reinterpret_cast<float *>(shared + S_AT) + (g * BN + tid % BN) * 2;
+            if (tid < BN) to[0] = gr.half(g);
             else to[1] = ZEROS ? static_cast<float>((gr.w[g / 2] >> (g % 2 * 16)) & 0xffu) : 8.0f;
         }
     };
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_tile_kernel(Q4Arg
             f16x2 m1[2], m16[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const float2 v = *reinterpret_cast<const float2 *>(sb + (g * 128 + (t0 + t) * 16) * 2);
+                const float2 v = *reinterpret_cast<const float2 *>(sb + (g * BN + (t0 + t) * 16) * 2);
                 sv[t] = v.x;
                 zv[t] = v.y;
                 const _Float16 one = static_cast<_Float16>(-1024.0f - v.y), sixteen = static_cast<_Float16>(-64.0f - v.y);
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_tile_kernel(Q4Arg
         multiply_stage();
         __syncthreads();
     }
-    if (!join<KS>(total, all_shared, tile_lds(BM, G), part_of, tid)) return;
+    if (!join<KS, NT>(total, all_shared, tile_lds(BM, BN, G), part_of, tid)) return;
 
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, column (wn * TN + t) * 16 + fr: sixteen columns of four
     // rows per instruction, 64 bytes each
@@ -814,7 +814,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
         multiply_stage((i & 1) * X_BUF);
         __syncthreads();
     }
-    const bool joined = join<KS>(total, all_shared, ready_lds(BM, G), part_of, tid);
+    const bool joined = join<KS, 256>(total, all_shared, ready_lds(BM, G), part_of, tid);
 
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, its code row (wn * TN + t) * 16 + fr.  Out through
     // LDS, as whole lines.
@@ -887,14 +887,11 @@ void with_tile(int R, int E, int tiles, F f)
     else if (blocks > 256) f(integral_constant<int, 32>{}, integral_constant<int, 2>{});
     else f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
 }
-// Whether rows go through the kernel for few of them: with tiles 128 columns wide on no more than a quarter of the compute units,
-// up to 32 per expert, else up to 16.  Stream / tiles, us: 20 and 40 rows of 4096 x 4096 12 / 18 and 17 / 18, of 8192 x 8192 22 / 37 and
-// 32 / 37, of 2048 x 12000 21 / 18 and 31 / 19.  The gated block (always 16): 8 experts of 2048 x 8192, 10, 14 and 18 rows each 51 / 72,
-// 78 / 72, 84 / 73; 4096 x 4096 63 / 97, 91 / 97, 98 / 97.
-bool few_rows(int R, int E, int tiles)
-{
-    return R <= 16 * E || (R <= 32 * E && std::min(R, E) * static_cast<int64_t>(tiles) <= 64);
-}
+// Whether a linear map's rows go through the kernel for few of them, which takes sixteen at a time.  That kernel / tiles, us: 16 and 20 rows of
+// 4096 x 4096 7 / 10 and 12 / 10, of 8192 x 8192 12 / 18 and 21 / 18, of 2048 x 12000 12 / 13 and 21 / 13; 4 experts, 2048 x 2048, 8 and 12 uneven
+// rows each 6 / 8 and 10 / 8.  (The gated block, up to 16 per expert: 8 experts of 2048 x 8192, 10, 14 and 18 rows each 51 / 72, 78 / 72,
+// 84 / 73; 4096 x 4096 63 / 97, 91 / 97, 98 / 97.)
+bool few_rows(int R, int E) { return R <= 16 || R <= 10 * E; }
 
 // rows that are ready
 void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
@@ -920,16 +917,25 @@ template <int XT>
 void launch_q4_tiles(Q4Args a, int R, int E, int group, hipStream_t st)
 {
     a.E = E;
-    a.tiles = ceil_div(a.N, 128);
     with_codes(a, group, [&](auto g, auto zeros) {
-        with_tile(R, E, a.tiles, [&](auto bmc, auto ksc) {
-            constexpr int BM = decltype(bmc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
-            auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM, KS>;
-            constexpr int lds = KS * tile_lds(BM, G);
+        auto launch = [&](auto bmc, auto bnc, auto ksc) {
+            constexpr int BM = decltype(bmc)::value, BN = decltype(bnc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
+            auto kern = q4_tile_kernel<XT, G, decltype(zeros)::value, BM, BN, KS>;
+            constexpr int lds = KS * tile_lds(BM, BN, G);
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
-            hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256 * KS), lds, st, a);
-        });
+            a.tiles = ceil_div(a.N, BN);
+            hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(2 * BN * KS), lds, st, a);
+        };
+        // Columns in 32s, the depth in 4 or 8 parts, while tiles of 128 columns would leave most compute units without one.  Blocks
+        // of 32 x 32, 8 / 4 parts / the tiles above, us: 64 .. 128 blocks 10 / 11 / 18, 256 10.4 / 11.5 / 18 and 20 / 21 / 37, 375 19 / 13 / 18, 504 51 /
+        // 41 / 53, 512 20 / 15.5 / 18 and 36 / 29 / 37, 640 27 / 19.5 / 18 and 34 / 23 / 23, 750 27 / 16.5 / 19, 768 52 / 38 / 37, 1024 37 / 26 / 20.
+        using std::integral_constant;
+        const int64_t blocks = (R + 16ll * std::min(R, E) + 15) / 32 * ceil_div(a.N, 32);
+        const integral_constant<int, 32> narrow;
+        if (blocks <= 256) return launch(narrow, narrow, integral_constant<int, 8>{});
+        if (blocks <= 600) return launch(narrow, narrow, integral_constant<int, 4>{});
+        with_tile(R, E, ceil_div(a.N, 128), [&](auto bm, auto ks) { launch(bm, integral_constant<int, 128>{}, ks); });
     });
 }
 
@@ -1044,7 +1050,7 @@ moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *of
     a.K = s->K;
     a.kind = kOutF32;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few_rows(s->R, s->E, ceil_div(s->N, 128))) launch_q4_stream(a, s->R, s->E, s->group, s->x, -1, st);
+    if (few_rows(s->R, s->E)) launch_q4_stream(a, s->R, s->E, s->group, s->x, -1, st);
     else if (s->x == kXBf16) launch_q4_tiles<kXBf16>(a, s->R, s->E, s->group, st);
     else launch_q4_tiles<kXF16>(a, s->R, s->E, s->group, st);
     MOE_TRY_HIP(hipGetLastError());
