@@ -419,9 +419,9 @@ constexpr int tile_lds(int bm, int bn, int group)
 {
     return bm * 272 + bn * 80 + 128 / group * bn * 8;
 }
-constexpr int ready_lds(int bm, int group)
+constexpr int ready_lds(int bm, int bn, int group)
 {
-    const int stages = 2 * bm * 256 + 128 * 64 + 128 / group * 128 * 8, tile = bm * 136 * 2;
+    const int stages = 2 * bm * 256 + bn * 64 + 128 / group * bn * 8, tile = bm * (bn + 8) * 2;
     return stages > tile ? stages : tile;
 }
 // Where KS times NT threads share out a tile's depth, stage by stage in turn: the first NT add up all sums, in a fixed
@@ -658,7 +658,7 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
     }
 }
 
-// The tile kernel for rows that are ready: fp16 in the codes' order.  They go from memory straight into LDS, one stage ahead,
+// The tile kernel for rows that are ready, fp16 in the codes' order; tiles, wavefronts and parts as above.  They go from memory straight into LDS, one stage ahead,
 // two places in turn; of a row's sixteen 16-byte pieces the one that quarter o of a wavefront reads with dword j lies at
 // 4 j + o, XOR-swizzled with the row, both done by the choice of the loads' addresses: fragment reads are free of bank conflicts
 // (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).  Codes, scales and zeros of the next stage
@@ -669,18 +669,18 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
 // instructions placed by hand between the matrix instructions 375 + 225; weights scaled before the product (no sums per group,
 // rounded to fp16) on four wavefronts and 128 x 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its
 // loads and numbers with nobody to step in.
-template <int G, bool ZEROS, int BM, int KS>
-__global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Args a)
+template <int G, bool ZEROS, int BM, int BN, int KS>
+__global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_ready_kernel(Q4Args a)
 {
-    constexpr int WM = BM / 64 > 1 ? 2 : 1, WN = 4 / WM, TM = BM / WM / 16, TN = 8 / WN;
+    constexpr int NT = 2 * BN, WAVES = NT / kWave, WM = BM / 64 > 1 ? 2 : 1, WN = WAVES / WM, TM = BM / WM / 16, TN = BN / 16 / WN;
     constexpr int GS = 128 / G, PER = 4 / GS;                // groups of a stage, dwords of 128 k and one group
-    constexpr int X_BUF = BM * 256, Q_AT = 2 * X_BUF, S_AT = Q_AT + 128 * 64;
-    constexpr int XV = BM / 16;                              // loads of x per wavefront and stage, four rows each
-    static_assert(KS == 1 || ready_lds(BM, G) >= BM * 128 * 4, "the sums lie there, too");
+    constexpr int X_BUF = BM * 256, Q_AT = 2 * X_BUF, S_AT = Q_AT + BN * 64;
+    constexpr int XV = BM / 4 / WAVES;                           // loads of x per wavefront and stage, four rows each
+    static_assert(KS == 1 || ready_lds(BM, BN, G) >= BM * BN * 4, "the sums lie there, too");
     extern __shared__ __attribute__((aligned(16))) char all_shared[];
-    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-    char *const shared = all_shared + part_of * ready_lds(BM, G);
-    const int tid = threadIdx.x & 255, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
+    const int part_of = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+    char *const shared = all_shared + part_of * ready_lds(BM, BN, G);
+    const int tid = threadIdx.x % NT, lane = tid & 63, fr = lane & 15, oct = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
     const bool gated = a.kind == kOutGated;
     const int width = gated ? a.N / 2 : a.N, KG = a.K / G, KB = a.K / 2;
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
     expert = __builtin_amdgcn_readfirstlane(expert);
     row0 = __builtin_amdgcn_readfirstlane(row0);
     row1 = __builtin_amdgcn_readfirstlane(row1);
-    col0 = __builtin_amdgcn_readfirstlane(col0) * (gated ? 64 : 128);
+    col0 = __builtin_amdgcn_readfirstlane(col0) * (gated ? BN / 2 : BN);
 
     // (rows past the expert's end: zeros that no load fetches)
     const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
@@ -697,11 +697,11 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
     int x_src[XV], x_col[4];                                 // (a lane's piece repeats every four loads)
 #pragma unroll
     for (int q = 0; q < XV; ++q) {
-        const int row = wave * (BM / 4) + q * 4 + (lane >> 4), at = (lane & 15) ^ (row & 15), piece = k_of<G>(at >> 2, at & 3) >> 3;
+        const int row = wave * (BM / WAVES) + q * 4 + (lane >> 4), at = (lane & 15) ^ (row & 15), piece = k_of<G>(at >> 2, at & 3) >> 3;
         x_src[q] = (row * a.K + piece * 8) * 2;
         if (q < 4) x_col[q] = piece * 8;
     }
-    const uint32_t x_dest = lds_address(shared) + wave * (X_BUF / 4);
+    const uint32_t x_dest = lds_address(shared) + wave * (X_BUF / WAVES);
     auto load_x = [&](int s, int place) {
 #pragma unroll
         for (int q = 0; q < XV; ++q)
@@ -710,15 +710,15 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
     const uint8_t *q_src[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q)
-        q_src[q] = a.q + (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, (tid + 256 * q) / 4, col0, width)) * KB;
-    const size_t g_row = (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, tid & 127, col0, width)) * KG;
+        q_src[q] = a.q + (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, (tid + NT * q) / 4, col0, width)) * KB;
+    const size_t g_row = (static_cast<size_t>(expert) * a.N + tile_code_row<TN>(gated, tid % BN, col0, width)) * KG;
     u32x4 qr[2];
-    Run<GS * 2> gr;                                          // threads < 128: scales, others: zeros
+    Run<GS * 2> gr;                                          // threads < BN: scales, others: zeros
     auto load_codes = [&](int s) {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
-            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + 256 * q) % 4 * 16, KB - 16));
-        if (tid < 128) {
+            qr[q] = *reinterpret_cast<const u32x4 *>(q_src[q] + min(s * 64 + (tid + NT * q) % 4 * 16, KB - 16));
+        if (tid < BN) {
             if (s * GS + GS <= KG) {
                 gr.load(a.scale + g_row + s * GS);
             } else {
@@ -733,14 +733,14 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
     auto place = [&]() {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const int p = tid + 256 * q, row = p / 4;
+            const int p = tid + NT * q, row = p / 4;
             *reinterpret_cast<u32x4 *>(shared + Q_AT + row * 64 + ((p % 4) ^ (row >> 2 & 3)) * 16) = qr[q];
         }
-        // [group][128] pairs of scale and -1024 - zero (twice, in fp16)
+        // [group][BN] pairs of scale and -1024 - zero (twice, in fp16)
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
-            uint32_t *to = reinterpret_cast<uint32_t *>(shared + S_AT) + (g * 128 + (tid & 127)) * 2;
-            if (tid < 128) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(shared + S_AT) + (g * BN + tid % BN) * 2;
+            if (tid < BN) {
                 to[0] = __float_as_uint(gr.half(g));
             } else {
                 const _Float16 m = static_cast<_Float16>(-1024.0f - (ZEROS ? static_cast<float>((gr.w[g / 2] >> (g % 2 * 16)) & 0xffu) : 8.0f));
@@ -773,7 +773,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
             f32x4 part[TN][TM];
             u32x2 sz[TN];
 #pragma unroll
-            for (int t = 0; t < TN; ++t) sz[t] = sb[g * 128 + t * 16];
+            for (int t = 0; t < TN; ++t) sz[t] = sb[g * BN + t * 16];
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 u32x4 xf[TM];
@@ -814,13 +814,13 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
         multiply_stage((i & 1) * X_BUF);
         __syncthreads();
     }
-    const bool joined = join<KS, 256>(total, all_shared, ready_lds(BM, G), part_of, tid);
+    const bool joined = join<KS, NT>(total, all_shared, ready_lds(BM, BN, G), part_of, tid);
 
     // total[t][r][c]: row wm * BM / WM + 16 r + 4 oct + c of the tile, its code row (wn * TN + t) * 16 + fr.  Out through
     // LDS, as whole lines.
     const int rows = row1 - row0;
     _Float16 *const tile = reinterpret_cast<_Float16 *>(all_shared);
-    const int cols = gated ? 64 : 128, pitch = cols + 8;
+    const int cols = gated ? BN / 2 : BN, pitch = cols + 8;
     float by[TM][4];
 #pragma unroll
     for (int r = 0; r < TM; ++r)
@@ -843,7 +843,7 @@ __global__ __launch_bounds__(256 * KS, KS > 2 ? 4 : 2) void q4_ready_kernel(Q4Ar
     }
     __syncthreads();
     // (width is a multiple of 32)
-    for (int p = threadIdx.x; p < BM * cols / 8; p += 256 * KS) {
+    for (int p = threadIdx.x; p < BM * cols / 8; p += NT * KS) {
         const int row = p / (cols / 8), col = p % (cols / 8) * 8;
         if (row < rows && col0 + col < width)
             *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + static_cast<size_t>(row0 + row) * width + col0 + col) =
@@ -868,7 +868,7 @@ void with_codes(const Q4Args &a, int group, F f)
     else with_group(std::false_type{});
 }
 
-// f(rows of a tile, parts that its depth is shared out in) as constants.  Measured on either side of the lines, us:
+// f(rows of a tile, its columns, parts that its depth is shared out in) as constants.  Measured on either side of the lines, us:
 //  * Tiles of 32 rows leave the fewest compute units idle; widening the codes once for every 32 rows costs most where
 //    there are enough of larger tiles, too.  Block of 8 experts, 2048 x 8192, 32 / 64 rows a tile: 48 rows per expert 98 / 100,
 //    96 153 / 133; of 4, 1024 x 2048, where tiles are few: 300 46 / 48, 512 64 / 66.  Linear map 4096 x 4096 of 640 rows 48 / 51,
@@ -876,40 +876,51 @@ void with_codes(const Q4Args &a, int group, F f)
 //  * 64 / 128 rows, 8 experts, 2048 x 8192: 512 per expert 525 / 540, 1024 1017 / 985, 2048 2139 / 1958; 4096 x 4096 654 / 684,
 //    1247 / 1227, 2557 / 2297; linear map 2048 x 12000: 1000 rows 115 / 123, 2000 241 / 218.
 //  * Few blocks of 32 rows, depth in 1 / 2 / 4 parts: 192 blocks 25 / 20 / 19, 352 36 / 32 / 36, 470 35 / 32 / 37, 640 48 / 49 / 57.
+//  * Columns in 32s, the depth in 4 or 8 parts, while tiles of 128 columns would leave most compute units without one.  Blocks
+//    of 32 x 32 in 8 / 4 parts / the tiles above: 64 .. 128 blocks 10 / 11 / 18, 256 10.4 / 11.5 / 18 and 20 / 21 / 37, 375 19 / 13 / 18, 504 51 /
+//    41 / 53, 512 20 / 15.5 / 18 and 36 / 29 / 37, 640 27 / 19.5 / 18 and 34 / 23 / 23, 750 27 / 16.5 / 19, 768 52 / 38 / 37, 1024 37 / 26 / 20.
 template <typename F>
-void with_tile(int R, int E, int tiles, F f)
+void with_tile(int R, int E, int N, F f)
 {
     using std::integral_constant;
-    const int64_t blocks = (R / 32 + (std::min(R, E) + 1) / 2) * static_cast<int64_t>(tiles);   // of 32 rows
-    if (R / 1024 >= E) f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
-    else if (R / 64 >= E && blocks > 900) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (blocks > 512) f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    else if (blocks > 256) f(integral_constant<int, 32>{}, integral_constant<int, 2>{});
-    else f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+    const integral_constant<int, 32> c32;
+    const integral_constant<int, 64> c64;
+    const integral_constant<int, 128> c128;
+    const integral_constant<int, 1> whole;
+    const int64_t blocks = (R / 32 + (std::min(R, E) + 1) / 2) * static_cast<int64_t>(ceil_div(N, 128));   // of 32 x 128
+    const int64_t narrow = (R + 16ll * std::min(R, E) + 15) / 32 * ceil_div(N, 32);                        // of 32 x 32
+    if (narrow <= 256) f(c32, c32, integral_constant<int, 8>{});
+    else if (narrow <= 600) f(c32, c32, integral_constant<int, 4>{});
+    else if (R / 1024 >= E) f(c128, c128, whole);
+    else if (R / 64 >= E && blocks > 900) f(c64, c128, whole);
+    else if (blocks > 512) f(c32, c128, whole);
+    else if (blocks > 256) f(c32, c128, integral_constant<int, 2>{});
+    else f(c32, c128, integral_constant<int, 4>{});
 }
-// Whether a linear map's rows go through the kernel for few of them, which takes sixteen at a time.  That kernel / tiles, us: 16 and 20 rows of
-// 4096 x 4096 7 / 10 and 12 / 10, of 8192 x 8192 12 / 18 and 21 / 18, of 2048 x 12000 12 / 13 and 21 / 13; 4 experts, 2048 x 2048, 8 and 12 uneven
-// rows each 6 / 8 and 10 / 8.  (The gated block, up to 16 per expert: 8 experts of 2048 x 8192, 10, 14 and 18 rows each 51 / 72, 78 / 72,
-// 84 / 73; 4096 x 4096 63 / 97, 91 / 97, 98 / 97.)
-bool few_rows(int R, int E) { return R <= 16 || R <= 10 * E; }
+// Whether rows go through the kernel for few of them, which takes sixteen of an expert at a time.  That kernel / tiles, us: 16 and 20
+// rows of 4096 x 4096 7 / 10 and 12 / 10, of 8192 x 8192 12 / 18 and 21 / 18, of 2048 x 12000 12 / 13 and 21 / 13; 4 experts, 2048 x 2048, 8
+// and 12 rows each 6 / 8 and 10 / 8.  The gated block, 8 experts of 2048 x 8192, 10 and 14 rows each 52 / 54 and 79 / 54, of 1024 x 4096 26 /
+// 28 and 39 / 28; one expert of 2048 x 5632, 14 and 20 rows 20 / 25 and 34 / 25.
+bool few_rows(int64_t R, int E) { return R <= 16 || R <= 10 * E; }
 
 // rows that are ready
 void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
 {
     const bool gated = a.kind == kOutGated;
     a.E = E;
-    a.tiles = ceil_div(gated ? a.N / 2 : a.N, gated ? 64 : 128);
     with_codes(a, group, [&](auto g, auto zeros) {
-        with_tile(R, E, a.tiles, [&](auto bmc, auto ksc) {
-            constexpr int BM = decltype(bmc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
-            auto kern = q4_ready_kernel<G, decltype(zeros)::value, BM, KS>;
-            constexpr int lds = KS * ready_lds(BM, G);
+        auto launch = [&](auto bmc, auto bnc, auto ksc) {
+            constexpr int BM = decltype(bmc)::value, BN = decltype(bnc)::value, KS = decltype(ksc)::value, G = decltype(g)::value;
+            auto kern = q4_ready_kernel<G, decltype(zeros)::value, BM, BN, KS>;
+            constexpr int lds = KS * ready_lds(BM, BN, G);
             static PerDeviceOnce once;
             once.raise_lds(reinterpret_cast<const void *>(kern), lds);
+            a.tiles = ceil_div(a.N, BN);                         // (of a gated product: of gates and values together)
             hipEvent_t t0, t1;
             prof_kernel_events(stage, &t0, &t1);
-            hipExtLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(256 * KS), lds, st, t0, t1, 0, a);
-        });
+            hipExtLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(2 * BN * KS), lds, st, t0, t1, 0, a);
+        };
+        with_tile(R, E, a.N, launch);
     });
 }
 
@@ -927,15 +938,7 @@ void launch_q4_tiles(Q4Args a, int R, int E, int group, hipStream_t st)
             a.tiles = ceil_div(a.N, BN);
             hipLaunchKernelGGL(kern, dim3(block_tile_grid(R, E, BM, a.tiles)), dim3(2 * BN * KS), lds, st, a);
         };
-        // Columns in 32s, the depth in 4 or 8 parts, while tiles of 128 columns would leave most compute units without one.  Blocks
-        // of 32 x 32, 8 / 4 parts / the tiles above, us: 64 .. 128 blocks 10 / 11 / 18, 256 10.4 / 11.5 / 18 and 20 / 21 / 37, 375 19 / 13 / 18, 504 51 /
-        // 41 / 53, 512 20 / 15.5 / 18 and 36 / 29 / 37, 640 27 / 19.5 / 18 and 34 / 23 / 23, 750 27 / 16.5 / 19, 768 52 / 38 / 37, 1024 37 / 26 / 20.
-        using std::integral_constant;
-        const int64_t blocks = (R + 16ll * std::min(R, E) + 15) / 32 * ceil_div(a.N, 32);
-        const integral_constant<int, 32> narrow;
-        if (blocks <= 256) return launch(narrow, narrow, integral_constant<int, 8>{});
-        if (blocks <= 600) return launch(narrow, narrow, integral_constant<int, 4>{});
-        with_tile(R, E, ceil_div(a.N, 128), [&](auto bm, auto ks) { launch(bm, integral_constant<int, 128>{}, ks); });
+        with_tile(R, E, a.N, launch);
     });
 }
 
@@ -1005,7 +1008,7 @@ moe_status check_q4_block(const moe_shape *s)
 }
 
 // Whether a block's rows are made ready and its products run on tiles.
-bool many_rows(const moe_shape &s) { return moe_max_rows(&s) > 16 * static_cast<int64_t>(s.E); }
+bool many_rows(const moe_shape &s) { return !few_rows(moe_max_rows(&s), s.E); }
 
 }  // namespace
 }  // namespace moe

@@ -252,3 +252,19 @@ def test_gated_ffn_tiles(kw):
     b.check()
     b.ye.fill_(7.0)
     assert torch.equal(b.run(), first)
+
+
+# Few tiles: 32 columns at a time (sixteen gates and their values), widths that end inside them, the depth in eight and four parts
+NARROW = [
+    dict(R=17, d=96, h=160, group=32, zeros=True), dict(R=40, d=1152, h=1408, group=128), dict(R=90, d=704, h=1088, group=64, act="gelu"),
+    dict(R=64, d=352, h=544, group=32, E=3, counts=[33, 0, 31], act="relu"), dict(R=150, d=512, h=1024, group=128, E=2, zeros=True),
+]
+
+
+@pytest.mark.parametrize("kw", NARROW, ids=lambda kw: "-".join(str(v) for v in kw.values()))
+def test_gated_ffn_narrow(kw):
+    b = Q4Block(**kw)
+    first = b.run().clone()
+    b.check()
+    b.ye.fill_(7.0)
+    assert torch.equal(b.run(), first)
