@@ -298,16 +298,17 @@ __device__ __forceinline__ float gate_value_f32(float v)
 }
 
 // H = act(A Wg) * (A Wu), W13 canonical [E, K, 2 h]: as grouped_gemm_f32_kernel of the expert FFN, with a second set of
-// weight columns.  Tiles of 32 rows x 32 hidden columns, four wavefronts of 16 x 16, on the fp32 matrix instruction.  512 rows, 4
-// experts, 128 x 256: 5.3 us, most of it a launch's latency (tiles from the offsets; behind a list of them 3 us more).
-template <int ACT>
+// weight columns.  Tiles of 32 TM rows x 32 hidden columns, four wavefronts of 16 TM x 16, on the fp32 matrix instruction.  512 rows,
+// 4 experts, 128 x 256: 5.3 us, most of it a launch's latency (tiles from the offsets; behind a list of them 3 us more); 4096 rows,
+// one expert, 1024 x 2560, the block 106 TFLOP/s.
+template <int ACT, int TM>
 __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict__ A, const float *__restrict__ B,
                                                         float *__restrict__ H, const int32_t *__restrict__ offsets, int E, int h, int K)
 {
     WorkItem tile;
-    if (!block_tile<32>(offsets, E, (h + 31) / 32, blockIdx.x, tile.expert, tile.row0, tile.row1, tile.n0)) return;
+    if (!block_tile<32 * TM>(offsets, E, (h + 31) / 32, blockIdx.x, tile.expert, tile.row0, tile.row1, tile.n0)) return;
     const int n0 = tile.n0 * 32;
-    constexpr int BM = 32, BN = 32, BK = 32, PD = 4, LDA = BK + 4, LDB = BN + 4;
+    constexpr int BM = 32 * TM, BN = 32, BK = 32, PD = 4, LDA = BK + 4, LDB = BN + 4;
     __shared__ __attribute__((aligned(16))) float As[2][BM * LDA];
     __shared__ __attribute__((aligned(16))) float Bs[2][2][BK * LDB];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -317,23 +318,28 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict_
     const size_t N = 2 * static_cast<size_t>(h);
 
     const int a_row = tid / 8, a_k = tid % 8 * 4, b_k = tid / 8, b_n = tid % 8 * 4;
-    const float *a_src = A + static_cast<size_t>(min(tile.row0 + a_row, tile.row1 - 1)) * K;
+    const float *a_src[TM];
+#pragma unroll
+    for (int m = 0; m < TM; ++m) a_src[m] = A + static_cast<size_t>(min(tile.row0 + a_row + 32 * m, tile.row1 - 1)) * K;
     const float *b_src = B + static_cast<size_t>(tile.expert) * K * N + min(n0 + b_n, h - 4);   // (columns past h are not stored)
-    f32x4 ar[PD], br[PD][2];
+    f32x4 ar[PD][TM], br[PD][2];
     // (no branches around the loads: what lies past K is read from inside and zeroed on its way into LDS)
     auto load = [&](auto slot, int s) {
         constexpr int u = decltype(slot)::value;
-        ar[u] = *reinterpret_cast<const f32x4 *>(a_src + min(s * BK + a_k, K - 4));
+#pragma unroll
+        for (int m = 0; m < TM; ++m) ar[u][m] = *reinterpret_cast<const f32x4 *>(a_src[m] + min(s * BK + a_k, K - 4));
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             br[u][t] = *reinterpret_cast<const f32x4 *>(b_src + static_cast<size_t>(min(s * BK + b_k, K - 1)) * N + t * h);
     };
-    f32x4 acc[2];
-    acc[0] = acc[1] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[2][TM];
+#pragma unroll
+    for (int m = 0; m < TM; ++m) acc[0][m] = acc[1][m] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     auto stage = [&](auto slot, int s) {
         constexpr int u = decltype(slot)::value, buf = u & 1;
         const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-        *reinterpret_cast<f32x4 *>(&As[buf][a_row * LDA + a_k]) = s * BK + a_k < K ? ar[u] : zero;
+#pragma unroll
+        for (int m = 0; m < TM; ++m) *reinterpret_cast<f32x4 *>(&As[buf][(a_row + 32 * m) * LDA + a_k]) = s * BK + a_k < K ? ar[u][m] : zero;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             *reinterpret_cast<f32x4 *>(&Bs[buf][t][b_k * LDB + b_n]) = s * BK + b_k < K ? br[u][t] : zero;
@@ -344,13 +350,18 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict_
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int c = 0; c < BK; c += 16) {
-            const f32x4 af = *reinterpret_cast<const f32x4 *>(&As[buf][(wm * 16 + r16) * LDA + c + 4 * kq]);
+            f32x4 af[TM];
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+                af[m] = *reinterpret_cast<const f32x4 *>(&As[buf][((wm * TM + m) * 16 + r16) * LDA + c + 4 * kq]);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(Bs[buf][t][(c + 4 * kq + q) * LDB + wn * 16 + r16], af[q],
-                                                                  acc[t], 0, 0, 0);
+                for (int t = 0; t < 2; ++t) {
+                    const float w = Bs[buf][t][(c + 4 * kq + q) * LDB + wn * 16 + r16];
+#pragma unroll
+                    for (int m = 0; m < TM; ++m) acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, af[m][q], acc[t][m], 0, 0, 0);
+                }
         }
     };
     static_for<PD>([&](auto u) { load(u, min(decltype(u)::value, KT - 1)); });
@@ -359,13 +370,18 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict_
     static_for<PD>([&](auto u) {
         if (s0 + decltype(u)::value < KT) stage(u, s0 + decltype(u)::value);
     });
-    // acc[t][c]: column n0 + wn * 16 + 4 kq + c, row row0 + wm * 16 + r16
-    const int n = n0 + wn * 16 + 4 * kq, r = tile.row0 + wm * 16 + r16;
-    if (n >= h || r >= tile.row1) return;
-    f32x4 o;
+    // acc[t][m][c]: column n0 + wn * 16 + 4 kq + c, row row0 + (wm * TM + m) * 16 + r16
+    const int n = n0 + wn * 16 + 4 * kq;
+    if (n >= h) return;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] = gate_value_f32<ACT>(acc[0][c]) * acc[1][c];
-    *reinterpret_cast<f32x4 *>(H + static_cast<size_t>(r) * h + n) = o;
+    for (int m = 0; m < TM; ++m) {
+        const int r = tile.row0 + (wm * TM + m) * 16 + r16;
+        if (r >= tile.row1) return;
+        f32x4 o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = gate_value_f32<ACT>(acc[0][m][c]) * acc[1][m][c];
+        *reinterpret_cast<f32x4 *>(H + static_cast<size_t>(r) * h + n) = o;
+    }
 }
 
 // ---------------------------------------------------------------- backward: dH and through the gate
@@ -730,10 +746,18 @@ void launch_first_gemm(const moe_shape &s, const void *xe, const void *W13p, voi
 {
     with_activation(s.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        if (s.dtype == MOE_F32)
-            launch_timed(gated_f32_kernel<ACT>, block_tile_grid(direct.rows, direct.E, 32, (s.d_ff + 31) / 32), 256, 0, kStageGemm1, st,
-                         static_cast<const float *>(xe), static_cast<const float *>(W13p), static_cast<float *>(H), direct.offsets,
-                         direct.E, s.d_ff, s.d_model);
+        // Tiles of 64 rows where they are a few per compute unit (32 / 64 rows a tile, us of the block: 896 tiles 124 / 128, 470 86 / 100, 1280
+        // 169 / 158, 1400 58 / 56, 2496 236 / 227, 5120 659 / 610).
+        auto f32 = [&](auto tmc) {
+            constexpr int TM = decltype(tmc)::value;
+            launch_timed(gated_f32_kernel<ACT, TM>, block_tile_grid(direct.rows, direct.E, 32 * TM, (s.d_ff + 31) / 32), 256, 0,
+                         kStageGemm1, st, static_cast<const float *>(xe), static_cast<const float *>(W13p), static_cast<float *>(H),
+                         direct.offsets, direct.E, s.d_ff, s.d_model);
+        };
+        if (s.dtype == MOE_F32 && (direct.rows / 64 + direct.E / 2) * ((s.d_ff + 31) / 32) >= 1200)
+            f32(std::integral_constant<int, 2>{});
+        else if (s.dtype == MOE_F32)
+            f32(std::integral_constant<int, 1>{});
         else if (pre != nullptr)
             launch_first<ACT, true>(s, static_cast<const uint16_t *>(xe), static_cast<const uint16_t *>(W13p),
                                     static_cast<uint16_t *>(H), static_cast<uint16_t *>(pre), gp, items, direct, st);
