@@ -660,17 +660,17 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
     }
 }
 
-// The tile kernel for rows that are ready, fp16 in the codes' order; tiles, wavefronts and parts as above.  They go from memory straight into LDS, one stage ahead,
-// two places in turn; of a row's sixteen 16-byte pieces the one that quarter o of a wavefront reads with dword j lies at
-// 4 j + o, XOR-swizzled with the row, both done by the choice of the loads' addresses: fragment reads are free of bank conflicts
-// (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).  Codes, scales and zeros of the next stage
-// are on their way in registers, requested behind x, so that the wait for them covers it.
-// Bound by issue: beside 64 matrix instructions of a wavefront and stage stand 300 vector instructions (widening, scaling), and
-// a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, the two products, tiles of 64 rows: 380 + 215
-// us, 720 and 640 TFLOP/s; of 128 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector
-// instructions placed by hand between the matrix instructions 375 + 225; weights scaled before the product (no sums per group,
-// rounded to fp16) on four wavefronts and 128 x 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its
-// loads and numbers with nobody to step in.
+// The tile kernel for rows that are ready, fp16 in the codes' order; tiles, wavefronts and parts as above.  They go from memory
+// straight into LDS, one stage ahead, two places in turn; of a row's sixteen 16-byte pieces the one that quarter o of a
+// wavefront reads with dword j lies at 4 j + o, XOR-swizzled with the row, both done by the choice of the loads' addresses:
+// fragment reads are free of bank conflicts (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).
+// Codes, scales and zeros of the next stage are on their way in registers, requested behind x, so that the wait for them covers
+// it. Bound by issue: beside 64 matrix instructions of a wavefront and stage stand 300 vector instructions (widening, scaling),
+// and a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, the two products, tiles of 64 rows: 380
+// + 215 us, 720 and 640 TFLOP/s; of 128 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x
+// 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector instructions placed by hand between the matrix
+// instructions 375 + 225; weights scaled before the product (no sums per group, rounded to fp16) on four wavefronts and 128 x
+// 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its loads and numbers with nobody to step in.
 template <int G, bool ZEROS, int BM, int BN, int KS>
 __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_ready_kernel(Q4Args a)
 {
