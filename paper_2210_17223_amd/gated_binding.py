@@ -65,13 +65,15 @@ _sizes = {}
 
 
 def _sizes_of(s: Shape):
-    """Rows and bytes that depend on the shape's values alone: (rows, W13p, W2p, workspace)."""
+    """Rows and bytes that depend on the shape's values alone: (rows, W13p, W2p, workspace).  The table is read once: another
+    thread may clear it at any time."""
     key = bytes(s)
-    if key not in _sizes:
+    sizes = _sizes.get(key)
+    if sizes is None:
         if len(_sizes) >= 1024:
             _sizes.clear()
-        _sizes[key] = (moe_max_rows(s), moe_gated_packed_bytes(s), moe_packed_weight_bytes(s), moe_gated_workspace_bytes(s))
-    return _sizes[key]
+        sizes = _sizes[key] = (moe_max_rows(s), moe_gated_packed_bytes(s), moe_packed_weight_bytes(s), moe_gated_workspace_bytes(s))
+    return sizes
 
 
 def moe_pack_gated_weights(s: Shape, W13, W2, W13p, W2p, stream=None) -> None:

@@ -110,3 +110,23 @@ def test_gated_ffn_q4_refusals():
         if i not in (4, 7):
             assert L.moe_gated_ffn_q4(C.byref(s), 64, *args, z) == 1 and "is NULL" in moe.moe_last_error()
     assert L.moe_gated_ffn_q4(None, 64, *[ok] * 10, z) == 1
+
+
+def test_another_thread_may_clear_the_table_of_sizes(monkeypatch):
+    class Cleared(dict):                              # whatever a call has seen or put there is gone when it looks again
+        def __contains__(self, key):
+            found = super().__contains__(key)
+            self.clear()
+            return found
+
+        def __setitem__(self, key, value):
+            super().__setitem__(key, value)
+            self.clear()
+
+    s = shape()
+    want = (moe.moe_max_rows(s), moe.moe_gated_packed_bytes(s), moe.moe_packed_weight_bytes(s), moe.moe_gated_workspace_bytes(s))
+    table = Cleared()
+    monkeypatch.setattr(gated_binding, "_sizes", table)
+    assert gated_binding._sizes_of(s) == want
+    dict.__setitem__(table, bytes(s), want)
+    assert gated_binding._sizes_of(s) == want
