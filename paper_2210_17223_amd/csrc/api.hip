@@ -188,11 +188,7 @@ moe_status check_common(const moe_shape *s)
 moe_status check_plain_expert(const moe_shape *s)
 {
     MOE_TRY(check_common(s));
-    if (s->act == MOE_ACT_SILU) {
-        set_error("MOE_ACT_SILU is an activation of the gated block (moe_gated.h)");
-        return MOE_EUNSUPPORTED;
-    }
-    return MOE_OK;
+    return check_plain_activation(*s);
 }
 
 moe_status check_bias(const moe_shape &s, const float *gate_bias, int32_t stride)
@@ -277,6 +273,13 @@ moe_status scratch_address(void **out)
 }  // namespace
 
 moe_status check_layer_shape(const moe_shape *s) { return check_common(s); }
+
+moe_status check_plain_activation(const moe_shape &s)
+{
+    if (s.act != MOE_ACT_SILU) return MOE_OK;
+    set_error("MOE_ACT_SILU is an activation of the gated block (moe_gated.h)");
+    return MOE_EUNSUPPORTED;
+}
 
 // The expert FFN of a chunked layer runs once per GROUP of consecutive chunks.  A launch
 // reads every expert's two weight matrices from HBM once whatever its row count, and is bound

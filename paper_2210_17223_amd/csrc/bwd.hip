@@ -1625,6 +1625,7 @@ moe_status moe_backward_gemm_kernel(const moe_shape *s, int32_t which, char *nam
         set_error("moe_backward_gemm_kernel: which must be in 0..3, name a buffer, the shape one that moe_layer_backward takes");
         return MOE_EINVAL;
     }
+    if (check_plain_activation(*s) != MOE_OK) return MOE_EINVAL;
     const int64_t R = moe_max_rows(s);
     const int d = s->d_model, h = s->d_ff;
     if (which < 2) {
@@ -1639,7 +1640,7 @@ moe_status moe_backward_gemm_kernel(const moe_shape *s, int32_t which, char *nam
 
 size_t moe_backward_workspace_bytes(const moe_shape *s)
 {
-    if (!supported(s)) return 0;
+    if (!supported(s) || check_plain_activation(*s) != MOE_OK) return 0;
     BwdWorkspace w;
     layout_bwd(*s, reinterpret_cast<void *>(static_cast<uintptr_t>(256)), &w);   // sizes only
     return w.bytes;
@@ -1675,6 +1676,7 @@ moe_status moe_layer_backward_chunked(const moe_shape *s, int32_t n_chunks, cons
                   "k <= %d, d_model and d_ff multiples of 8", kMaxExperts, kMaxTopK);
         return s == nullptr ? MOE_EINVAL : MOE_EUNSUPPORTED;
     }
+    if (check_plain_activation(*s) != MOE_OK) return MOE_EUNSUPPORTED;
     if (gate_bias != nullptr && bias_token_stride != 0 && bias_token_stride != s->E) {
         set_error("bias_token_stride must be 0 or E");
         return MOE_EINVAL;

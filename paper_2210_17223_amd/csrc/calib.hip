@@ -2,6 +2,7 @@
 // delivers on a plain device copy and on a register-resident MFMA loop, so that roofline
 // fractions can be quoted against measured peaks beside the nominal ones.
 #include "common.h"
+#include "gated.h"
 
 namespace moe {
 namespace {
@@ -133,6 +134,7 @@ moe_status moe_expert_gemm_kernel(const moe_shape *s, int32_t which, char *name,
         set_error("moe_expert_gemm_kernel: which must be 0 or 1, name a buffer, the shape a supported bf16 layer");
         return MOE_EINVAL;
     }
+    if (check_plain_activation(*s) != MOE_OK) return MOE_EINVAL;
     expert_gemm_kernel_name(*s, which, name, len);
     return MOE_OK;
 }

@@ -12,6 +12,7 @@
 //   moe_layer_padded   gate, padded plan, pack, and per micro-op: first all-to-all, FFN,
 //                      second all-to-all; combine at the end
 #include "common.h"
+#include "gated.h"
 #include "moe_comm.h"
 
 #include <chrono>
@@ -349,10 +350,7 @@ struct PaddedWorkspace {
 bool padded_shape_ok(const moe_shape *s, int n_micro)
 {
     if (moe_workspace_bytes(s, 1) == 0) return false;            // the common shape checks
-    if (s->act == MOE_ACT_SILU) {
-        set_error("MOE_ACT_SILU is an activation of the gated block (moe_gated.h)");
-        return false;
-    }
+    if (check_plain_activation(*s) != MOE_OK) return false;
     if (static_cast<int64_t>(s->E) * s->capacity >= (1ll << 31)) {
         set_error("E * capacity does not fit 31 bits");
         return false;

@@ -26,5 +26,7 @@ void launch_weight_grad_bf16(bool a_f16, const uint16_t *A, const uint16_t *B, u
                              int M, int N, int64_t max_rows, int stage, hipStream_t st);
 // api.hip: the checks that every call makes of its shape
 moe_status check_layer_shape(const moe_shape *s);
+// api.hip: MOE_EUNSUPPORTED where the shape's activation is the gated block's alone; for the calls whose experts are two plain products
+moe_status check_plain_activation(const moe_shape &s);
 
 }  // namespace moe

@@ -130,3 +130,15 @@ def test_another_thread_may_clear_the_table_of_sizes(monkeypatch):
     assert gated_binding._sizes_of(s) == want
     dict.__setitem__(table, bytes(s), want)
     assert gated_binding._sizes_of(s) == want
+
+
+def test_silu_is_refused_by_the_plain_layers_backward_pass():
+    s, L, ok, z = shape(), moe.lib(), C.c_void_p(4096), C.c_void_p(0)
+    assert moe.moe_backward_workspace_bytes(s) == 0 and "gated" in moe.moe_last_error()
+    with pytest.raises(moe.MoeError, match="gated"):
+        moe.moe_backward_gemm_kernel(s, 0)
+    with pytest.raises(moe.MoeError, match="gated"):
+        moe.moe_expert_gemm_kernel(s, 0)
+    args = [ok, ok, z, C.c_int32(0), *[ok] * 19, z]
+    assert L.moe_layer_backward(C.byref(s), *args) == 2 and "gated" in moe.moe_last_error()
+    assert moe.moe_backward_workspace_bytes(shape(act="gelu")) > 0
