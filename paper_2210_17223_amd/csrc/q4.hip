@@ -2,10 +2,11 @@
 // gated feed-forward block on them.
 //
 // The codes go from memory into registers and from there into the matrix instruction: eight codes of a lane become eight
-// 16-bit numbers in place, by masks and an exponent: in bf16 128 + q, in fp16 1024 + q.  Products and sums over a group are
-// then exact but for fp32's roundings, and a group's sum is scaled in fp32:
+// 16-bit numbers in place, by masks and an exponent: in bf16 2^-16 (128 + q), in fp16 1024 + q.  Products and sums over a group
+// are then exact but for fp32's roundings, and a group's sum is scaled in fp32:
 //   bf16   sum (q - z) x = sum (128 + q) x - (128 + z) sum x, with sum x from one more matrix instruction against ones
-//          (shared by all of a wavefront's columns)
+//          (shared by all of a wavefront's columns); codes and ones over 2^16, which the result is multiplied by, since bf16 rows
+//          have fp32's range and a group's 128 terms of up to 143 x (and 383 sum x: zeros are bytes) would pass it from |x| = 7e33 on
 //   fp16   q - z by one packed subtraction (exact), no correction
 #include "activation.h"
 #include "block_tile.h"
@@ -49,10 +50,13 @@ __device__ __forceinline__ void unrolled(F f)
 template <int XT>
 __device__ __forceinline__ uint32_t exponent_of()
 {
-    uint32_t e = XT == kXBf16 ? 0x43004300u : 0x64006400u;
+    uint32_t e = XT == kXBf16 ? 0x3b003b00u : 0x64006400u;
     asm volatile("" : "+v"(e));
     return e;
 }
+constexpr uint32_t kOnes = 0x37803780u;   // two times 2^-16 in bf16
+template <int XT>
+constexpr float kBack = XT == kXBf16 ? 65536.0f : 1.0f;
 template <int XT>
 __device__ __forceinline__ u32x4 widen(uint32_t w, uint32_t exponent, f16x2 minus, f16x2 minus16)
 {
@@ -281,7 +285,7 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
         // the step's sums, with scales s and zeros z (every lane's own)
         auto use = [&](auto &s, auto &z) {
             const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-            const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+            const u32x4 ones = {kOnes, kOnes, kOnes, kOnes};
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 u32x4 xf[4];
@@ -381,7 +385,7 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) mine[(t * 4 + c) * 64 + lane] = total[t][c];
+            for (int c = 0; c < 4; ++c) mine[(t * 4 + c) * 64 + lane] = total[t][c] * kBack<XT>;
         __syncthreads();
         const int rows = min(r1 - row0, XR), cols = half * 16;
         auto add_up = [&](int row, int t, int n) {
@@ -544,7 +548,7 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
         const char *const xb = shared + (wm * (BM / WM) + fr) * XPITCH, *const qb = shared + Q_AT + (wn * TN * 16 + fr) * QPITCH + oct * 16;
         const float *const sb = reinterpret_cast<const float *>(shared + S_AT) + (wn * TN * 16 + fr) * 2;
         const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        const u32x4 ones = {kOnes, kOnes, kOnes, kOnes};
         u32x4 code[TN];
 #pragma unroll
         for (int t = 0; t < TN; ++t) {
@@ -619,7 +623,7 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
             for (int t = 0; t < TN; ++t) {
                 const int col = col0 + (wn * TN + t) * 16 + fr;
                 if (row < rows && col < width)
-                    static_cast<float *>(a.out)[static_cast<size_t>(row0 + row) * width + col] = total[t][r][c];
+                    static_cast<float *>(a.out)[static_cast<size_t>(row0 + row) * width + col] = total[t][r][c] * kBack<XT>;
             }
         }
 }

@@ -268,3 +268,56 @@ def test_gated_ffn_narrow(kw):
     b.check()
     b.ye.fill_(7.0)
     assert torch.equal(b.run(), first)
+
+
+# bf16 rows have fp32's range: of every path (few rows, tiles of 32, 64 and 128 rows, a shared depth), with zeros of four and of eight bits
+RANGE = [
+    dict(R=1, N=100, K=512, group=128), dict(R=16, N=70, K=608, group=32, zeros=True), dict(R=24, N=40, K=512, group=64, E=3, zeros=True),
+    dict(R=60, N=300, K=640, group=128, zeros=True), dict(R=200, N=4224, K=384, group=64), dict(R=800, N=5000, K=160, group=32, zeros=True),
+    dict(R=2050, N=300, K=384, group=128, zeros=True),
+]
+
+
+@pytest.mark.parametrize("bytes_", [False, True], ids=["nibbles", "bytes"])
+@pytest.mark.parametrize("kw", RANGE, ids=lambda kw: "-".join(str(v) for v in kw.values()))
+def test_linear_of_rows_of_any_size(kw, bytes_):
+    """Rows of 1e-25 to 1e37: what is finite in 64 bits is finite here, and each row is held to its own digits.  (Outputs are below
+    1e37 * 255 * 0.3 / sqrt(K) * K < 3.4e38 only with smaller scales: those are taken by 2^-10.)"""
+    if bytes_ and not kw.get("zeros"):
+        pytest.skip("no zeros")
+    c = Linear(**kw)
+    if bytes_:
+        g = torch.Generator(device=DEV).manual_seed(3)
+        c.z.copy_(torch.randint(0, 256, c.z.shape, generator=g, device=DEV))
+    c.sc.mul_(2.0 ** -10 if c.s.K < 1024 else 2.0 ** -12)
+    size = torch.logspace(-25, 37, kw["R"], device=DEV, dtype=torch.float64) if kw["R"] > 1 else torch.tensor([1e37], device=DEV)
+    c.x.copy_((c.x.double() * size[:, None]).clamp(-3.3e38, 3.3e38))
+    c.run()
+    for e in range(c.s.E):
+        rows = slice(int(c.offs[e]), int(c.offs[e + 1]))
+        codes, s = wide(c.q, c.sc, c.z, e, c.s.group)
+        x = c.x[rows].double()
+        want = x @ (codes * s).T
+        assert bool((want.abs() < 3e38).all())
+        bound = (c.s.K + 8) * U32 * (x.abs() @ ((codes.abs() + 136) * s).T)
+        assert bool(((c.y[rows].double() - want).abs() <= bound).all())
+
+
+def test_block_of_few_rows_of_any_size():
+    """As test_tiny_and_huge_rows, on the path for few rows.  (H is fp16: a row whose H passes 65504 has no finite output.)"""
+    b = Q4Block(R=20, d=512, h=512, group=128, E=2, zeros=True)
+    b.x[:20] = (b.x[:20].float() * torch.logspace(-30, 2, 20, device=DEV)[:, None]).bfloat16()
+    b.x[5, :] = 0.0
+    first = b.run().clone()
+    most = torch.zeros(b.R + 2, dtype=torch.float64, device=DEV)
+    for e in range(b.E):
+        rows = slice(int(b.offs[e]), int(b.offs[e + 1]))
+        c, s = wide(*b.w13, e, b.group)
+        GU = b.x[rows].double() @ (c * s).T
+        most[rows] = (act64(GU[:, :512], "silu")[0] * GU[:, 512:]).abs().amax(1)
+    over, near = most > 65504 * 1.01, most > 65504 * 0.99
+    assert not torch.isfinite(first[over].float()).any()
+    b.x[near] = 0.0
+    b.run()
+    b.check()
+    assert torch.equal(b.ye[~near], first[~near])
