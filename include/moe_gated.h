@@ -90,8 +90,9 @@ typedef struct {
 } moe_q4_shape;
 
 /* y fp32 [R, N] = x [R, K] times the rows' expert's matrix; expert e owns rows [offsets[e], offsets[e+1]).
- * Codes and zeros enter the products exactly, scales and sums are fp32.  bf16 rows may hold finite values of any size (below
- * about 2^-90 they lose digits); a row with an infinity or NaN has no finite output, the others are untouched. */
+ * Codes and zeros enter the products exactly, scales and sums are fp32: of (code - zero) x for fp16 rows, of (16 + code) x less
+ * (16 + zero) x for bf16 rows, whose values may be finite ones of any size (below about 2^-90 they lose digits).  A row with
+ * an infinity or NaN has no finite output; the others are untouched. */
 moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *offsets, const void *q,
                          const void *scale, const void *zero, float *y, void *stream);
 

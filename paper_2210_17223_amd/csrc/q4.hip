@@ -2,11 +2,14 @@
 // gated feed-forward block on them.
 //
 // The codes go from memory into registers and from there into the matrix instruction: eight codes of a lane become eight
-// 16-bit numbers in place, by masks and an exponent: in bf16 2^-16 (128 + q), in fp16 1024 + q.  Products and sums over a group
+// 16-bit numbers in place, by masks and an exponent: in bf16 2^-16 (16 + q), in fp16 1024 + q.  Products and sums over a group
 // are then exact but for fp32's roundings, and a group's sum is scaled in fp32:
-//   bf16   sum (q - z) x = sum (128 + q) x - (128 + z) sum x, with sum x from one more matrix instruction against ones
-//          (shared by all of a wavefront's columns); codes and ones over 2^16, which the result is multiplied by, since bf16 rows
-//          have fp32's range and a group's 128 terms of up to 143 x (and 383 sum x: zeros are bytes) would pass it from |x| = 7e33 on
+//   bf16   sum (q - z) x = sum (16 + q) x - (16 + z) sum x, with sum x from one more matrix instruction against ones
+//          (shared by all of a wavefront's columns).  16 is the least that an exponent can add: the code is then the first
+//          four of the seven digits behind the point.  Against 128 + q, whose code is the last four and needs no shift for one
+//          of its four pairs, sums that cancel keep three more bits, for one instruction in eight of the widening.
+//          Codes and ones are over 2^16, which the result is multiplied by, since bf16 rows have fp32's range and a group's 128
+//          terms of up to 31 x (and 271 sum x: zeros are bytes) would pass it from |x| = 1e34 on.
 //   fp16   q - z by one packed subtraction (exact), no correction
 #include "activation.h"
 #include "block_tile.h"
@@ -50,7 +53,7 @@ __device__ __forceinline__ void unrolled(F f)
 template <int XT>
 __device__ __forceinline__ uint32_t exponent_of()
 {
-    uint32_t e = XT == kXBf16 ? 0x3b003b00u : 0x64006400u;
+    uint32_t e = XT == kXBf16 ? 0x39803980u : 0x64006400u;
     asm volatile("" : "+v"(e));
     return e;
 }
@@ -61,8 +64,8 @@ template <int XT>
 __device__ __forceinline__ u32x4 widen(uint32_t w, uint32_t exponent, f16x2 minus, f16x2 minus16)
 {
     if constexpr (XT == kXBf16) {
-        auto part = [&](uint32_t v) { return (v & 0x000f000fu) | exponent; };
-        return (u32x4){part(w), part(w >> 4), part(w >> 8), part(w >> 12)};
+        auto part = [&](uint32_t v) { return (v & 0x00780078u) | exponent; };
+        return (u32x4){part(w << 3), part(w >> 1), part(w >> 5), part(w >> 9)};
     } else {
         // low four bits of a byte: 1024 + q; high: 1024 + 16 q, a sixteenth of which is 64 + q
         const f16x2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             float v = part[c];
-                            if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - zv, xsum[g][c], v);
+                            if constexpr (XT == kXBf16) v = __builtin_fmaf(-16.0f - zv, xsum[g][c], v);
                             total[t][c] = __builtin_fmaf(sv, v, total[t][c]);
                         }
                     }
@@ -594,7 +597,7 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         float v = part[t][r][c];
-                        if constexpr (XT == kXBf16) v = __builtin_fmaf(-128.0f - zv[t], xsum[r][c], v);
+                        if constexpr (XT == kXBf16) v = __builtin_fmaf(-16.0f - zv[t], xsum[r][c], v);
                         total[t0 + t][r][c] = __builtin_fmaf(sv[t], v, total[t0 + t][r][c]);
                     }
             __builtin_amdgcn_sched_barrier(0);

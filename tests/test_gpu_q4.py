@@ -321,3 +321,23 @@ def test_block_of_few_rows_of_any_size():
     b.run()
     b.check()
     assert torch.equal(b.ye[~near], first[~near])
+
+
+# (The bounds above count an offset of the codes of 128 in bf16 sums; it is 16.)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("R", [1, 16, 50, 200, 2100])
+def test_codes_of_bf16_rows_cost_few_digits(R, group):
+    """Rows of large whole numbers of one sign among which lie odd ones: a group's sum of (16 + q) x stays below 2^24 and is
+    exact in fp32, and so are the totals; a larger offset of the codes would round it.  (A group's x: numbers of 128 .. 255 times
+    2048 / group, at most 2^19 together, and one odd number below 256 instead of one of them.)"""
+    K = 2 * group
+    c = Linear(R, 48, K, group, zeros=True, seed=R)
+    g = torch.Generator(device=DEV).manual_seed(R + group)
+    x = torch.randint(128, 256, c.x.shape, generator=g, device=DEV) * (2048 // group)
+    odd = torch.randint(0, 128, (R, 2), generator=g, device=DEV) * 2 + 1
+    x[:, 5], x[:, group + 7] = odd[:, 0], odd[:, 1]
+    c.x.copy_(x)
+    c.sc.fill_(1.0)
+    assert torch.equal(c.x.double(), x.double()) and int(x.view(R, 2, group).sum(2).max()) * 31 < 2 ** 24
+    codes, s = wide(c.q, c.sc, c.z, 0, group)
+    assert torch.equal(c.run().double(), c.x.double() @ (codes * s).T)
