@@ -504,8 +504,9 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
     auto load = [&](int s) {
 #pragma unroll
         for (int q = 0; q < XV; ++q) {
-            const int p = tid + NT * q, k = s * 128 + p % 16 * 8;
-            xr[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, k < a.K ? (p / 16 * a.K + k) * 2 : 0x7ffffff0, 0, 0));
+            // (offsets are unsigned: 128 rows of 2^24 values are nearly 2^32 bytes, and what lies past K lies past those)
+            const unsigned p = tid + NT * q, k = s * 128 + p % 16 * 8, K = a.K;
+            xr[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsx, k < K ? (p / 16 * K + k) * 2 : 0xfffffff0u, 0, 0));
         }
 #pragma unroll
         for (int q = 0; q < 2; ++q)

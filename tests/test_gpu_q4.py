@@ -341,3 +341,24 @@ def test_codes_of_bf16_rows_cost_few_digits(R, group):
     assert torch.equal(c.x.double(), x.double()) and int(x.view(R, 2, group).sum(2).max()) * 31 < 2 ** 24
     codes, s = wide(c.q, c.sc, c.z, 0, group)
     assert torch.equal(c.run().double(), c.x.double() @ (codes * s).T)
+
+
+def test_linear_past_2_to_31_bytes_of_a_tiles_rows():
+    """128 rows of more than 2^23 values each, whose last stage ends inside 128: what lies past a row's end is zeros, not the
+    values 2^31 bytes behind it (infinities here, of a row that has nothing else)."""
+    R, N, K, group = 1024, 640, (1 << 23) + 96, 32
+    s = moe.Q4Shape.make(R, 1, N, K, group)
+    x = torch.zeros(R, K, dtype=torch.bfloat16, device=DEV)
+    x[:, ::4099], x[:, K - 1] = 1.0, 3.0
+    x[127::128] = math.inf
+    q = torch.full((1, N, K // 2), 0x9a, dtype=torch.uint8, device=DEV)     # codes 10, 9, 10, 9, ...
+    scale = torch.ones(1, N, K // group, dtype=torch.float16, device=DEV)
+    offsets = torch.tensor([0, R], dtype=torch.int32, device=DEV)
+    y = torch.full((R, N), 7.0, device=DEV)
+    moe.moe_q4_linear(s, x, offsets, q, scale, None, y)
+    k = torch.arange(0, K, 4099, device=DEV)
+    k = k[k != K - 1]
+    want = float(torch.where(k % 2 == 0, 2.0, 1.0).sum()) + 3.0
+    rows = torch.ones(R, dtype=torch.bool, device=DEV)
+    rows[127::128] = False
+    assert bool((y[rows] == want).all()) and not torch.isfinite(y[~rows]).any()
