@@ -165,6 +165,15 @@ struct Run {                               // BYTES consecutive bytes, from an a
     __device__ __forceinline__ uint32_t byte(int i) const { return (w[i / 4] >> (i % 4 * 8)) & 0xffu; }
 };
 
+// What a wavefront's lanes have written to its own LDS is read by other lanes behind this, and what they have read is written
+// over behind it.  (It takes a wavefront's accesses in order: nothing is waited for, but nothing is moved across either.)
+__device__ __forceinline__ void lds_handover()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 struct Q4Args {
     const uint16_t *x;
     const int32_t *offsets;
@@ -339,6 +348,7 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
                 unrolled<8>([&](auto ic) {
                     constexpr int i = decltype(ic)::value, c = i / 4;
                     if (s + i >= s1) return;
+                    lds_handover();
                     x_into_lds();
                     codes_into_lds(integral_constant<int, i % 2>{});
                     load_x(min(s + i + 1, s1 - 1));
@@ -351,6 +361,7 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
                         mine[t] = sc[c][t].template quarter<i % 4>();
                         if constexpr (ZEROS) zeros[t] = zr[c][t].template quarter<i % 4>();
                     }
+                    lds_handover();
                     use(mine, zeros);
                 });
             }
@@ -376,14 +387,17 @@ __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
                 for (int i = 0; i < XP; ++i)
                     xr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
                         rsx, steps * 256 + (lane & 31) * 8 < a.K ? x_at + i * 4 * a.K + steps * 512 : 0x7ffffff0, 0, 0));
+                lds_handover();
                 x_into_lds();
                 codes_into_lds(integral_constant<int, 0>{});
+                lds_handover();
                 use(mine, zeros);
             }
         }
 
         // total[t][c]: row row0 + 4 oct + c, column fr of group t
-        // (over x, whose reads are through: a wavefront's accesses are taken in order)
+        // (over x, whose reads are through)
+        lds_handover();
         float *mine = reinterpret_cast<float *>(own);
 #pragma unroll
         for (int t = 0; t < NT; ++t)

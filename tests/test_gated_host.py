@@ -142,3 +142,18 @@ def test_silu_is_refused_by_the_plain_layers_backward_pass():
     args = [ok, ok, z, C.c_int32(0), *[ok] * 19, z]
     assert L.moe_layer_backward(C.byref(s), *args) == 2 and "gated" in moe.moe_last_error()
     assert moe.moe_backward_workspace_bytes(shape(act="gelu")) > 0
+
+
+def test_values_that_lanes_pass_through_lds_have_a_barrier_between():
+    """In the 4-bit kernel of few rows a wavefront's lanes write x, codes and sums to LDS that other lanes of it read, with no
+    workgroup barrier in between: a handover stands in front of the first write and of the read behind it, whatever the
+    compiler knows of the addresses."""
+    import os
+    path = os.path.join(os.path.dirname(moe.lib_path()), "csrc", "q4.hip")
+    with open(path) as f:
+        text = f.read()
+    body = text[text.index("void q4_stream_kernel("):text.index("many rows per expert")]
+    calls = [line.strip() for line in body.splitlines()
+             if line.strip().startswith(("lds_handover();", "x_into_lds();", "codes_into_lds(", "use(", "float *mine"))]
+    step = ["lds_handover();", "x_into_lds();", "codes_into_lds(", "lds_handover();", "use("]
+    assert len(calls) == 12 and all(c.startswith(p) for c, p in zip(calls, step + step + ["lds_handover();", "float *mine"]))
