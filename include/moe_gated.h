@@ -44,7 +44,7 @@ moe_status moe_pack_gated_weights(const moe_shape *s, const void *W13, const voi
 size_t moe_gated_workspace_bytes(const moe_shape *s);
 
 /* The block.  ye [rows, d_model].  pre, hid: both NULL, or (MOE_BF16) what the backward pass reads:
- * pre fp16 [rows, 2 d_ff] = [G | U], hid fp16 [rows, d_ff] = H, each rounded from fp32. */
+ * pre fp16 [rows, 2 d_ff] = [G | U], hid fp16 [rows, d_ff] = H, each rounded from fp32 (to infinity past 65504). */
 moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offsets,
                          const void *W13p, const void *W2p, void *ye, void *pre, void *hid,
                          void *workspace, void *stream);
@@ -62,7 +62,8 @@ size_t moe_gated_backward_workspace_bytes(const moe_shape *s);
  *   dxe        bf16 [rows, d_model]; dW13, dW2 bf16 in the weights' layouts: overwritten, zeros for an
  *              expert without rows
  * The products run on bf16 operands (dG, dU and H rounded to bf16) with fp32 sums, each rounded once to its
- * gradient's type.
+ * gradient's type.  A G or U past 65504 enters as infinity: with act'(G) and act(G) as their limits, and 0 where dH or act'(G)
+ * is 0, so that a closed gate has gradients of 0 whatever its size; else the gradients are not finite.
  */
 moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int32_t *offsets,
                                   const void *W13, const void *W2, const void *W13p, const void *pre,

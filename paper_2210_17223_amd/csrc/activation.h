@@ -66,6 +66,8 @@ __device__ __forceinline__ float sigmoid_fast(float v)
 
 // The gated block's activation of a 16-bit layer, and with its derivative (the derivative's name for the sums: s for the
 // logistic function of silu, s = (1 + tanh u) / 2 for the tanh form).
+// With its derivative it is taken of gates as they were kept, in fp16: a gate past 65504 is infinite there, and value and slope
+// are the limits, finite but for the value of +infinity.  (NaN stays NaN.)
 template <int ACT>
 __device__ __forceinline__ float gate_value(float v)
 {
@@ -78,18 +80,20 @@ __device__ __forceinline__ float gate_value(float v)
 template <int ACT>
 __device__ __forceinline__ void gate_value_and_slope(float v, float &value, float &slope)
 {
+    constexpr float most = 65504.0f;
     if constexpr (ACT == MOE_ACT_SILU) {
-        const float s = sigmoid_fast(v);
-        value = v * s;
-        slope = __builtin_fmaf(value, 1.0f - s, s);
+        const float above = __builtin_elementwise_maximum(v, -most), s = sigmoid_fast(above);
+        value = above * s;
+        slope = __builtin_fmaf(__builtin_elementwise_minimum(value, most), 1.0f - s, s);
     } else if constexpr (ACT == MOE_ACT_GELU_ERF) {
         value = gelu_erf_fast(v);
-        slope = gelu_erf_derivative_fast(v);
+        slope = gelu_erf_derivative_fast(__builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -most), most));
     } else if constexpr (ACT == MOE_ACT_GELU_TANH) {
         constexpr float c = 0.7978845608028654f, a = 0.044715f;
-        const float s = half_one_plus_tanh(v);
-        value = v * s;
-        slope = __builtin_fmaf(2.0f * value * (1.0f - s), c * (1.0f + 3.0f * a * v * v), s);
+        const float above = __builtin_elementwise_maximum(v, -most), in = __builtin_elementwise_minimum(above, most);
+        const float s = half_one_plus_tanh(in);
+        value = above * s;
+        slope = __builtin_fmaf(2.0f * (in * s) * (1.0f - s), c * (1.0f + 3.0f * a * in * in), s);
     } else if constexpr (ACT == MOE_ACT_RELU) {
         value = __builtin_elementwise_maximum(v, 0.0f);
         slope = v > 0.0f ? 1.0f : 0.0f;

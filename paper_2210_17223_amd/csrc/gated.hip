@@ -385,6 +385,16 @@ __global__ __launch_bounds__(256) void gated_f32_kernel(const float *__restrict_
 }
 
 // ---------------------------------------------------------------- backward: dH and through the gate
+// a b, and 0 where either is 0 and the other infinite
+__device__ __forceinline__ float times_or_zero(float a, float b)
+{
+    float v = 0.0f;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
+#endif
+    return v;
+}
+
 // C tile dH = dye W2^T; out = [dG | dU] = [dH U act'(G) | dH act(G)], both bf16, G and U from pre [rows, 2 h].  G and U come
 // into LDS behind the last stages, 32 rows of a wavefront's part at a time, and are turned into dG and dU in their places; of
 // 256 x 256 tiles the rows from 64 on follow while the first ones are computed.  16384 rows, 8 experts, 2048 x 5632: 414 us alone,
@@ -431,9 +441,10 @@ __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
                 for (int c = 0; c < 4; ++c) {
                     float value, slope;
                     gate_value_and_slope<ACT>(static_cast<float>(g[i][c]), value, slope);
+                    // (0 times what fp16 has made infinite is 0, as it is with the value itself)
                     const float dh = acc[i][j][c];
-                    dg[c] = dh * static_cast<float>(v[i][c]) * slope;
-                    du[c] = dh * value;
+                    dg[c] = times_or_zero(dh * slope, static_cast<float>(v[i][c]));
+                    du[c] = times_or_zero(dh, value);
                 }
                 store_bf16x4(gp + place(i), dg);
                 store_bf16x4(up + place(i), du);

@@ -345,3 +345,30 @@ def test_another_stream_and_a_graph():
         b.backward()
         torch.cuda.synchronize()
         assert same()
+
+
+@pytest.mark.parametrize("size", [dict(R=50, d=64, h=72), dict(R=2000, d=128, h=1096)], ids=["128", "256"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_gates_that_fp16_does_not_hold(act, size):
+    """Every other gate lies far below -65504 in every row, and the values of some of these gates past 65504: kept in fp16
+    they are infinite.  These gates are closed, so the forward pass is finite, and what they give to any gradient is 0.  One
+    row has an open gate past 65504 and a gradient of 0."""
+    b = Block(E=1, act=act, **size)
+    R, h = b.R, b.h
+    b.xe[:R] = b.xe[:R].abs() + 0.5
+    b.W13[0, :, :h:2] = -b.W13[0, :, :h:2].abs() * 1e5 - 2e4
+    b.W13[0, :, h:2 * h:4] *= 1e6
+    b.W13[0, 0, 1] = 6e4                              # gate 1: open, past 65504 in the last row alone
+    b.xe[:R, 0], b.xe[R - 1, 0] = 0.0, 4.0
+    b.W13[0, :, h + 1] *= 1e-4
+    b.dye[R - 1] = 0.0
+    moe.moe_pack_gated_weights(b.s, b.W13, b.W2, b.W13p, b.W2p)
+    b.forward(True)
+    G, U = b.pre[:R, :h], b.pre[:R, h:]
+    assert bool((G[:, ::2] == -math.inf).all()) and bool(torch.isinf(U[:, ::4]).any()) and bool(torch.isfinite(b.ye[:R]).all())
+    assert float(G[R - 1, 1]) == math.inf and bool(torch.isfinite(G[:R - 1, 1::2]).all())
+    kept = b.backward()
+    again = b.backward(kept=False)
+    assert all(torch.equal(p, q) for p, q in zip(kept, again))
+    b.pre[:R] = b.pre[:R].clamp(-65504, 65504)        # (as the formulas take them)
+    check_backward(b, *kept)
