@@ -278,3 +278,18 @@ def test_captured_into_a_graph_replays_the_same_bits():
         torch.cuda.synchronize()
         assert torch.equal(r2, r) and torch.equal(nx2, nx) and all(torch.equal(outs[k], o[k]) for k in o)
         c.after_backward(r)                       # the program's own eager work in between
+
+
+# next in fp32 beside a residual in bf16: pieces of eight columns of which next has sixteen bytes twice
+WIDE_NEXT = [
+    dict(T=3, d=8, kind="layer", dtype="f32", res="bf16", z="f16"), dict(T=37, d=512, dtype="f32", res="bf16", z="bf16"),
+    dict(T=300, d=1000, kind="layer", dtype="f32", res="bf16", z="f16", gate_tokens=7), dict(T=16, d=4096, dtype="f32", res="bf16", z="bf16"),
+    dict(T=9, d=4104, kind="layer", dtype="f32", res="bf16", z="f16"), dict(T=5, d=8200, dtype="f32", res="bf16", z="bf16"),
+    dict(T=3, d=16384, kind="layer", dtype="f32", res="bf16", z="f16"), dict(T=9, d=2056, dtype="f32", res="bf16"),
+]
+
+
+@pytest.mark.parametrize("kw", WIDE_NEXT, ids=lambda kw: "-".join(str(v) for v in kw.values()))
+def test_next_in_fp32_beside_a_bf16_residual(kw):
+    test_after_and_its_gradients(kw)
+    test_before_and_its_gradients(kw)
