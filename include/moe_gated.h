@@ -70,6 +70,13 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
                                   const void *hid, const void *dye, void *dxe, void *dW13, void *dW2,
                                   void *workspace, void *stream);
 
+/* Which kernel the calls above launch for a GEMM of a block of shape s (0: first projections; 1: second; of the backward
+ * pass 2: dH; 3: dxe; 4: dW2; 5: dW13), written to name (host, len bytes, always terminated) as "<kernel> <tile rows>x<tile
+ * columns>", with " deep" behind it where five stages of loads are on their way and " tail" where the depth is not taken in whole
+ * stages of 64, so that a measurement or a test can say which kernel it ran.  MOE_EINVAL for which outside 0..5, a null name or
+ * len == 0; else as the call that launches it. */
+moe_status moe_gated_gemm_kernel(const moe_shape *s, int32_t which, char *name, size_t len);
+
 /* ---- weights held as 4-bit codes -------------------------------------------------------------
  *
  *   w[n, k] = (code[n, k] - zero[n, k / group]) * scale[n, k / group]         y[r, n] = sum_k x[r, k] w[e][n, k]

@@ -1258,6 +1258,17 @@ void launch_gemm(const uint16_t *A, const uint16_t *W, void *C, _Float16 *P, con
         launch_gemm_k<EPI, ACT, false>(A, W, C, P, items, N, K, grid_items, stage, st);
 }
 
+}  // namespace
+
+// As wide_wgrad_tiles, for sums rounded to bf16, whose kernel takes any M and N.
+bool wide_weight_grad_bf16(int E, int M, int N, int64_t max_rows)
+{
+    const uint64_t span = static_cast<uint64_t>(max_rows + 192) * static_cast<uint64_t>(std::max(M, N) + 256) * 2;
+    return static_cast<int64_t>(E) * ceil_div(M, 256) * ceil_div(N, 256) >= 256 && span < (1ull << 31);
+}
+
+namespace {
+
 // 256 x 256 tiles on four wavefronts when they fit the matrix, there are 512 of them, and the buffer offsets (an expert's
 // rows times the row length, in bytes) stay below 2^31.  Time of both gradients / of the training step over that with 128 x
 // 128 tiles, 60 layers of 1024 .. 16384 tokens, rows spread evenly; by Zipf(1.2): 512 .. 599 tiles 0.66 .. 0.83 / 0.87 .. 0.88;
@@ -1273,13 +1284,6 @@ bool wide_wgrad_tiles(int E, int M, int N, int64_t max_rows)
     return M % 256 == 0 && N % 256 == 0 && static_cast<int64_t>(E) * (M / 256) * (N / 256) >= 512 && span < (1ull << 31);
 }
 
-// The same for sums rounded to bf16, whose kernel takes any M and N.
-bool wide_wgrad_tiles_bf16(int E, int M, int N, int64_t max_rows)
-{
-    const uint64_t span = static_cast<uint64_t>(max_rows + 192) * static_cast<uint64_t>(std::max(M, N) + 256) * 2;
-    return static_cast<int64_t>(E) * ceil_div(M, 256) * ceil_div(N, 256) >= 256 && span < (1ull << 31);
-}
-
 // dW[e] [M][N] = A[rows of e]^T B[rows of e] from row-major operands
 template <bool AF16, typename TOut>
 void launch_wgrad(const uint16_t *A, const uint16_t *B, TOut *C, const int32_t *offsets, int E, int M,
@@ -1287,7 +1291,7 @@ void launch_wgrad(const uint16_t *A, const uint16_t *B, TOut *C, const int32_t *
 {
     hipEvent_t t0, t1;
     constexpr bool F32 = std::is_same_v<TOut, float>;
-    if (F32 ? wide_wgrad_tiles(E, M, N, max_rows) : wide_wgrad_tiles_bf16(E, M, N, max_rows)) {
+    if (F32 ? wide_wgrad_tiles(E, M, N, max_rows) : wide_weight_grad_bf16(E, M, N, max_rows)) {
         constexpr size_t kLds4 = kW4Lds;
         auto kern = wgrad_w4_kernel<AF16, TOut>;
         static PerDeviceOnce once;

@@ -24,6 +24,8 @@ moe_status launch_second_gemm(const moe_shape &s, const void *hidden, const void
 // bwd.hip: dW[e] [M][N] = A[rows of e]^T B[rows of e] rounded to bf16; A holds fp16 values where a_f16
 void launch_weight_grad_bf16(bool a_f16, const uint16_t *A, const uint16_t *B, uint16_t *C, const int32_t *offsets, int E,
                              int M, int N, int64_t max_rows, int stage, hipStream_t st);
+// bwd.hip: whether that runs on 256 x 256 tiles, else on 128 x 128
+bool wide_weight_grad_bf16(int E, int M, int N, int64_t max_rows);
 // api.hip: the checks that every call makes of its shape
 moe_status check_layer_shape(const moe_shape *s);
 // api.hip: MOE_EUNSUPPORTED where the shape's activation is the gated block's alone; for the calls whose experts are two plain products

@@ -14,6 +14,7 @@
 #include "moe_gated.h"
 
 #include <algorithm>
+#include <cstdio>
 
 #include <hip/hip_ext.h>
 
@@ -638,6 +639,10 @@ GemmPlan plan_gated(int64_t rows, int E, int N, int K, bool few, bool mid, int64
     return gp;
 }
 
+// Whether the form of a tile kernel that takes its depth in whole stages of 64 serves (with loads that run on from tile to
+// tile, also four of them at least); else that with a tail.
+bool whole_stages(const GemmPlan &gp, int K) { return K % 64 == 0 && (gp.bn != 256 || K >= 256); }
+
 struct GatedWorkspace {
     Workspace lists;           // work lists of the two GEMMs, and the hidden activations
     size_t bytes;
@@ -748,24 +753,26 @@ void launch_first(const moe_shape &s, const uint16_t *xe, const uint16_t *W13p, 
         else if (gp.deep) tile(gated_tile_kernel<ACT, KEEP, TAIL, true>, once[2], kW4Lds);
         else tile(gated_tile_kernel<ACT, KEEP, TAIL, false>, once[3], w4_lds(128, 128));
     };
-    if (K % 64 == 0 && (gp.bn != 256 || K >= 256)) shape(std::false_type{});
+    if (whole_stages(gp, K)) shape(std::false_type{});
     else shape(std::true_type{});
 }
+
+// fp32 tiles of 64 rows where they are a few per compute unit (32 / 64 rows a tile, us of the block: 896 tiles 124 / 128, 470 86 / 100, 1280
+// 169 / 158, 1400 58 / 56, 2496 236 / 227, 5120 659 / 610).
+bool tall_f32_tiles(int64_t rows, int E, int d_ff) { return (rows / 64 + E / 2) * ((d_ff + 31) / 32) >= 1200; }
 
 void launch_first_gemm(const moe_shape &s, const void *xe, const void *W13p, void *H, void *pre, const GemmPlan &gp,
                        const WorkItem *items, const DirectTiles &direct, hipStream_t st)
 {
     with_activation(s.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        // Tiles of 64 rows where they are a few per compute unit (32 / 64 rows a tile, us of the block: 896 tiles 124 / 128, 470 86 / 100, 1280
-        // 169 / 158, 1400 58 / 56, 2496 236 / 227, 5120 659 / 610).
         auto f32 = [&](auto tmc) {
             constexpr int TM = decltype(tmc)::value;
             launch_timed(gated_f32_kernel<ACT, TM>, block_tile_grid(direct.rows, direct.E, 32 * TM, (s.d_ff + 31) / 32), 256, 0,
                          kStageGemm1, st, static_cast<const float *>(xe), static_cast<const float *>(W13p), static_cast<float *>(H),
                          direct.offsets, direct.E, s.d_ff, s.d_model);
         };
-        if (s.dtype == MOE_F32 && (direct.rows / 64 + direct.E / 2) * ((s.d_ff + 31) / 32) >= 1200)
+        if (s.dtype == MOE_F32 && tall_f32_tiles(direct.rows, direct.E, s.d_ff))
             f32(std::integral_constant<int, 2>{});
         else if (s.dtype == MOE_F32)
             f32(std::integral_constant<int, 1>{});
@@ -821,7 +828,7 @@ void launch_dxe(const moe_shape &s, const uint16_t *dGU, const uint16_t *W13, ui
         else if (gp.deep) tile(rows_bf16_tile_kernel<TAIL, true>, once[2], kW4Lds);
         else tile(rows_bf16_tile_kernel<TAIL, false>, once[3], w4_lds(128, 128));
     };
-    if (K % 64 == 0 && (gp.bn != 256 || K >= 256)) shape(std::false_type{});
+    if (whole_stages(gp, K)) shape(std::false_type{});
     else shape(std::true_type{});
 }
 
@@ -945,6 +952,46 @@ size_t moe_gated_backward_workspace_bytes(const moe_shape *s)
     GatedBwdWorkspace w;
     layout_gated_bwd(*s, nullptr, &w);
     return w.bytes;
+}
+
+moe_status moe_gated_gemm_kernel(const moe_shape *s, int32_t which, char *name, size_t len)
+{
+    if (name == nullptr || len == 0 || which < 0 || which > 5) {
+        set_error("moe_gated_gemm_kernel: which must be in 0..5, name a buffer");
+        return MOE_EINVAL;
+    }
+    const moe_status rc = check_gated(s, which > 1);
+    if (rc != MOE_OK) return rc;
+    const int64_t R = moe_max_rows(s);
+    const int d = s->d_model, h = s->d_ff, NP = gated_packed_columns(h);
+    auto put = [&](const char *kernel, int bm, int bn, const char *form) { std::snprintf(name, len, "%s %dx%d%s", kernel, bm, bn, form); };
+    auto tiles = [&](const char *run, const char *tile, const GemmPlan &gp, int K) {
+        const char *form = whole_stages(gp, K) ? gp.deep ? " deep" : "" : gp.deep ? " deep tail" : " tail";
+        put(gp.bn == 256 ? run : tile, gp.bm, gp.bn, form);
+    };
+    if (which == 0 && s->dtype == MOE_F32) {
+        put("gated_f32_kernel", tall_f32_tiles(R, s->E, h) ? 64 : 32, 32, "");
+    } else if (which == 0) {
+        const GemmPlan gp = plan_gated(R, s->E, NP, d, true, true, R);
+        if (gp.w4) tiles("gated_run_kernel", "gated_tile_kernel", gp, d);
+        else put("gated_stream_kernel", 32, 32, d % 64 == 0 ? "" : " tail");
+    } else if (which == 1 && s->dtype == MOE_F32) {
+        const GemmPlan gp = choose_gemm_plan(*s, 1, 1, s->T);
+        put("grouped_gemm_f32_kernel", gp.bm, gp.bn, "");
+    } else if (which == 1) {
+        expert_gemm_kernel_name(*s, 1, name, len);
+    } else if (which == 2) {
+        const GemmPlan gp = plan_gated(R, s->E, h, d, false, false, R);
+        put("gated_dh_kernel", gp.bm, gp.bn, d % 64 == 0 ? "" : " tail");
+    } else if (which == 3) {
+        const GemmPlan gp = plan_gated(R, s->E, d, 2 * h, false, true, R);
+        tiles("rows_bf16_run_kernel", "rows_bf16_tile_kernel", gp, 2 * h);
+    } else {
+        const int M = which == 4 ? h : d, N = which == 4 ? d : 2 * h;
+        if (wide_weight_grad_bf16(s->E, M, N, R)) put("wgrad_w4_kernel", 256, 256, "");
+        else put("wgrad_gemm_kernel", 128, 128, "");
+    }
+    return MOE_OK;
 }
 
 moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int32_t *offsets, const void *W13, const void *W2,

@@ -45,8 +45,17 @@ def _lib():
             f = getattr(L, "moe_" + name)
             f.restype = C.c_int
             f.argtypes = [sp] + [vp] * pointers
+        L.moe_gated_gemm_kernel.restype = C.c_int
+        L.moe_gated_gemm_kernel.argtypes = [sp, C.c_int32, C.c_char_p, C.c_size_t]
         _ready = True
     return L
+
+
+def moe_gated_gemm_kernel(s: Shape, which: int) -> str:
+    """Name, tile and form of the kernel of a gated block's GEMM (0: first projections, 1: second, 2: dH, 3: dxe, 4: dW2, 5: dW13)."""
+    buf = C.create_string_buffer(96)
+    _check(_lib().moe_gated_gemm_kernel(C.byref(s), int(which), buf, C.sizeof(buf)))
+    return buf.value.decode()
 
 
 def moe_gated_packed_bytes(s: Shape) -> int:

@@ -157,3 +157,21 @@ def test_values_that_lanes_pass_through_lds_have_a_barrier_between():
              if line.strip().startswith(("lds_handover();", "x_into_lds();", "codes_into_lds(", "use(", "float *mine"))]
     step = ["lds_handover();", "x_into_lds();", "codes_into_lds(", "lds_handover();", "use("]
     assert len(calls) == 12 and all(c.startswith(p) for c, p in zip(calls, step + step + ["lds_handover();", "float *mine"]))
+
+
+def test_gemm_kernel_names():
+    name = moe.moe_gated_gemm_kernel
+    s = moe.Shape.make(16384, 2048, 8, 5632, 1, 16384, act="silu")
+    assert [name(s, w) for w in range(6)] == ["gated_run_kernel 256x256", "grouped_gemm_mfma_kernel 128x256", "gated_dh_kernel 256x256",
+                                              "rows_bf16_run_kernel 128x256", "wgrad_w4_kernel 256x256", "wgrad_w4_kernel 256x256"]
+    s = moe.Shape.make(512, 128, 4, 256, 1, 512, act="silu", dtype="f32")
+    assert [name(s, w) for w in range(2)] == ["gated_f32_kernel 32x32", "grouped_gemm_f32_kernel 32x32"]
+    for bad, frag in ((2, "bf16"), (6, "0..5"), (-1, "0..5")):
+        with pytest.raises(moe.MoeError, match=frag):
+            name(s, bad)
+    with pytest.raises(moe.MoeError):
+        name(shape(d_model=100), 0)
+    L, buf = gated_binding._lib(), C.create_string_buffer(8)
+    assert L.moe_gated_gemm_kernel(C.byref(s), 0, None, 8) == 1 and L.moe_gated_gemm_kernel(C.byref(s), 0, buf, 0) == 1
+    assert L.moe_gated_gemm_kernel(None, 0, buf, 8) == 1
+    assert L.moe_gated_gemm_kernel(C.byref(s), 0, buf, 8) == 0 and buf.value == b"gated_f"

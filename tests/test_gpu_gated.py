@@ -347,7 +347,7 @@ def test_another_stream_and_a_graph():
         assert same()
 
 
-@pytest.mark.parametrize("size", [dict(R=50, d=64, h=72), dict(R=2000, d=128, h=1096)], ids=["128", "256"])
+@pytest.mark.parametrize("size", [dict(R=50, d=64, h=72), dict(R=2000, d=128, h=1096), dict(R=4000, d=1024, h=2056)], ids=["few", "128", "256"])
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
 def test_gates_that_fp16_does_not_hold(act, size):
     """Every other gate lies far below -65504 in every row, and the values of some of these gates past 65504: kept in fp16
@@ -355,6 +355,7 @@ def test_gates_that_fp16_does_not_hold(act, size):
     row has an open gate past 65504 and a gradient of 0."""
     b = Block(E=1, act=act, **size)
     R, h = b.R, b.h
+    assert moe.moe_gated_gemm_kernel(b.s, 2) == "gated_dh_kernel " + ("256x256" if R == 4000 else "128x128")
     b.xe[:R] = b.xe[:R].abs() + 0.5
     b.W13[0, :, :h:2] = -b.W13[0, :, :h:2].abs() * 1e5 - 2e4
     b.W13[0, :, h:2 * h:4] *= 1e6
