@@ -42,8 +42,9 @@ class TrainBlock:
         self.dr, self.dx, self.dz, self.dxn = new(T, d, dtype=torch.float32), new(T, d, dtype=torch.float32), new(T, d), new(T, d)
         self.dW13, self.dW2 = torch.empty_like(self.W13), torch.empty_like(self.W2)
         self.dw0, self.dw1, self.dw2 = (torch.empty_like(self.w0) for _ in range(3))
-        self.ws = new(moe.moe_gated_workspace_bytes(s), dtype=torch.uint8)
-        self.bwd_ws = new(moe.moe_gated_backward_workspace_bytes(s), dtype=torch.uint8)
+        # (of calls that are given pre and hid)
+        self.ws = new(moe.moe_gated_kept_workspace_bytes(s), dtype=torch.uint8)
+        self.bwd_ws = new(moe.moe_gated_kept_backward_workspace_bytes(s), dtype=torch.uint8)
         self.norm_ws = new(moe.moe_norm_workspace_bytes(n), dtype=torch.uint8)
 
     def forward(self, x):

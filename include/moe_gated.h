@@ -40,8 +40,9 @@ size_t moe_gated_packed_bytes(const moe_shape *s);
 moe_status moe_pack_gated_weights(const moe_shape *s, const void *W13, const void *W2, void *W13p,
                                   void *W2p, void *stream);
 
-/* Host, pure.  Bytes of workspace of moe_gated_ffn. */
+/* Host, pure.  Bytes of workspace of moe_gated_ffn; of one that is given pre and hid (0 if unsupported). */
 size_t moe_gated_workspace_bytes(const moe_shape *s);
+size_t moe_gated_kept_workspace_bytes(const moe_shape *s);
 
 /* The block.  ye [rows, d_model].  pre, hid: both NULL, or (MOE_BF16) what the backward pass reads:
  * pre fp16 [rows, 2 d_ff] = [G | U], hid fp16 [rows, d_ff] = H, each rounded from fp32 (to infinity past 65504). */
@@ -49,8 +50,9 @@ moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offs
                          const void *W13p, const void *W2p, void *ye, void *pre, void *hid,
                          void *workspace, void *stream);
 
-/* Host, pure.  Bytes of workspace of moe_gated_ffn_backward; 0 if unsupported. */
+/* Host, pure.  Bytes of workspace of moe_gated_ffn_backward; of one that is given pre and hid; 0 if unsupported. */
 size_t moe_gated_backward_workspace_bytes(const moe_shape *s);
+size_t moe_gated_kept_backward_workspace_bytes(const moe_shape *s);
 
 /*
  * The block's gradients for a loss whose gradient with respect to ye is dye.  MOE_BF16 layers.

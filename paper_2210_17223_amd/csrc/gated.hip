@@ -644,8 +644,8 @@ GemmPlan plan_gated(int64_t rows, int E, int N, int K, bool few, bool mid, int64
 bool whole_stages(const GemmPlan &gp, int K) { return K % 64 == 0 && (gp.bn != 256 || K >= 256); }
 
 struct GatedWorkspace {
-    Workspace lists;           // work lists of the two GEMMs, and the hidden activations
-    size_t bytes;
+    Workspace lists;           // work lists of the two GEMMs, and (last) the hidden activations
+    size_t bytes, kept_bytes;  // kept_bytes: where the caller keeps those
 };
 void layout_gated(const moe_shape &s, void *base, GatedWorkspace *w)
 {
@@ -667,6 +667,7 @@ void layout_gated(const moe_shape &s, void *base, GatedWorkspace *w)
     w->lists.gp[1] = choose_gemm_plan(s, 1, 1, s.T);
     for (int g = 0; g < 2; ++g)
         w->lists.items[g] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->lists.gp[g].max_items));
+    w->kept_bytes = off;
     w->lists.hidden = take(static_cast<size_t>(R) * s.d_ff * (f32 ? 4 : 2));
     w->bytes = off;
 }
@@ -674,7 +675,7 @@ void layout_gated(const moe_shape &s, void *base, GatedWorkspace *w)
 struct GatedBwdWorkspace {
     Workspace lists, again;    // of dH and dxe; of the first projections, computed again
     uint16_t *dGU, *pre, *hid; // [R][2 h], [R][2 h], [R][h]
-    size_t bytes;
+    size_t bytes, kept_bytes;  // kept_bytes: without what only first projections computed again need, which lies last
 };
 void layout_gated_bwd(const moe_shape &s, void *base, GatedBwdWorkspace *w)
 {
@@ -693,10 +694,11 @@ void layout_gated_bwd(const moe_shape &s, void *base, GatedBwdWorkspace *w)
     w->again.gp[1] = w->lists.gp[1];
     for (int g = 0; g < 2; ++g)
         w->lists.items[g] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->lists.gp[g].max_items));
-    w->again.items[0] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->again.gp[0].max_items));
-    w->again.items[1] = w->lists.items[1];
     const size_t Rh = static_cast<size_t>(R) * s.d_ff;
     w->dGU = reinterpret_cast<uint16_t *>(take(Rh * 4));
+    w->kept_bytes = off;
+    w->again.items[0] = reinterpret_cast<WorkItem *>(take(sizeof(WorkItem) * w->again.gp[0].max_items));
+    w->again.items[1] = w->lists.items[1];
     w->pre = reinterpret_cast<uint16_t *>(take(Rh * 4));
     w->hid = reinterpret_cast<uint16_t *>(take(Rh * 2));
     w->bytes = off;
@@ -913,6 +915,14 @@ size_t moe_gated_workspace_bytes(const moe_shape *s)
     return w.bytes;
 }
 
+size_t moe_gated_kept_workspace_bytes(const moe_shape *s)
+{
+    if (check_gated(s, true) != MOE_OK) return 0;
+    GatedWorkspace w;
+    layout_gated(*s, nullptr, &w);
+    return w.kept_bytes;
+}
+
 moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offsets, const void *W13p, const void *W2p,
                          void *ye, void *pre, void *hid, void *workspace, void *stream)
 {
@@ -952,6 +962,14 @@ size_t moe_gated_backward_workspace_bytes(const moe_shape *s)
     GatedBwdWorkspace w;
     layout_gated_bwd(*s, nullptr, &w);
     return w.bytes;
+}
+
+size_t moe_gated_kept_backward_workspace_bytes(const moe_shape *s)
+{
+    if (check_gated(s, true) != MOE_OK) return 0;
+    GatedBwdWorkspace w;
+    layout_gated_bwd(*s, nullptr, &w);
+    return w.kept_bytes;
 }
 
 moe_status moe_gated_gemm_kernel(const moe_shape *s, int32_t which, char *name, size_t len)

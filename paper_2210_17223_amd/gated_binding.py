@@ -31,7 +31,7 @@ def _lib():
     L = lib()
     if not _ready:
         sp, vp = C.POINTER(Shape), C.c_void_p
-        for name in ("packed", "workspace", "backward_workspace"):
+        for name in ("packed", "workspace", "kept_workspace", "backward_workspace", "kept_backward_workspace"):
             f = getattr(L, f"moe_gated_{name}_bytes")
             f.restype = C.c_size_t
             f.argtypes = [sp]
@@ -70,6 +70,16 @@ def moe_gated_backward_workspace_bytes(s: Shape) -> int:
     return int(_lib().moe_gated_backward_workspace_bytes(C.byref(s)))
 
 
+def moe_gated_kept_workspace_bytes(s: Shape) -> int:
+    """Of a call that is given pre and hid."""
+    return int(_lib().moe_gated_kept_workspace_bytes(C.byref(s)))
+
+
+def moe_gated_kept_backward_workspace_bytes(s: Shape) -> int:
+    """Of a call that is given pre and hid."""
+    return int(_lib().moe_gated_kept_backward_workspace_bytes(C.byref(s)))
+
+
 _sizes = {}
 
 
@@ -98,19 +108,21 @@ def moe_gated_ffn(s: Shape, xe, offsets, W13p, W2p, ye, pre, hid, workspace, str
     _check(_lib().moe_gated_ffn(
         C.byref(s), arg(xe, s.torch_dtype, rows * d, "xe"), arg(offsets, torch.int32, s.E + 1, "offsets"),
         arg(W13p, U8, n13, "W13p"), arg(W2p, U8, n2, "W2p"), arg(ye, s.ye_dtype, rows * d, "ye"),
-        opt(pre, F16, rows * 2 * h, "pre"), opt(hid, F16, rows * h, "hid"), arg(workspace, U8, nw, "workspace"),
+        opt(pre, F16, rows * 2 * h, "pre"), opt(hid, F16, rows * h, "hid"),
+        arg(workspace, U8, nw if hid is None else moe_gated_kept_workspace_bytes(s), "workspace"),
         raw_stream(stream, xe)))
 
 
 def moe_gated_ffn_backward(s: Shape, xe, offsets, W13, W2, W13p, pre, hid, dye, dxe, dW13, dW2, workspace,
                            stream=None) -> None:
     rows, n, h, b = moe_max_rows(s), s.E * s.d_model * s.d_ff, s.d_ff, torch.bfloat16
+    nw = moe_gated_backward_workspace_bytes(s) if pre is None else moe_gated_kept_backward_workspace_bytes(s)
     _check(_lib().moe_gated_ffn_backward(
         C.byref(s), arg(xe, b, rows * s.d_model, "xe"), arg(offsets, torch.int32, s.E + 1, "offsets"),
         arg(W13, b, 2 * n, "W13"), arg(W2, b, n, "W2"), arg(W13p, torch.uint8, moe_gated_packed_bytes(s), "W13p"),
         opt(pre, torch.float16, rows * 2 * h, "pre"), opt(hid, torch.float16, rows * h, "hid"),
         arg(dye, b, rows * s.d_model, "dye"), arg(dxe, b, rows * s.d_model, "dxe"), arg(dW13, b, 2 * n, "dW13"),
-        arg(dW2, b, n, "dW2"), arg(workspace, torch.uint8, moe_gated_backward_workspace_bytes(s), "workspace"),
+        arg(dW2, b, n, "dW2"), arg(workspace, torch.uint8, nw, "workspace"),
         raw_stream(stream, xe)))
 
 

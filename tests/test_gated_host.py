@@ -175,3 +175,15 @@ def test_gemm_kernel_names():
     assert L.moe_gated_gemm_kernel(C.byref(s), 0, None, 8) == 1 and L.moe_gated_gemm_kernel(C.byref(s), 0, buf, 0) == 1
     assert L.moe_gated_gemm_kernel(None, 0, buf, 8) == 1
     assert L.moe_gated_gemm_kernel(C.byref(s), 0, buf, 8) == 0 and buf.value == b"gated_f"
+
+
+def test_workspaces_of_calls_that_keep_what_the_backward_pass_reads():
+    s = moe.Shape.make(16384, 2048, 8, 5632, 1, 16384, act="silu")
+    Rh = moe.moe_max_rows(s) * 5632
+    lists = 4 << 20
+    assert moe.moe_gated_workspace_bytes(s) >= 2 * Rh and moe.moe_gated_kept_workspace_bytes(s) <= lists
+    assert moe.moe_gated_backward_workspace_bytes(s) >= 10 * Rh
+    assert 4 * Rh <= moe.moe_gated_kept_backward_workspace_bytes(s) <= 4 * Rh + lists
+    f32 = shape(dtype="f32")
+    for size in (moe.moe_gated_kept_workspace_bytes, moe.moe_gated_kept_backward_workspace_bytes):
+        assert size(f32) == 0 and "bf16" in moe.moe_last_error()

@@ -107,3 +107,24 @@ def test_weight_gradients_beside_the_other_gemms(kept):
         b.backward(kept)                          # the program's own eager work in between
         torch.cuda.synchronize()
         assert same()
+
+
+@pytest.mark.parametrize("kw", [dict(R=40, E=4, d=264, h=136), dict(R=4000, E=4, d=1024, h=2048)], ids=["few", "many"])
+def test_what_is_kept_takes_no_workspace(kw):
+    """Workspaces of exactly the size for calls that are given pre and hid, and nothing behind them is written."""
+    b = Block(**kw)
+    b.forward(True)
+    ye, want = b.ye.clone(), b.backward()
+    for name, size in (("ws", moe.moe_gated_kept_workspace_bytes(b.s)), ("bws", moe.moe_gated_kept_backward_workspace_bytes(b.s))):
+        assert 0 < size < getattr(b, name).numel()
+        held = torch.full((size + 4096,), 255, dtype=torch.uint8, device=b.xe.device)
+        setattr(b, name + "_held", held)
+        setattr(b, name, held[:size])
+    b.ye[:b.R] = 0.0
+    b.forward(True)
+    got = b.backward()
+    assert torch.equal(b.ye, ye) and all(torch.equal(p, q) for p, q in zip(got, want))
+    assert bool((b.ws_held[-4096:] == 255).all()) and bool((b.bws_held[-4096:] == 255).all())
+    for call in (lambda: b.forward(False), lambda: b.backward(kept=False)):
+        with pytest.raises(moe.MoeError, match="workspace"):
+            call()
