@@ -924,8 +924,13 @@ void with_tile(int R, int E, int N, F f)
 // Whether rows go through the kernel for few of them, which takes sixteen of an expert at a time.  That kernel / tiles, us: 16 and 20
 // rows of 4096 x 4096 7 / 10 and 12 / 10, of 8192 x 8192 12 / 18 and 21 / 18, of 2048 x 12000 12 / 13 and 21 / 13; 4 experts, 2048 x 2048, 8
 // and 12 rows each 6 / 8 and 10 / 8.  The gated block, 8 experts of 2048 x 8192, 10 and 14 rows each 52 / 54 and 79 / 54, of 1024 x 4096 26 /
-// 28 and 39 / 28; one expert of 2048 x 5632, 14 and 20 rows 20 / 25 and 34 / 25.
-bool few_rows(int64_t R, int E) { return R <= 16 || R <= 10 * E; }
+// 28 and 39 / 28; one expert of 2048 x 5632, 14 and 20 rows 20 / 25 and 34 / 25.  At most 96 in all, since an expert's sixteens
+// come one after the other, and of many experts' rows a popular one may have many: block, rows spread evenly (by 1 / rank; all
+// of one expert), 64 experts of 2048 x 1536, 96 and 128 rows 67 / 89 (57 / 64; 113 / 42) and 73 / 94 (58 / 65; 150 / 42), of 512 x 1376, 128, 256 and
+// 640 rows 33 / 34 (33 / 30; 100 / 18), 36 / 34 (56 / 30; 195 / 22) and 43 / 34 (106 / 44; 481 / 25); 32 of 2048 x 2048, 96 and 128 rows
+// 47 / 48 (47 / 43) and 52 / 48 (50 / 48); 16 of 1024 x 4096, 96 and 112 rows 34 / 36 (37 / 36) and 36 / 35 (44 / 35); 8 of 4096 x 14336, group 64
+// with zeros, 64 and 80 rows 197 / 311 (214 / 315) and 204 / 310 (219 / 315), group 128 172 / 193 (186 / 198) and 181 / 195 (190 / 202).
+bool few_rows(int64_t R, int E) { return R <= 16 || (R <= 10 * E && R <= 96); }
 
 // rows that are ready
 void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)

@@ -187,3 +187,14 @@ def test_workspaces_of_calls_that_keep_what_the_backward_pass_reads():
     f32 = shape(dtype="f32")
     for size in (moe.moe_gated_kept_workspace_bytes, moe.moe_gated_kept_backward_workspace_bytes):
         assert size(f32) == 0 and "bf16" in moe.moe_last_error()
+
+
+def test_few_rows_of_many_experts_may_be_one_experts():
+    """The kernel for few rows of 4-bit weights, which needs no room for rows made ready, takes at most 96 of any number of experts."""
+    def ready(R, E):
+        s = moe.Shape.make(R, 512, E, 256, 1, R, act="silu")
+        hidden = -(-R * 256 * 2 // 256) * 256
+        assert moe.moe_gated_q4_workspace_bytes(s) - hidden in (0, -(-R * 512 * 2 // 256) * 256 + -(-R * 4 // 256) * 256)
+        return moe.moe_gated_q4_workspace_bytes(s) > hidden
+    assert not any(ready(R, E) for R, E in ((1, 1), (16, 1), (80, 8), (96, 10), (96, 64), (16, 64)))
+    assert all(ready(R, E) for R, E in ((17, 1), (81, 8), (97, 10), (97, 64), (640, 64)))

@@ -362,3 +362,16 @@ def test_linear_past_2_to_31_bytes_of_a_tiles_rows():
     rows = torch.ones(R, dtype=torch.bool, device=DEV)
     rows[127::128] = False
     assert bool((y[rows] == want).all()) and not torch.isfinite(y[~rows]).any()
+
+
+# Few rows of many experts, and the first counts that are too many for that path
+@pytest.mark.parametrize("kw", [dict(R=96, N=300, K=608, group=32, E=64, zeros=True), dict(R=97, N=300, K=608, group=32, E=64),
+                                dict(R=95, N=72, K=512, group=128, E=16, x="f16", counts=[0, 60] + [0] * 13 + [35])],
+                         ids=lambda kw: "-".join(str(v) for v in kw.values() if not isinstance(v, list)))
+def test_linear_of_many_experts(kw):
+    test_linear(kw)
+
+
+@pytest.mark.parametrize("R", [96, 97])
+def test_block_of_many_experts(R):
+    test_gated_ffn(dict(R=R, d=256, h=544, group=32, E=20, zeros=True, spare=0))
