@@ -1260,7 +1260,12 @@ void launch_gemm(const uint16_t *A, const uint16_t *W, void *C, _Float16 *P, con
 
 }  // namespace
 
-// As wide_wgrad_tiles, for sums rounded to bf16, whose kernel takes any M and N.
+// As wide_wgrad_tiles, for sums rounded to bf16, whose kernel takes any M and N.  A gated block's forward and backward pass with
+// 128 x 128 tiles in both gradients / 256 x 256 in that of W13 alone / in both, us, rows spread evenly (by 1 / rank; all of one
+// expert), by the tiles of 256 x 256 of dW2 and dW13: 216 and 432 151 / 139 / 130 (184 / 167 / 154; 258 / 253 / 269); 192, 384 224 / 208 / 190 (288 /
+// 250 / 229; 447 / 393 / 367); 176, 352 310 / 298 / 285 (377 / 333 / 311; 504 / 448 / 415); 128, 256 421 / 390 / 372 (456 / 409 / 381; 517 / 442 /
+// 388); 96, 192 196 / 174 / 169 (232 / 207 / 188; 306 / 271 / 263); 64, 128 82 / 78 / 83 (93 / 93 / 103; 123 / 126 / 148).  So 256 is on the
+// safe side: down to 96 tiles the larger ones are no slower but for a short contraction whose rows are all one expert's.
 bool wide_weight_grad_bf16(int E, int M, int N, int64_t max_rows)
 {
     const uint64_t span = static_cast<uint64_t>(max_rows + 192) * static_cast<uint64_t>(std::max(M, N) + 256) * 2;

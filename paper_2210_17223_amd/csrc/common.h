@@ -166,7 +166,8 @@ struct SideStream {
     hipEvent_t dispatched = nullptr, hidden = nullptr, joined = nullptr;
     uint64_t used = 0;                  // 0: not created yet
 };
-// The one of `st`, held by `enqueue` while the caller enqueues on it; NULL where weight gradients are to run in order on `st`.
+// The one of `st`, held by `enqueue` while the caller enqueues on it; NULL where weight gradients are to run in order on `st`:
+// by `work`, rows x d_model x d_ff of a plain layer.
 SideStream *lend_side_stream(double work, hipStream_t st, std::unique_lock<std::mutex> &enqueue);
 
 // ---- kernel launchers (each only enqueues on `st`) ---------------------------

@@ -1065,7 +1065,12 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
         launch_weight_grad_bf16(false, xeb, w.dGU, static_cast<uint16_t *>(dW13), offsets, s->E, d, 2 * h, R, kStageBwdWgrad1, q);
     };
     std::unique_lock<std::mutex> enqueue;
-    SideStream *side = lend_side_stream(static_cast<double>(R) * d * h, st, enqueue);
+    // (Half as much work again as a plain layer of these sizes.  us of forward and backward pass in order / beside each other, rows
+    // spread evenly (by 1 / rank), by rows x d_model x d_ff: 4e8 87 / 91 (88 / 89), 1.1e9 107 / 110 (113 / 119), 1.5e9 107 / 112 (123 / 128),
+    // 1.6e9 148 / 142 (182 / 178); above the line, which lies at 1.8e9: 5.9e9 184 / 174, 6.4e9 240 / 240 (322 / 284), 1.6e10 545 / 456 (733 / 600),
+    // 1.9e11 3213 / 3160 (4547 / 4306), 4e11 6997 / 6956 (12297 / 11999); past it, at 4.7e11: 5.5e11 8490 / 8696 (14358 / 14405), 1.9e12 28493 /
+    // 29609.)
+    SideStream *side = lend_side_stream(1.5 * static_cast<double>(R) * d * h, st, enqueue);
     if (side == nullptr) {
         hidden_grads();
         input_grads();

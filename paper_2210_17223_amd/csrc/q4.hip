@@ -935,7 +935,6 @@ bool few_rows(int64_t R, int E) { return R <= 16 || (R <= 10 * E && R <= 96); }
 // rows that are ready
 void launch_q4_ready(Q4Args a, int R, int E, int group, int stage, hipStream_t st)
 {
-    const bool gated = a.kind == kOutGated;
     a.E = E;
     with_codes(a, group, [&](auto g, auto zeros) {
         auto launch = [&](auto bmc, auto bnc, auto ksc) {

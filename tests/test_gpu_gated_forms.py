@@ -62,10 +62,10 @@ def test_every_form_is_among_the_cases():
 
 @pytest.mark.parametrize("kept", [True, False], ids=["keep", "recompute"])
 def test_weight_gradients_beside_the_other_gemms(kept):
-    """Rows x d x h above 2.7e9: the weight gradients run on a side stream; in launch order while stages are timed, and in a
+    """Rows x d x h above 1.8e9: the weight gradients run on a side stream; in launch order while stages are timed, and in a
     graph.  The same bits each way, on another stream, and from call to call."""
-    b = Block(R=6000, E=3, d=768, h=1000, counts=[5000, 0, 1000])
-    assert moe.moe_max_rows(b.s) * b.d * b.h >= 2.7e9
+    b = Block(R=2600, E=3, d=768, h=1000, counts=[2000, 0, 600])
+    assert 1.8e9 <= moe.moe_max_rows(b.s) * b.d * b.h < 2.7e9
     b.forward(True)
     calls = moe.moe_path_calls(BESIDE)
     want = b.backward(kept)
