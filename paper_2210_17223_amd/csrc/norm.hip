@@ -1,7 +1,8 @@
 // The step between two blocks: r = x + scale gate norm(z), next = norm(r), or next = norm(x) in front of the first one,
 // forward and backward (include/moe_norm.h).
 //
-// All of it is bound by HBM: a row is read once, stays in registers through both norms, and is written once.  TPR threads
+// A row is read once, stays in registers through both norms, and is written once, so that rows of up to 8192 forward and 4096
+// backward are bound by HBM.  TPR threads
 // (a wavefront, or a block) own a row, EPT of its columns each; a run of consecutive rows is one group of TPR threads' work,
 // which keeps the vectors (weights, biases, gates) in registers; the forward pass has the next row's loads on their way
 // while it reduces this one's.  Statistics are fp32: the mean first, then the sum of squares around it, from the registers.
@@ -10,6 +11,12 @@
 // Measured: forward, 32768 x 2048, fp32 x and z, bf16 next (0.94 GB) 188 us, 5.0 TB/s; 16384 x 4096, bf16 throughout, layer
 // (0.54 GB) 106 us, 5.1 TB/s, its backward pass (0.81 GB, and 42 MB of partial sums both ways) 195 + 9 us, 4.3 TB/s.  A plain
 // copy reaches 4.5 to 4.6 TB/s on these cards.
+// Past these widths a block of 1024 threads, which has 128 registers a thread, does not hold a row and its vectors, and what
+// it spills goes through the caches once a row: forward with z past 8192 34 to 97 registers, backward behind a block up to 8192 up to 60 and
+// past it 185 to 385 (up to 4096 at most 18: with biases on eight bf16 columns a thread).  TB/s of the bytes that a row needs, forward /
+// backward / the norm in front of the first block alone, 64 M values, bf16 layer with gates (fp32 x and z, RMS): d = 4096 4.6 / 4.2 / 6.1
+// (5.0 / 4.8 / 5.0), 5120 4.5 / 2.2 / 5.4 (5.0 / 3.0 / 5.1), 8192 4.9 / 3.7 / 6.0 (5.1 / 4.3 / 5.1), 12288 2.8 / 0.6 / 5.6 (3.0 / 1.1 / 5.2),
+// 16384 3.1 / 0.7 / 6.1 (3.3 / 1.2 / 5.3).  (At 5120 and 12288 three of eight and a quarter of the threads have no columns, too.)
 #include "common.h"
 #include "moe_norm.h"
 
@@ -676,7 +683,7 @@ moe_status launch_norm_backward(const moe_norm_shape &n, NormArgs a, bool after,
         };
         using std::integral_constant;
         // As few columns per thread as a block of 1024 allows: without the next row's loads on their way in registers
-        // and with at most 128 of these, other wavefronts' rows cover a row's latency (16384 rows of 4096, bf16 throughout,
+        // and with 128 of these, other wavefronts' rows cover a row's latency, also where that spills some (16384 rows of 4096, bf16 throughout,
         // layer, with sixteen columns per thread and a row ahead 296 us, with eight 313, without the row ahead 195; fp32
         // throughout with eight columns 425, with four 358).
         if constexpr (row_vec(decltype(res)::value, decltype(z)::value) == 4) {
