@@ -149,22 +149,6 @@ moe_status check_supported(const moe_shape &s)
     return MOE_OK;
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define MOE_REQUIRE_PTR(p)                                          \
-    do {                                                            \
-        if ((p) == nullptr || !aligned16(p)) {                      \
-            set_error(#p " is NULL or not 16-byte aligned");        \
-            return MOE_EINVAL;                                      \
-        }                                                           \
-    } while (0)
-#define MOE_OPTIONAL_PTR(p)                                         \
-    do {                                                            \
-        if ((p) != nullptr && !aligned16(p)) {                      \
-            set_error(#p " is not 16-byte aligned");                \
-            return MOE_EINVAL;                                      \
-        }                                                           \
-    } while (0)
 #define MOE_TIMED(stage, stream, expr)        \
     do {                                     \
         prof_begin(stage, stream);           \

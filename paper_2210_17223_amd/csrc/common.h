@@ -28,6 +28,23 @@ moe_status hip_fail(hipError_t e, const char *what);
         if (e_ != hipSuccess) return ::moe::hip_fail(e_, #expr);      \
     } while (0)
 
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+#define MOE_REQUIRE_PTR(p)                                          \
+    do {                                                            \
+        if ((p) == nullptr || !aligned16(p)) {                      \
+            set_error(#p " is NULL or not 16-byte aligned");        \
+            return MOE_EINVAL;                                      \
+        }                                                           \
+    } while (0)
+#define MOE_OPTIONAL_PTR(p)                                         \
+    do {                                                            \
+        if ((p) != nullptr && !aligned16(p)) {                      \
+            set_error(#p " is not 16-byte aligned");                \
+            return MOE_EINVAL;                                      \
+        }                                                           \
+    } while (0)
+
 // Raises a kernel's dynamic-LDS limit once per kernel and per device.  Any host thread may be
 // the first to launch a kernel: the flag word is atomic, and a thread that arrives while
 // another is still setting the attribute waits for it instead of launching too early.
@@ -49,6 +66,7 @@ struct PerDeviceOnce {
 
 __host__ __device__ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline int parts_of(int n, int size) { return (n - 1) / size + 1; }          // ceil_div of n from 1 up to 2^31 - 1
 
 // One output tile of a grouped GEMM: rows [row0, row1) of the expert-major buffer, all
 // owned by `expert`, output columns [n0, n0 + tile width).  expert < 0: no tile.

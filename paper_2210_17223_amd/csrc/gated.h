@@ -7,7 +7,6 @@ namespace moe {
 
 // Packed columns of the two first projections: sixteen of Wg and the same sixteen of Wu in turn.
 inline int gated_packed_columns(int d_ff) { return (d_ff + 15) / 16 * 32; }
-constexpr int kGatedBlock = 16;
 
 // In place of a work list: the experts' offsets, and the most rows there can be.
 struct DirectTiles {

@@ -6,6 +6,11 @@
 // the epilogue, and G and U go to memory only where a backward pass will read them.  The second GEMM is the expert FFN's.
 // Backward: dH = dye W2^T with G and U brought into LDS behind its last stages, dG and dU its epilogue; dxe = [dG | dU] W13^T,
 // one product over 2 d_ff; the weight gradients are the expert FFN's kernels, rounded to bf16.
+// H is rounded to fp16, since the second product's operands are of 16 bits: 2^-11 of a value where bf16 is off by 2^-8 (the block's
+// output 2.9e-4 root mean square from 64-bit results where fp32 throughout and one rounding of the output are 2.1e-4), for a
+// largest value of 65504.  What is kept for the backward pass, G, U and H, is rounded to fp16 for the same reason and to half the bytes;
+// dG, dU and, as an operand, H to bf16, whose range gradients need and which all operands of a product share: 2.4e-3 where one rounding
+// of the gradients alone is 1.7e-3.
 // The loops are the expert FFN's: tiles of 256 columns on gemm_w4_run.h's, 128 x 128 on gemm_w4_body.inc's, decode steps
 // straight from global memory.
 #include "activation.h"
@@ -558,7 +563,7 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void rows_bf16_tile_kernel(
 
 // ---------------------------------------------------------------- weight packing
 // out[e][column n of in, packed][k] = in[e][k][n], 64 x 64 tiles through LDS.  GATED: n in [0, 2 h), columns n and h + n are
-// sixteen apart (kGatedBlock), padding columns zeros; else out[e][n][k], from bf16 to fp16.
+// sixteen apart, padding columns zeros; else out[e][n][k], from bf16 to fp16.
 // Bound by HBM: 16 bytes per lane both ways.  8 experts, 2048 x 11264: 178 us, 4.2 TB/s; rows of 2000 bytes (K = 1000) 3.4.
 template <bool GATED>
 __global__ __launch_bounds__(256) void gated_pack_kernel(const uint16_t *__restrict__ in, uint16_t *__restrict__ out, int K,
@@ -855,19 +860,6 @@ moe_status check_gated(const moe_shape *s, bool training)
     return MOE_OK;
 }
 
-bool bad_pointer(const void *p, const char *name, bool optional)
-{
-    if ((p == nullptr && !optional) || (reinterpret_cast<uintptr_t>(p) & 15u) != 0) {
-        set_error(optional ? "%s is not 16-byte aligned" : "%s is NULL or not 16-byte aligned", name);
-        return true;
-    }
-    return false;
-}
-#define MOE_GATED_PTR(p) \
-    if (bad_pointer(p, #p, false)) return MOE_EINVAL
-#define MOE_GATED_OPTIONAL(p) \
-    if (bad_pointer(p, #p, true)) return MOE_EINVAL
-
 }  // namespace
 }  // namespace moe
 
@@ -886,10 +878,10 @@ moe_status moe_pack_gated_weights(const moe_shape *s, const void *W13, const voi
 {
     const moe_status rc = check_gated(s, false);
     if (rc != MOE_OK) return rc;
-    MOE_GATED_PTR(W13);
-    MOE_GATED_PTR(W2);
-    MOE_GATED_PTR(W13p);
-    MOE_GATED_PTR(W2p);
+    MOE_REQUIRE_PTR(W13);
+    MOE_REQUIRE_PTR(W2);
+    MOE_REQUIRE_PTR(W13p);
+    MOE_REQUIRE_PTR(W2p);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int d = s->d_model, h = s->d_ff;
     if (s->dtype == MOE_F32) {
@@ -928,14 +920,14 @@ moe_status moe_gated_ffn(const moe_shape *s, const void *xe, const int32_t *offs
 {
     moe_status rc = check_gated(s, pre != nullptr || hid != nullptr);
     if (rc != MOE_OK) return rc;
-    MOE_GATED_PTR(xe);
-    MOE_GATED_PTR(offsets);
-    MOE_GATED_PTR(W13p);
-    MOE_GATED_PTR(W2p);
-    MOE_GATED_PTR(ye);
-    MOE_GATED_OPTIONAL(pre);
-    MOE_GATED_OPTIONAL(hid);
-    MOE_GATED_PTR(workspace);
+    MOE_REQUIRE_PTR(xe);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(W13p);
+    MOE_REQUIRE_PTR(W2p);
+    MOE_REQUIRE_PTR(ye);
+    MOE_OPTIONAL_PTR(pre);
+    MOE_OPTIONAL_PTR(hid);
+    MOE_REQUIRE_PTR(workspace);
     if ((pre == nullptr) != (hid == nullptr)) {
         set_error("moe_gated_ffn: pre and hid come together (both or neither)");
         return MOE_EINVAL;
@@ -1018,18 +1010,18 @@ moe_status moe_gated_ffn_backward(const moe_shape *s, const void *xe, const int3
 {
     moe_status rc = check_gated(s, true);
     if (rc != MOE_OK) return rc;
-    MOE_GATED_PTR(xe);
-    MOE_GATED_PTR(offsets);
-    MOE_GATED_PTR(W13);
-    MOE_GATED_PTR(W2);
-    MOE_GATED_PTR(W13p);
-    MOE_GATED_OPTIONAL(pre);
-    MOE_GATED_OPTIONAL(hid);
-    MOE_GATED_PTR(dye);
-    MOE_GATED_PTR(dxe);
-    MOE_GATED_PTR(dW13);
-    MOE_GATED_PTR(dW2);
-    MOE_GATED_PTR(workspace);
+    MOE_REQUIRE_PTR(xe);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(W13);
+    MOE_REQUIRE_PTR(W2);
+    MOE_REQUIRE_PTR(W13p);
+    MOE_OPTIONAL_PTR(pre);
+    MOE_OPTIONAL_PTR(hid);
+    MOE_REQUIRE_PTR(dye);
+    MOE_REQUIRE_PTR(dxe);
+    MOE_REQUIRE_PTR(dW13);
+    MOE_REQUIRE_PTR(dW2);
+    MOE_REQUIRE_PTR(workspace);
     if ((pre == nullptr) != (hid == nullptr)) {
         set_error("moe_gated_ffn_backward: pre and hid come together (both or neither)");
         return MOE_EINVAL;

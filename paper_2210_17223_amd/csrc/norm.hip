@@ -571,7 +571,6 @@ __global__ __launch_bounds__(256) void norm_reduce_kernel(NormReduceArgs a)
 }
 
 // ---------------------------------------------------------------- host side
-int parts_of(int n, int size) { return (n - 1) / size + 1; }    // (n up to 2^31 - 1)
 int norm_gates(const moe_norm_shape &n) { return n.gate_tokens != 0 ? parts_of(n.T, n.gate_tokens) : 1; }
 
 // Runs of the backward pass: as many as stay resident (their partial sums are 1 / per_run of a row's traffic).
@@ -606,19 +605,6 @@ moe_status check_norm(const moe_norm_shape *n)
     }
     return MOE_OK;
 }
-
-bool bad_pointer(const void *p, const char *name, bool optional)
-{
-    if ((p == nullptr && !optional) || (reinterpret_cast<uintptr_t>(p) & 15u) != 0) {
-        set_error(optional ? "%s is not 16-byte aligned" : "%s is NULL or not 16-byte aligned", name);
-        return true;
-    }
-    return false;
-}
-#define MOE_NORM_PTR(p) \
-    if (bad_pointer(p, #p, false)) return MOE_EINVAL
-#define MOE_NORM_OPTIONAL(p) \
-    if (bad_pointer(p, #p, true)) return MOE_EINVAL
 
 // f(residual type, z's type or -1)
 template <typename F>
@@ -737,10 +723,10 @@ moe_status moe_norm_before(const moe_norm_shape *n, const void *x, const float *
 {
     const moe_status rc = check_norm(n);
     if (rc != MOE_OK) return rc;
-    MOE_NORM_PTR(x);
-    MOE_NORM_PTR(w_next);
-    MOE_NORM_OPTIONAL(b_next);
-    MOE_NORM_PTR(next);
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_OPTIONAL_PTR(b_next);
+    MOE_REQUIRE_PTR(next);
     NormArgs a = norm_args(*n);
     a.x = x;
     a.w_next = w_next;
@@ -755,14 +741,14 @@ moe_status moe_norm_before_backward(const moe_norm_shape *n, const void *x, cons
 {
     const moe_status rc = check_norm(n);
     if (rc != MOE_OK) return rc;
-    MOE_NORM_PTR(x);
-    MOE_NORM_PTR(w_next);
-    MOE_NORM_PTR(dnext);
-    MOE_NORM_PTR(dr);
-    MOE_NORM_PTR(dx);
-    MOE_NORM_PTR(dw_next);
-    MOE_NORM_OPTIONAL(db_next);
-    MOE_NORM_PTR(workspace);
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_REQUIRE_PTR(dnext);
+    MOE_REQUIRE_PTR(dr);
+    MOE_REQUIRE_PTR(dx);
+    MOE_REQUIRE_PTR(dw_next);
+    MOE_OPTIONAL_PTR(db_next);
+    MOE_REQUIRE_PTR(workspace);
     NormArgs a = norm_args(*n);
     a.r = x;
     a.w_next = w_next;
@@ -780,15 +766,15 @@ moe_status moe_norm_after(const moe_norm_shape *n, const void *x, const void *z,
 {
     const moe_status rc = check_norm(n);
     if (rc != MOE_OK) return rc;
-    MOE_NORM_PTR(x);
-    MOE_NORM_PTR(z);
-    MOE_NORM_PTR(w);
-    MOE_NORM_OPTIONAL(b);
-    MOE_NORM_OPTIONAL(gate);
-    MOE_NORM_PTR(r);
-    MOE_NORM_PTR(w_next);
-    MOE_NORM_OPTIONAL(b_next);
-    MOE_NORM_PTR(next);
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(z);
+    MOE_REQUIRE_PTR(w);
+    MOE_OPTIONAL_PTR(b);
+    MOE_OPTIONAL_PTR(gate);
+    MOE_REQUIRE_PTR(r);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_OPTIONAL_PTR(b_next);
+    MOE_REQUIRE_PTR(next);
     NormArgs a = norm_args(*n);
     a.x = x;
     a.z = z;
@@ -810,22 +796,22 @@ moe_status moe_norm_after_backward(const moe_norm_shape *n, const void *z, const
 {
     const moe_status rc = check_norm(n);
     if (rc != MOE_OK) return rc;
-    MOE_NORM_PTR(z);
-    MOE_NORM_PTR(r);
-    MOE_NORM_PTR(w);
-    MOE_NORM_OPTIONAL(b);
-    MOE_NORM_OPTIONAL(gate);
-    MOE_NORM_PTR(w_next);
-    MOE_NORM_PTR(dr);
-    MOE_NORM_PTR(dnext);
-    MOE_NORM_PTR(dx);
-    MOE_NORM_PTR(dz);
-    MOE_NORM_PTR(dw);
-    MOE_NORM_OPTIONAL(db);
-    MOE_NORM_OPTIONAL(dgate);
-    MOE_NORM_PTR(dw_next);
-    MOE_NORM_OPTIONAL(db_next);
-    MOE_NORM_PTR(workspace);
+    MOE_REQUIRE_PTR(z);
+    MOE_REQUIRE_PTR(r);
+    MOE_REQUIRE_PTR(w);
+    MOE_OPTIONAL_PTR(b);
+    MOE_OPTIONAL_PTR(gate);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_REQUIRE_PTR(dr);
+    MOE_REQUIRE_PTR(dnext);
+    MOE_REQUIRE_PTR(dx);
+    MOE_REQUIRE_PTR(dz);
+    MOE_REQUIRE_PTR(dw);
+    MOE_OPTIONAL_PTR(db);
+    MOE_OPTIONAL_PTR(dgate);
+    MOE_REQUIRE_PTR(dw_next);
+    MOE_OPTIONAL_PTR(db_next);
+    MOE_REQUIRE_PTR(workspace);
     NormArgs a = norm_args(*n);
     a.z = z;
     a.r = r;

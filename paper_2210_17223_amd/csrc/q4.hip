@@ -2,7 +2,8 @@
 // gated feed-forward block on them.
 //
 // The codes go from memory into registers and from there into the matrix instruction: eight codes of a lane become eight
-// 16-bit numbers in place, by masks and an exponent: in bf16 2^-16 (16 + q), in fp16 1024 + q.  Products and sums over a group
+// 16-bit numbers in place, by masks and an exponent (the conversion of narrow integers by their place in a number's digits that Kim,
+// Henry, Fahim and Hassan Awadalla give in "Who Says Elephants Can't Run", 2022): in bf16 2^-16 (16 + q), in fp16 1024 + q.  Products and sums over a group
 // are then exact but for fp32's roundings, and a group's sum is scaled in fp32:
 //   bf16   sum (q - z) x = sum (16 + q) x - (16 + z) sum x, with sum x from one more matrix instruction against ones
 //          (shared by all of a wavefront's columns).  16 is the least that an exponent can add: the code is then the first
@@ -876,8 +877,6 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
 }
 
 // ---------------------------------------------------------------- host side
-unsigned parts_of(int n, int size) { return static_cast<unsigned>((n - 1) / size + 1); }
-
 // f(group, zeros or not) as constants
 template <typename F>
 void with_codes(const Q4Args &a, int group, F f)
@@ -1008,19 +1007,6 @@ void launch_q4_stream(Q4Args a, int R, int E, int group, int x, int stage, hipSt
     });
 }
 
-bool bad_pointer(const void *p, const char *name, bool optional)
-{
-    if ((p == nullptr && !optional) || (reinterpret_cast<uintptr_t>(p) & 15u) != 0) {
-        set_error(optional ? "%s is not 16-byte aligned" : "%s is NULL or not 16-byte aligned", name);
-        return true;
-    }
-    return false;
-}
-#define MOE_Q4_PTR(p) \
-    if (bad_pointer(p, #p, false)) return MOE_EINVAL
-#define MOE_Q4_OPTIONAL(p) \
-    if (bad_pointer(p, #p, true)) return MOE_EINVAL
-
 bool known_group(int group) { return group == 32 || group == 64 || group == 128; }
 
 moe_status check_q4_block(const moe_shape *s)
@@ -1067,12 +1053,12 @@ moe_status moe_q4_linear(const moe_q4_shape *s, const void *x, const int32_t *of
         set_error("moe_q4_linear: group %d must be 32, 64 or 128 and divide K = %d", s->group, s->K);
         return MOE_EUNSUPPORTED;
     }
-    MOE_Q4_PTR(x);
-    MOE_Q4_PTR(offsets);
-    MOE_Q4_PTR(q);
-    MOE_Q4_PTR(scale);
-    MOE_Q4_OPTIONAL(zero);
-    MOE_Q4_PTR(y);
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(q);
+    MOE_REQUIRE_PTR(scale);
+    MOE_OPTIONAL_PTR(zero);
+    MOE_REQUIRE_PTR(y);
     Q4Args a = {};
     a.x = static_cast<const uint16_t *>(x);
     a.offsets = offsets;
@@ -1110,16 +1096,16 @@ moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, c
         set_error("moe_gated_ffn_q4: group %d must be 32, 64 or 128 and divide d_model = %d and d_ff = %d", group, s->d_model, s->d_ff);
         return MOE_EUNSUPPORTED;
     }
-    MOE_Q4_PTR(xe);
-    MOE_Q4_PTR(offsets);
-    MOE_Q4_PTR(q13);
-    MOE_Q4_PTR(scale13);
-    MOE_Q4_OPTIONAL(zero13);
-    MOE_Q4_PTR(q2);
-    MOE_Q4_PTR(scale2);
-    MOE_Q4_OPTIONAL(zero2);
-    MOE_Q4_PTR(ye);
-    MOE_Q4_PTR(workspace);
+    MOE_REQUIRE_PTR(xe);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(q13);
+    MOE_REQUIRE_PTR(scale13);
+    MOE_OPTIONAL_PTR(zero13);
+    MOE_REQUIRE_PTR(q2);
+    MOE_REQUIRE_PTR(scale2);
+    MOE_OPTIONAL_PTR(zero2);
+    MOE_REQUIRE_PTR(ye);
+    MOE_REQUIRE_PTR(workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int R = static_cast<int>(moe_max_rows(s));
     Q4Args a = {};
