@@ -649,37 +649,40 @@ __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_
 
 // The rows of a block's first product, ready for the kernel below: fp16, in the codes' order, each row divided by a power of two
 // such that its largest value is at most 2^15 (bf16's eight digits are then exact down to 2^-29 of it, and below that off by
-// less than fp32 sums of such rows round).  A wavefront per row.
+// less than fp32 sums of such rows round).  A wavefront per row (a grid holds fewer than 2^32 threads: past 2^22 rows it takes
+// several).
 __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict__ x, const int32_t *__restrict__ offsets, int E,
                                                       _Float16 *__restrict__ out, float *__restrict__ row_scale, int K)
 {
-    const int lane = lane_id(), row = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (row >= offsets[E]) return;
-    const uint16_t *src = x + static_cast<size_t>(row) * K;
-    float most = 0.0f;
-    for (int k = lane * 8; k < K; k += kWave * 8) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(src + k);
+    const int lane = lane_id();
+    const unsigned rows = max(offsets[E], 0);
+    for (unsigned row = blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += gridDim.x * 4) {
+        const uint16_t *src = x + static_cast<size_t>(row) * K;
+        float most = 0.0f;
+        for (int k = lane * 8; k < K; k += kWave * 8) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(src + k);
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(v[c] << 16)), fabsf(__uint_as_float(v[c] & 0xffff0000u))));
-    }
-#pragma unroll
-    for (int m = kWave / 2; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
-    // 2^15 / 2^ceil(log2 most), within fp32's range of normal numbers; a row of zeros or without a largest value as it is
-    const int e = static_cast<int>(__float_as_uint(most) >> 23 & 0xff) - 127;
-    const bool plain = most == 0.0f || e == 128;
-    const int shift = plain ? 0 : min(max(14 - e, -126), 126);
-    const float by = __uint_as_float(static_cast<uint32_t>(shift + 127) << 23);
-    if (lane == 0) row_scale[row] = __uint_as_float(static_cast<uint32_t>(127 - shift) << 23);
-    for (int k = lane * 8; k < K; k += kWave * 8) {
-        const u32x4 v = reorder(*reinterpret_cast<const u32x4 *>(src + k));
-        u32x4 o;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const f16x2 h = {static_cast<_Float16>(__uint_as_float(v[c] << 16) * by), static_cast<_Float16>(__uint_as_float(v[c] & 0xffff0000u) * by)};
-            o[c] = __builtin_bit_cast(uint32_t, h);
+            for (int c = 0; c < 4; ++c)
+                most = fmaxf(most, fmaxf(fabsf(__uint_as_float(v[c] << 16)), fabsf(__uint_as_float(v[c] & 0xffff0000u))));
         }
-        *reinterpret_cast<u32x4 *>(out + static_cast<size_t>(row) * K + k) = o;
+#pragma unroll
+        for (int m = kWave / 2; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+        // 2^15 / 2^ceil(log2 most), within fp32's range of normal numbers; a row of zeros or without a largest value as it is
+        const int e = static_cast<int>(__float_as_uint(most) >> 23 & 0xff) - 127;
+        const bool plain = most == 0.0f || e == 128;
+        const int shift = plain ? 0 : min(max(14 - e, -126), 126);
+        const float by = __uint_as_float(static_cast<uint32_t>(shift + 127) << 23);
+        if (lane == 0) row_scale[row] = __uint_as_float(static_cast<uint32_t>(127 - shift) << 23);
+        for (int k = lane * 8; k < K; k += kWave * 8) {
+            const u32x4 v = reorder(*reinterpret_cast<const u32x4 *>(src + k));
+            u32x4 o;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const f16x2 h = {static_cast<_Float16>(__uint_as_float(v[c] << 16) * by), static_cast<_Float16>(__uint_as_float(v[c] & 0xffff0000u) * by)};
+                o[c] = __builtin_bit_cast(uint32_t, h);
+            }
+            *reinterpret_cast<u32x4 *>(out + static_cast<size_t>(row) * K + k) = o;
+        }
     }
 }
 
@@ -1123,7 +1126,7 @@ moe_status moe_gated_ffn_q4(const moe_shape *s, int32_t group, const void *xe, c
     if (many) {
         char *at = static_cast<char *>(workspace) + align_up(static_cast<size_t>(R) * s->d_ff * 2, 256);
         float *row_scale = reinterpret_cast<float *>(at + align_up(static_cast<size_t>(R) * s->d_model * 2, 256));
-        hipLaunchKernelGGL(q4_rows_kernel, dim3(parts_of(R, 4)), dim3(256), 0, st, a.x, offsets, s->E, reinterpret_cast<_Float16 *>(at),
+        hipLaunchKernelGGL(q4_rows_kernel, dim3(std::min(parts_of(R, 4), 1 << 20)), dim3(256), 0, st, a.x, offsets, s->E, reinterpret_cast<_Float16 *>(at),
                            row_scale, s->d_model);
         a.x = reinterpret_cast<const uint16_t *>(at);
         a.row_scale = row_scale;

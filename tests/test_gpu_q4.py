@@ -375,3 +375,22 @@ def test_linear_of_many_experts(kw):
 @pytest.mark.parametrize("R", [96, 97])
 def test_block_of_many_experts(R):
     test_gated_ffn(dict(R=R, d=256, h=544, group=32, E=20, zeros=True, spare=0))
+
+
+def test_block_of_more_rows_than_a_grid_has_wavefronts():
+    """Past 2^26 rows (a grid has fewer than 2^32 threads, and a wavefront makes a row ready); checked on rows all over them."""
+    R, d, h, group = (1 << 26) + 5, 32, 32, 32
+    s = moe.Shape.make(R, d, 1, h, 1, R, act="silu")
+    g = torch.Generator(device=DEV).manual_seed(0)
+    x = torch.randint(-7, 8, (R, d), generator=g, device=DEV, dtype=torch.int8).bfloat16()
+    offsets = torch.tensor([0, R], dtype=torch.int32, device=DEV)
+    w13, w2 = make_codes(g, 1, 2 * h, d, group, True, 0.05), make_codes(g, 1, d, h, group, True, 0.05)
+    ye = torch.full((R, d), 7.0, dtype=torch.float16, device=DEV)
+    ws = torch.full((moe.moe_gated_q4_workspace_bytes(s),), 255, dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q4(s, group, x, offsets, *w13, *w2, ye, ws)
+    at = torch.cat([torch.arange(0, R, 1 << 16, device=DEV), torch.arange(R - 300, R, device=DEV)])
+    b = Q4Block(R=len(at), d=d, h=h, group=group, zeros=True)
+    b.x[:b.R], b.w13, b.w2 = x[at], w13, w2
+    b.run()
+    b.check()
+    assert torch.equal(ye[at], b.ye[:b.R])        # (a row's result does not depend on where it lies)
