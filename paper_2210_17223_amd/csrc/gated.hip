@@ -61,8 +61,8 @@ __device__ __forceinline__ void store_bf16x4(char *p, const float (&v)[4])
 
 // ---------------------------------------------------------------- first projections, tiles of 256 packed columns
 // Bound by the matrix cores at the clock that their energy leaves, as the expert FFN's: 32768 rows, 32 experts, 2048 x 8192,
-// 256 x 256 tiles, 1753 us, 1254 TFLOP/s (a vendor library's dense product of that size 1200); keeping G, U and H for the backward
-// pass, 16384 rows, 8 experts, 2048 x 5632, 632 us, 1196 TFLOP/s.
+// 256 x 256 tiles, 1745 us, 1260 TFLOP/s (a vendor library's dense product of that size 1200); keeping G, U and H for the backward
+// pass, 16384 rows, 8 experts, 2048 x 5632, 596 us, 1269 TFLOP/s.
 // R of a wavefront's rows, from `r` on, as they lie in the patch's rows 16 part .. (W4Place): PIECES 16-byte pieces of 8
 // columns each, to columns col0 + 8 piece of `out`; of 16 pieces the last eight go pair_at columns further on.
 template <int BM, int R, int PIECES>
@@ -403,8 +403,8 @@ __device__ __forceinline__ float times_or_zero(float a, float b)
 
 // C tile dH = dye W2^T; out = [dG | dU] = [dH U act'(G) | dH act(G)], both bf16, G and U from pre [rows, 2 h].  G and U come
 // into LDS behind the last stages, 32 rows of a wavefront's part at a time, and are turned into dG and dU in their places; of
-// 256 x 256 tiles the rows from 64 on follow while the first ones are computed.  16384 rows, 8 experts, 2048 x 5632: 414 us alone,
-// 913 TFLOP/s: per 256 x 256 tile of 32 stages 512 KiB come in and go out behind the loop.
+// 256 x 256 tiles the rows from 64 on follow while the first ones are computed.  16384 rows, 8 experts, 2048 x 5632: 399 us alone,
+// 947 TFLOP/s: per 256 x 256 tile of 32 stages 512 KiB come in and go out behind the loop.
 template <int ACT, bool KTAIL, int BM>
 __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
     const uint16_t *__restrict__ A, const uint16_t *__restrict__ W, const uint16_t *__restrict__ pre, uint16_t *__restrict__ out,
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
 }
 
 // ---------------------------------------------------------------- backward: dxe
-// C [rows, N] bf16 = A W^T, A = [dG | dU].  16384 rows, 8 experts, N = 2048, K = 11264, 128 x 256 tiles: 860 us, 880 TFLOP/s (544 tiles of
+// C [rows, N] bf16 = A W^T, A = [dG | dU].  16384 rows, 8 experts, N = 2048, K = 11264, 128 x 256 tiles: 850 us alone, 889 TFLOP/s (544 tiles of
 // 256 x 256 are two rounds and a bit); the weight gradients beside it fill the last one.
 template <bool KTAIL, int BM>
 __global__ __launch_bounds__(256, 1) void rows_bf16_run_kernel(

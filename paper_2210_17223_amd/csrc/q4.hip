@@ -209,8 +209,8 @@ __device__ __forceinline__ float gated_by(int act, float g, float u)
 // as the instruction wants them; and of scales and zeros a lane loads one of four steps, which the quarters of the wavefront
 // then hand round.
 // Loads are waited for in the order of their issue: x of the next step goes out before the codes of the one behind it.
-// 2 rows, 8 experts, 4096 x 14336, group 128, the block's two products: 24 + 14 us, 5 TB/s of codes from the caches' side, 3.8 where
-// none are left there; 64 rows, group 64 with zeros, 130 + 70 us, 3.9 TB/s, the issue of vector instructions beside the loads.
+// 2 rows, 8 experts, 4096 x 14336, group 128, the block's two products: 25 + 14 us, 5 TB/s of codes from the caches' side, 3.8 where
+// none are left there; 64 rows, group 64 with zeros, 194 to 200 us a pass, 3.9 TB/s, the issue of vector instructions beside the loads.
 // KTAIL: K is not a multiple of 256.
 template <int XT, int G, bool ZEROS, int NT, int XR, bool KTAIL>
 __global__ __launch_bounds__(512) void q4_stream_kernel(Q4Args a)
@@ -481,8 +481,8 @@ __device__ __forceinline__ bool join(f32x4 (&total)[TN][TM], char *shared, int p
 // group's sums have accumulators of their own; behind the group they are scaled into the totals, four instructions for each tile
 // of 16 x 16 and group beside its G / 32 matrix instructions (and in bf16 four more for the zeros).  Each wavefront widens its own
 // columns' codes, seven instructions for eight of them, which feed BM / 32 matrix instructions: bound by the issue of vector
-// instructions, and with few tiles by the compute units that have none.  4096 x 4096, group 128: 64 rows 11 us, 160 rows 19 us,
-// 1000 rows 56 us (600 TFLOP/s); 8192 x 8192 from fp16, 6000 rows 1132 us (712 TFLOP/s).
+// instructions, and with few tiles by the compute units that have none.  4096 x 4096, group 128: 64 rows 12 us, 160 rows 20 us,
+// 1000 rows 63 us (530 TFLOP/s); 8192 x 8192, 300 rows 91 us, from fp16 6000 rows 1047 us (770 TFLOP/s).
 template <int XT, int G, bool ZEROS, int BM, int BN, int KS>
 __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_tile_kernel(Q4Args a)
 {
@@ -692,8 +692,9 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
 // fragment reads are free of bank conflicts (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).
 // Codes, scales and zeros of the next stage are on their way in registers, requested behind x, so that the wait for them covers
 // it. Bound by issue: beside 64 matrix instructions of a wavefront and stage stand 300 vector instructions (widening, scaling),
-// and a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, the two products, tiles of 64 rows: 380
-// + 215 us, 720 and 640 TFLOP/s; of 128 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x
+// and a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, tiles of 64 rows: 511 to
+// 531 us a pass by the card, 810 to 780 TFLOP/s (356 + 197 with an event pair around each product).  In a kernel trace, where
+// all take a tenth longer, the two products on those tiles 380 + 215, of 128 rows 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x
 // 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector instructions placed by hand between the matrix
 // instructions 375 + 225; weights scaled before the product (no sums per group, rounded to fp16) on four wavefronts and 128 x
 // 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its loads and numbers with nobody to step in.
