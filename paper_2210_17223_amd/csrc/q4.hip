@@ -2,9 +2,9 @@
 // gated feed-forward block on them.
 //
 // The codes go from memory into registers and from there into the matrix instruction: eight codes of a lane become eight
-// 16-bit numbers in place, by masks and an exponent (the conversion of narrow integers by their place in a number's digits that Kim,
-// Henry, Fahim and Hassan Awadalla give in "Who Says Elephants Can't Run", 2022): in bf16 2^-16 (16 + q), in fp16 1024 + q.  Products and sums over a group
-// are then exact but for fp32's roundings, and a group's sum is scaled in fp32:
+// 16-bit numbers in place, by masks and an exponent (the conversion of narrow integers by their place in a number's digits that
+// Kim, Henry, Fahim and Hassan Awadalla give in "Who Says Elephants Can't Run", 2022): in bf16 2^-16 (16 + q), in fp16
+// 1024 + q.  Products and sums over a group are then exact but for fp32's roundings, and a group's sum is scaled in fp32:
 //   bf16   sum (q - z) x = sum (16 + q) x - (16 + z) sum x, with sum x from one more matrix instruction against ones
 //          (shared by all of a wavefront's columns).  16 is the least that an exponent can add: the code is then the first
 //          four of the seven digits behind the point.  Against 128 + q, whose code is the last four and needs no shift for one
@@ -678,7 +678,8 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
             u32x4 o;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const f16x2 h = {static_cast<_Float16>(__uint_as_float(v[c] << 16) * by), static_cast<_Float16>(__uint_as_float(v[c] & 0xffff0000u) * by)};
+                const float lo = __uint_as_float(v[c] << 16) * by, hi = __uint_as_float(v[c] & 0xffff0000u) * by;
+                const f16x2 h = {static_cast<_Float16>(lo), static_cast<_Float16>(hi)};
                 o[c] = __builtin_bit_cast(uint32_t, h);
             }
             *reinterpret_cast<u32x4 *>(out + static_cast<size_t>(row) * K + k) = o;
@@ -692,12 +693,13 @@ __global__ __launch_bounds__(256) void q4_rows_kernel(const uint16_t *__restrict
 // fragment reads are free of bank conflicts (with the pieces in their own order a third of the LDS's cycles, 1 % of the time).
 // Codes, scales and zeros of the next stage are on their way in registers, requested behind x, so that the wait for them covers
 // it. Bound by issue: beside 64 matrix instructions of a wavefront and stage stand 300 vector instructions (widening, scaling),
-// and a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, tiles of 64 rows: 511 to
-// 531 us a pass by the card, 810 to 780 TFLOP/s (356 + 197 with an event pair around each product).  In a kernel trace, where
-// all take a tenth longer, the two products on those tiles 380 + 215, of 128 rows 383 + 232, the matrix cores busy for 39 %.  Tried against the latter: tiles of 128 x
-// 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector instructions placed by hand between the matrix
-// instructions 375 + 225; weights scaled before the product (no sums per group, rounded to fp16) on four wavefronts and 128 x
-// 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its loads and numbers with nobody to step in.
+// and a matrix instruction hides three.  4096 rows, 8 experts, 2048 x 8192, group 128, tiles of 64 rows: 511 to 531 us a
+// pass by the card, 810 to 780 TFLOP/s (356 + 197 with an event pair around each product).  In a kernel trace, where all take a
+// tenth longer, the two products on those tiles 380 + 215, of 128 rows 383 + 232, the matrix cores busy for 39 %.  Tried
+// against the latter: tiles of 128 x 256 on eight wavefronts, one block a compute unit, 432 + 279 us; the vector instructions
+// placed by hand between the matrix instructions 375 + 225; weights scaled before the product (no sums per group, rounded to
+// fp16) on four wavefronts and 128 x 256 tiles 471 + 286, 256 x 256 480 + 252: one wavefront per SIMD waits for its loads and
+// numbers with nobody to step in.
 template <int G, bool ZEROS, int BM, int BN, int KS>
 __global__ __launch_bounds__(2 * BN * KS, KS == 4 && BN == 128 ? 4 : 2) void q4_ready_kernel(Q4Args a)
 {
