@@ -905,11 +905,13 @@ __global__ __launch_bounds__(256, 1) void wgrad_w4_kernel(
 #pragma unroll
                 for (int i = 0; i < TN; ++i)
                     *reinterpret_cast<f32x4 *>(patch + fr * 512 + (((i * 4 + oct) ^ fr) << 4)) = acc[i][j];
+                lds_handover();
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     const int row = 2 * q + (lane >> 5);
                     line[j & 1][q] = *reinterpret_cast<const u32x4 *>(patch + row * 512 + (((lane & 31) ^ row) << 4));
                 }
+                lds_handover();
                 MOE_SB();
             };
             auto leave = [&](auto jc) {
@@ -939,11 +941,13 @@ __global__ __launch_bounds__(256, 1) void wgrad_w4_kernel(
                     const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                     store_bf16x4(reinterpret_cast<uint16_t *>(patch + fr * 256 + (((i * 2 + (oct >> 1)) ^ fr) << 4) + (oct & 1) * 8), v);
                 }
+                lds_handover();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int row = 4 * q + (lane >> 4);
                     line[j & 1][q] = *reinterpret_cast<const u32x4 *>(patch + row * 256 + (((lane & 15) ^ row) << 4));
                 }
+                lds_handover();
                 MOE_SB();
             };
             auto leave = [&](auto jc) {

@@ -76,6 +76,7 @@ __device__ __forceinline__ void leave_gated(const W4Place<BM> &place, uint16_t *
     const int piece = place.lane % PIECES, lane_row = place.lane / PIECES, col = col0 + piece % 8 * 8;
     const int first = col < h ? (lane_row * pitch + col + (piece >= 8 ? pair_at : 0)) * 2 : 0x7ff00000;
     const int step = col < h ? ROWS * pitch * 2 : 0;
+    lds_handover();
     MOE_SB();
 #pragma unroll
     for (int it = 0; it < R / ROWS; ++it) {
@@ -84,6 +85,7 @@ __device__ __forceinline__ void leave_gated(const W4Place<BM> &place, uint16_t *
         __builtin_amdgcn_raw_buffer_store_b128(q, rs, first + it * step, 0, 0);
         if (it % 4 == 3) MOE_SB();
     }
+    lds_handover();
 }
 
 // acc[2 p] and acc[2 p + 1] of a lane: gate and value of the same four columns

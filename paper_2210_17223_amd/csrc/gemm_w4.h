@@ -145,6 +145,15 @@ __device__ __forceinline__ uint32_t lds_address(const void *p)
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
 }
 
+// What a wavefront's lanes have written to its own LDS is read by other lanes behind this, and what they have read is written
+// over behind it.  (It takes a wavefront's accesses in order: nothing is waited for, but nothing is moved across either.)
+__device__ __forceinline__ void lds_handover()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <int... I, typename F>
 __device__ __forceinline__ void static_for_each(std::integer_sequence<int, I...>, F f)
 {

@@ -58,6 +58,7 @@ struct W4Place {                       // where a wavefront stands in its tile
             out + static_cast<size_t>(row0) * N, 0, static_cast<unsigned>(max(item.row1 - row0, 0)) * N * 2u, 0x00020000);
         const int col = col0 + lane % 16 * 8;
         const int first = col < N ? (lane / 16 * N + col) * 2 : 0x7ff00000, step = col < N ? N * 8 : 0;
+        lds_handover();
         MOE_SB();
 #pragma unroll
         for (int it = 0; it < R / 4; ++it) {
@@ -66,6 +67,7 @@ struct W4Place {                       // where a wavefront stands in its tile
             __builtin_amdgcn_raw_buffer_store_b128(q, rs, first + it * step, 0, 0);
             if (it % 4 == 3) MOE_SB();
         }
+        lds_handover();
     }
 };
 

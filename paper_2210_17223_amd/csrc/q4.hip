@@ -166,15 +166,6 @@ struct Run {                               // BYTES consecutive bytes, from an a
     __device__ __forceinline__ uint32_t byte(int i) const { return (w[i / 4] >> (i % 4 * 8)) & 0xffu; }
 };
 
-// What a wavefront's lanes have written to its own LDS is read by other lanes behind this, and what they have read is written
-// over behind it.  (It takes a wavefront's accesses in order: nothing is waited for, but nothing is moved across either.)
-__device__ __forceinline__ void lds_handover()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 struct Q4Args {
     const uint16_t *x;
     const int32_t *offsets;

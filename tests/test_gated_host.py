@@ -198,3 +198,18 @@ def test_few_rows_of_many_experts_may_be_one_experts():
         return moe.moe_gated_q4_workspace_bytes(s) > hidden
     assert not any(ready(R, E) for R, E in ((1, 1), (16, 1), (80, 8), (96, 10), (96, 64), (16, 64)))
     assert all(ready(R, E) for R, E in ((17, 1), (81, 8), (97, 10), (97, 64), (640, 64)))
+
+
+def test_tiles_that_leave_through_lds_have_a_barrier_on_both_sides():
+    """The epilogues that write a wavefront's accumulators to its own part of LDS and read whole lines of other lanes' values back."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(moe.lib_path()), "csrc")
+    for name, start, count in (("gated.hip", "void leave_gated(", 1), ("gemm_w4_run.h", "void leave(", 1), ("bwd.hip", "auto through = ", 2)):
+        with open(os.path.join(csrc, name)) as f:
+            parts = f.read().split(start)[1:]
+        assert len(parts) == count
+        for body in parts:
+            read = body.index("*reinterpret_cast<const u32x4 *>(")
+            end = body.index("\n}\n") if name == "gated.hip" else body.index("};")
+            assert len(re.findall(r"lds_handover\(\);", body[:read])) == 1 and len(re.findall(r"lds_handover\(\);", body[read:end])) == 1, name
