@@ -211,5 +211,5 @@ def test_tiles_that_leave_through_lds_have_a_barrier_on_both_sides():
         assert len(parts) == count
         for body in parts:
             read = body.index("*reinterpret_cast<const u32x4 *>(")
-            end = body.index("\n}\n") if name == "gated.hip" else body.index("};")
+            end = body.index("\n}\n" if name == "gated.hip" else "};", read)
             assert len(re.findall(r"lds_handover\(\);", body[:read])) == 1 and len(re.findall(r"lds_handover\(\);", body[read:end])) == 1, name
