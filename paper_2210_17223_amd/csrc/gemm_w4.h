@@ -76,14 +76,20 @@ constexpr int kRunUnits = 256, kRunStages = 128;
 // close, registers moved on the way round a loop among it, tests/test_matrix_hazards.py reads
 // back from the built library.  (Two wait states at the top of every stage: gpt2s-sized layers, 8192
 // rows of 768 x 3072, 61.5 -> 61.9 us in the first GEMM.)
-// ZERO: the accumulator starts at zero.
-template <bool F16, bool WAIT, bool ZERO = false>
+// ZERO: the accumulator starts at zero.  OPS: the operands' type; of 8-bit ones (kI8) an instruction takes twice the depth in the
+// same bytes and cycles, and the accumulator's four registers hold 32-bit whole numbers.
+enum { kB16Operands = 0, kF16Operands = 1, kI8Operands = 2 };
+template <int OPS, bool WAIT, bool ZERO = false>
 __device__ __forceinline__ void mfma_16x16x32_agpr(f32x4 &acc, const u32x4 &a, const u32x4 &b)
 {
-    static_assert(!(F16 && WAIT), "no caller converts to fp16");
-    if constexpr (F16 && ZERO)
+    static_assert(OPS == kB16Operands || !WAIT, "no caller converts to fp16 or to 8 bits");
+    if constexpr (OPS == kI8Operands && ZERO)
+        asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));
+    else if constexpr (OPS == kI8Operands)
+        asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+    else if constexpr (OPS == kF16Operands && ZERO)
         asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));
-    else if constexpr (F16)
+    else if constexpr (OPS == kF16Operands)
         asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
     else if constexpr (ZERO && WAIT)
         asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));

@@ -77,11 +77,13 @@ struct W4Place {                       // where a wavefront stands in its tile
 // ABL: see grouped_gemm_w4_kernel.  epilogue(acc, prepare(item, wn, oct), item, place, landed) takes the finished tile out of
 // the accumulators, without a branch, acc[i][j][c] = column wn * 128 + i * 16 + oct * 4 + c, row wm * BM / 2 + j * 16 + fr, and calls landed() once, in
 // front of its first store: what the next tile waits for early has to be there before stores stand in front of it.
-template <bool F16, bool KTAIL, int BM, int ABL, typename Prepare, typename Epilogue>
+// items: the list, or what finds entry b by items[b].  F16 may be kI8Operands (K is then half the depth); PAIR: the tile's columns
+// are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).
+template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, typename Items, typename Prepare, typename Epilogue>
 __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uint16_t *__restrict__ W,
-                                       const WorkItem *__restrict__ items, const int32_t *__restrict__ nitems, int entries, int share,
+                                       const Items &items, const int32_t *__restrict__ nitems, int entries, int share,
                                        int N, int K, const int32_t *__restrict__ row_src, int row_div, int a_rows,
-                                       Prepare prepare, Epilogue epilogue)
+                                       Prepare prepare, Epilogue epilogue, int pair_h = 0)
 {
     constexpr int TM = BM / 32, TN = 8, BK = 64;
     constexpr bool RING5 = BM == 256;
@@ -122,8 +124,8 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(at), 0, n * static_cast<unsigned>(K) * 2u, 0x00020000);
     };
     auto weights_of = [&](const WorkItem &t) {
-        const uint16_t *at = t.expert < 0 ? W : W + (static_cast<size_t>(t.expert) * N + t.n0) * K;
-        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(min(N - t.n0, 256));     // (a tile's: 256 K values fit)
+        const uint16_t *at = t.expert < 0 ? W : W + (static_cast<size_t>(t.expert) * N + (PAIR ? t.n0 / 2 : t.n0)) * K;
+        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(PAIR ? N - t.n0 / 2 : min(N - t.n0, 256));     // (a tile's: 256 K values fit)
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(at), 0, n * static_cast<unsigned>(K) * 2u, 0x00020000);
     };
     // load q of this wavefront's TM (TN) of a unit: rows wave * AR (64) + 8 q .. + 7, eight 16-byte pieces
@@ -133,7 +135,8 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
 #pragma unroll
     for (int q = 0; q < TN; ++q) {
         const int r = wave * 64 + q * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
-        w_src[q] = (r * K + piece * 8) * 2;
+        // (of a pair, columns past pair_h are of its other half or past it: not stored)
+        w_src[q] = ((PAIR ? r / 32 * 16 + r % 16 + (r / 16 % 2) * pair_h : r) * K + piece * 8) * 2;
         if (q < 2) first_col[q] = piece * 8;
     }
     // lane l's: row l of the wavefront's AR of a tile, in A or (packed rows) in the tile, -1 past its last one; from

@@ -19,6 +19,8 @@
 // 16384 3.1 / 0.7 / 6.1 (3.3 / 1.2 / 5.3).  (At 5120 and 12288 three of eight and a quarter of the threads have no columns, too.)
 #include "common.h"
 #include "moe_norm.h"
+#include "moe_q8.h"
+#include "q8.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -148,6 +150,8 @@ struct NormArgs {
     const float *w, *b, *gate, *w_next, *b_next;
     void *r_out, *next, *dx, *dz;
     float *dgate, *part;                           // part [runs][slots][d]
+    uint32_t *q;                                   // next in 8 bits, and its scales
+    float *q_scale;
     int T, d, gate_tokens, per_run;
     bool layer, next_f32;
     float eps, scale;
@@ -155,8 +159,8 @@ struct NormArgs {
 
 constexpr int row_vec(int res, int z) { return res == kB16 && z != kF32 ? 8 : 4; }
 
-// Forward.  Columns of thread t: (v TPR + t) VEC .. + VEC - 1.
-template <int RES, int Z, int TPR, int EPT>
+// Forward.  Columns of thread t: (v TPR + t) VEC .. + VEC - 1.  Q8: next leaves in 8 bits too, or only so.
+template <int RES, int Z, int TPR, int EPT, bool Q8 = false>
 __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(NormArgs a)
 {
     constexpr bool AFTER = Z >= 0;
@@ -278,7 +282,36 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
         for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[v][e] = __builtin_fmaf(x[v][e], wn[v][e], bn[v][e]);
-            if (in[v]) store_row<VEC>(next, a.next_f32, col[v], x[v]);
+            if (in[v] && (!Q8 || a.next != nullptr)) store_row<VEC>(next, a.next_f32, col[v], x[v]);
+        }
+        if constexpr (Q8) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) most = max(most, in[v] ? magnitude(x[v][e]) : 0u);
+            most = wave_most(most);
+            if constexpr (TPR > kWave) {
+                __shared__ uint32_t row_most[2][TPR / kWave];
+                uint32_t (&place)[TPR / kWave] = row_most[i & 1];      // (two in turn, as of the sums)
+                if (lane_id() == 0) place[threadIdx.x / kWave] = most;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < TPR / kWave; ++w) most = max(most, place[w]);
+            }
+            const Q8Row row(most);
+            uint32_t *q = a.q + static_cast<size_t>(i) * (d / 4);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                int c[VEC];
+                row.codes(x[v], c);
+                if (!in[v]) continue;
+                if constexpr (VEC == 8)
+                    *reinterpret_cast<u32x2 *>(q + col[v] / 4) = (u32x2){pack_codes(c), pack_codes(c + 4)};
+                else
+                    q[col[v] / 4] = pack_codes(c);
+            }
+            if (t == 0) a.q_scale[i] = row.scale;
         }
     }
 }
@@ -640,8 +673,12 @@ moe_status launch_norm_forward(const moe_norm_shape &n, NormArgs a, bool after, 
             constexpr int TPR = decltype(tpr)::value;
             a.per_run = parts_of(n.T, std::min(n.T, most));
             const int runs = parts_of(n.T, a.per_run);
-            hipLaunchKernelGGL((norm_forward_kernel<decltype(res)::value, decltype(z)::value, TPR, decltype(ept)::value>),
-                               dim3(TPR == kWave ? ceil_div(runs, 4) : runs), dim3(TPR == kWave ? 256 : TPR), 0, st, a);
+            auto run = [&](auto q8) {
+                hipLaunchKernelGGL((norm_forward_kernel<decltype(res)::value, decltype(z)::value, TPR, decltype(ept)::value, decltype(q8)::value>),
+                                   dim3(TPR == kWave ? ceil_div(runs, 4) : runs), dim3(TPR == kWave ? 256 : TPR), 0, st, a);
+            };
+            if (a.q != nullptr) run(std::true_type{});
+            else run(std::false_type{});
         };
         using std::integral_constant;
         if (n.d <= 512) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 256 * 16);
@@ -785,6 +822,70 @@ moe_status moe_norm_after(const moe_norm_shape *n, const void *x, const void *z,
     a.w_next = w_next;
     a.b_next = b_next;
     a.next = next;
+    return launch_norm_forward(*n, a, true, static_cast<hipStream_t>(stream));
+}
+
+static moe_status check_norm_q8(const moe_norm_shape *n)
+{
+    const moe_status rc = check_norm(n);
+    if (rc != MOE_OK) return rc;
+    if (n->d % 16 != 0) {
+        set_error("rows in 8 bits: d = %d must be a multiple of 16", n->d);
+        return MOE_EUNSUPPORTED;
+    }
+    return MOE_OK;
+}
+
+moe_status moe_norm_before_q8(const moe_norm_shape *n, const void *x, const float *w_next, const float *b_next, void *next,
+                              void *q, float *scale, void *stream)
+{
+    const moe_status rc = check_norm_q8(n);
+    if (rc != MOE_OK) return rc;
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_OPTIONAL_PTR(b_next);
+    MOE_OPTIONAL_PTR(next);
+    MOE_REQUIRE_PTR(q);
+    MOE_REQUIRE_PTR(scale);
+    NormArgs a = norm_args(*n);
+    a.x = x;
+    a.w_next = w_next;
+    a.b_next = b_next;
+    a.next = next;
+    a.q = static_cast<uint32_t *>(q);
+    a.q_scale = scale;
+    return launch_norm_forward(*n, a, false, static_cast<hipStream_t>(stream));
+}
+
+moe_status moe_norm_after_q8(const moe_norm_shape *n, const void *x, const void *z, const float *w, const float *b,
+                             const float *gate, void *r, const float *w_next, const float *b_next, void *next, void *q,
+                             float *scale, void *stream)
+{
+    const moe_status rc = check_norm_q8(n);
+    if (rc != MOE_OK) return rc;
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(z);
+    MOE_REQUIRE_PTR(w);
+    MOE_OPTIONAL_PTR(b);
+    MOE_OPTIONAL_PTR(gate);
+    MOE_REQUIRE_PTR(r);
+    MOE_REQUIRE_PTR(w_next);
+    MOE_OPTIONAL_PTR(b_next);
+    MOE_OPTIONAL_PTR(next);
+    MOE_REQUIRE_PTR(q);
+    MOE_REQUIRE_PTR(scale);
+    NormArgs a = norm_args(*n);
+    a.x = x;
+    a.z = z;
+    a.w = w;
+    a.b = b;
+    a.gate = gate;
+    a.r_out = r;
+    a.w_next = w_next;
+    a.b_next = b_next;
+    a.next = next;
+    a.q = static_cast<uint32_t *>(q);
+    a.q_scale = scale;
     return launch_norm_forward(*n, a, true, static_cast<hipStream_t>(stream));
 }
 

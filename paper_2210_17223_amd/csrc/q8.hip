@@ -1,0 +1,1016 @@
+// Rows and weights held in 8 bits (include/moe_q8.h): rows to codes and back, one linear map, the gated feed-forward block,
+// and the dispatch of such rows.
+//
+// Products are of 8-bit whole numbers on the matrix cores, with 32-bit sums: exact, so that no kernel, tile or split of the depth
+// changes a sum.  (The 8-bit floating matrix instructions, of the same rate, drop what lies some 2^13 under the largest product
+// of an instruction's group: 1.4e-5 of a sum of normally distributed values.)  An instruction takes twice the depth of a 16-bit one
+// in the same bytes and cycles, so the loops are the expert FFN's with K in pairs of codes, "16-bit values", throughout.
+// The block's hidden rows are rounded to fp16 by the first product's epilogue and held in 8 bits from a pass of their own, since
+// a row's scale needs all of the row: 2 + 2 + 1 bytes a value beside the products.
+#include "activation.h"
+#include "moe_gated.h"
+#include "moe_q8.h"
+#include "gated.h"
+#include "q8.h"
+
+#include <algorithm>
+#include <type_traits>
+
+#include <hip/hip_ext.h>
+
+namespace moe {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+#include "gemm_w4.h"
+#include "gemm_w4_run.h"
+
+enum { kF32 = 0, kB16 = 1, kF16 = 2 };       // element types as in moe_q8_shape
+constexpr int kMaxDepth = 65536;             // values of a row
+
+// one of the two fp16 (bf16) values of a dword.  (By value: a bit cast of a vector's element casts its first one.)
+__device__ __forceinline__ float f16_of(uint32_t w, int i) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[i]); }
+__device__ __forceinline__ float b16_of(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
+
+// ---------------------------------------------------------------- rows to codes and back
+// 16 values of a row as they lie in memory
+struct Sixteen {
+    float v[16];
+    __device__ __forceinline__ void load(const void *row, int type, int col)
+    {
+        if (type == kF32) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 p = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(row) + col + 4 * q);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[4 * q + c] = p[c];
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const u32x4 p = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(row) + col + 8 * q);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    v[8 * q + 2 * c] = type == kB16 ? b16_of(p[c], 0) : f16_of(p[c], 0);
+                    v[8 * q + 2 * c + 1] = type == kB16 ? b16_of(p[c], 1) : f16_of(p[c], 1);
+                }
+            }
+        }
+    }
+};
+
+// A row is TPR threads' (a wavefront's, or a block's), NV pieces of 16 values each, and stays in registers between the search for
+// its largest magnitude and its codes.  rows_end: NULL, or where the number of rows stands, at most R.
+template <int TYPE, int TPR, int NV>
+__global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void q8_rows_kernel(const void *__restrict__ x, uint32_t *__restrict__ q,
+                                                                           float *__restrict__ scale, int64_t R, int K,
+                                                                           const int32_t *__restrict__ rows_end)
+{
+    constexpr int PER = TPR == kWave ? 4 : 1;          // rows of a block at a time
+    const int t = threadIdx.x % TPR;
+    if (rows_end != nullptr) R = min(R, static_cast<int64_t>(*rows_end));
+    __shared__ uint32_t row_most[2][TPR / kWave];
+    int turn = 0;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * PER + threadIdx.x / TPR; i < R; i += static_cast<int64_t>(gridDim.x) * PER) {
+        const char *row = static_cast<const char *>(x) + i * K * (TYPE == kF32 ? 4 : 2);
+        Sixteen p[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) p[v].load(row, TYPE, min((v * TPR + t) * 16, K - 16));
+        uint32_t most = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = max(most, magnitude(p[v].v[e]));      // (past the row's end: its last piece)
+        most = wave_most(most);
+        if constexpr (TPR > kWave) {
+            if (lane_id() == 0) row_most[turn][threadIdx.x / kWave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < TPR / kWave; ++w) most = max(most, row_most[turn][w]);
+            turn ^= 1;
+        }
+        const Q8Row held(most);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            int c[16];
+            held.codes(p[v].v, c);
+            const int col = (v * TPR + t) * 16;
+            if (col < K)
+                *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(q) + i * K + col) =
+                    (u32x4){pack_codes(c), pack_codes(c + 4), pack_codes(c + 8), pack_codes(c + 12)};
+        }
+        if (t == 0) scale[i] = held.scale;
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_16(int type, float lo, float hi)
+{
+    if (type == kF16) {
+        f16x2 h;
+        h[0] = static_cast<_Float16>(lo);
+        h[1] = static_cast<_Float16>(hi);
+        return __builtin_bit_cast(uint32_t, h);
+    }
+    bf16x2 b;
+    b[0] = static_cast<__bf16>(lo);
+    b[1] = static_cast<__bf16>(hi);
+    return __builtin_bit_cast(uint32_t, b);
+}
+
+// A block takes `rows` rows' pieces of 16 codes.
+template <int TYPE>
+__global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restrict__ q, const float *__restrict__ scale, void *__restrict__ x,
+                                                        int64_t R, int K, int rows)
+{
+    const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
+    for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * rows; r0 < R; r0 += step) {
+        const int per_row = K / 16, pieces = static_cast<int>(min(R - r0, static_cast<int64_t>(rows))) * per_row;
+        for (int p = threadIdx.x; p < pieces; p += 256) {
+            const int64_t at = r0 * per_row + p;
+            const u32x4 c = *(reinterpret_cast<const u32x4 *>(q) + at);
+            const float s = scale[r0 + p / per_row];
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(static_cast<int8_t>(c[i / 4] >> (i % 4 * 8))) * s;
+            if constexpr (TYPE == kF32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(reinterpret_cast<f32x4 *>(x) + at * 4 + i) = (f32x4){v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x4 o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = pack_16(TYPE, v[8 * i + 2 * e], v[8 * i + 2 * e + 1]);
+                    *(reinterpret_cast<u32x4 *>(x) + at * 2 + i) = o;
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- products: what they share
+// K: pairs of codes.  Tiles are found from the experts' offsets.
+struct Q8Args {
+    const uint16_t *x, *w;
+    const float *xs, *ws, *bias;
+    const void *r;
+    void *y;
+    const int32_t *offsets, *row_src;      // row_src: the first product takes row row_src[i] / row_div, of a_rows
+    int row_div, a_rows;
+    int E, N, K;                           // of a pair of projections N = 2 h
+    int h;                                 // else 0
+    int act, res, type;
+    int tiles, entries, share;
+};
+
+// acc columns of a tile: BN packed ones of a pair of projections, sixteen of the first and the same sixteen of the second in turn
+__host__ __device__ inline int tile_columns(const Q8Args &a) { return a.h != 0 ? gated_packed_columns(a.h) : a.N; }
+
+// The tile of block entry b: a panel of kPanel tiles' rows of an expert column by column, then the next; an eighth of all tiles for
+// each XCD.  A wavefront holds the experts' row tiles and their running sum, a lane each.
+constexpr int kPanel = 8;
+template <int BM, int BN>
+struct Tiles {
+    int first, end, row_tiles, sum, per_xcd, total, tiles;
+    __device__ __forceinline__ Tiles(const int32_t *__restrict__ offsets, int E, int column_tiles) : tiles(column_tiles)
+    {
+        const int lane = lane_id(), e = min(lane, E - 1);
+        first = offsets[e];
+        end = lane < E ? offsets[e + 1] : first;
+        row_tiles = end > first ? (end - first + BM - 1) / BM : 0;
+        sum = row_tiles * tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        total = __builtin_amdgcn_readlane(sum, kWave - 1);
+        per_xcd = (total + 7) / 8;
+    }
+    __device__ __forceinline__ WorkItem operator[](int b) const
+    {
+        const int slot = b / 8, index = b % 8 * per_xcd + slot;
+        if (slot >= per_xcd || index >= total) return WorkItem{-1, 0, 0, 0};
+        const int e = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
+        const int mt = __builtin_amdgcn_readlane(row_tiles, e);
+        const int within = index - (__builtin_amdgcn_readlane(sum, e) - mt * tiles);
+        const int panel = within / (kPanel * tiles), rest = within - panel * (kPanel * tiles), high = min(kPanel, mt - panel * kPanel);
+        const int column = rest / high, row0 = __builtin_amdgcn_readlane(first, e) + (panel * kPanel + rest - column * high) * BM;
+        return WorkItem{e, row0, min(row0 + BM, __builtin_amdgcn_readlane(end, e)), column * BN};
+    }
+};
+inline int64_t tile_entries(int64_t rows, int E, int bm, int tiles)
+{
+    return static_cast<int64_t>(align_up((static_cast<size_t>(rows) / bm + std::min<int64_t>(rows, E)) * tiles, 8));
+}
+
+// All activations but the erf form of the GeLU as factor * v / (1 + 2^-(v (a + b v^2))): silu; its tanh form; relu, whose a is so large
+// that the quotient is 1 or 0 from |v| = 1e-36 on; and identity, 2 v / 2.  An epilogue that holds accumulators takes no branch, and a
+// kernel for each activation is five times the code.  (v^2 is bounded so that 0 v^2 is 0.)
+struct ActForm {
+    float a, b, factor;
+    __device__ __forceinline__ explicit ActForm(int act)
+    {
+        a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : act == MOE_ACT_RELU ? 1e38f : 0.0f;
+        b = act == MOE_ACT_GELU_TANH ? 0.10294324f : 0.0f;
+        factor = act == MOE_ACT_IDENTITY ? 2.0f : 1.0f;
+    }
+    __device__ __forceinline__ float operator()(float v) const
+    {
+        const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
+        const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
+        return v * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
+    }
+};
+template <bool ERF>
+__device__ __forceinline__ float activate(const ActForm &form, float v)
+{
+    if constexpr (ERF) return gelu_erf_fast(v);
+    else return form(v);
+}
+__device__ __forceinline__ float activate_by(int act, float v)
+{
+    switch (act) {
+    case MOE_ACT_GELU_ERF: return gate_value<MOE_ACT_GELU_ERF>(v);
+    case MOE_ACT_GELU_TANH: return gate_value<MOE_ACT_GELU_TANH>(v);
+    case MOE_ACT_RELU: return gate_value<MOE_ACT_RELU>(v);
+    case MOE_ACT_SILU: return gate_value<MOE_ACT_SILU>(v);
+    default: return v;
+    }
+}
+__device__ __forceinline__ float sum_of(float bits) { return static_cast<float>(__builtin_bit_cast(int, bits)); }
+
+__device__ __forceinline__ float load_value(const void *p, int type, size_t at)
+{
+    if (type == kF32) return static_cast<const float *>(p)[at];
+    const uint16_t h = static_cast<const uint16_t *>(p)[at];
+    return type == kB16 ? bf16_to_f32(h) : static_cast<float>(__builtin_bit_cast(_Float16, h));
+}
+// y of columns n .. n + 3 of a row; v: sums times both scales
+__device__ __forceinline__ void finish(const Q8Args &a, int expert, size_t row, int n, float (&v)[4])
+{
+    const size_t at = row * a.N + n;
+    const float *bias = a.bias != nullptr ? a.bias + static_cast<size_t>(expert) * a.N + n : nullptr;
+    if (a.N % 4 == 0) {                    // (whole groups, and their addresses are multiples of the groups' size)
+        if (bias != nullptr) {
+            const f32x4 b = *reinterpret_cast<const f32x4 *>(bias);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += b[c];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = activate_by(a.act, v[c]);
+        if (a.r != nullptr) {
+            if (a.res == kF32) {
+                const f32x4 r = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.r) + at);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] += r[c];
+            } else {
+                const u32x2 r = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.r) + at);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] += a.res == kF16 ? f16_of(r[c / 2], c % 2) : b16_of(r[c / 2], c % 2);
+            }
+        }
+        if (a.type == kF32)
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + at) = (f32x4){v[0], v[1], v[2], v[3]};
+        else
+            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + at) = (u32x2){pack_16(a.type, v[0], v[1]), pack_16(a.type, v[2], v[3])};
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        if (n + c >= a.N) return;
+        float u = activate_by(a.act, v[c] + (bias != nullptr ? bias[c] : 0.0f));
+        if (a.r != nullptr) u += load_value(a.r, a.res, at + c);
+        if (a.type == kF32) static_cast<float *>(a.y)[at + c] = u;
+        else static_cast<uint16_t *>(a.y)[at + c] = static_cast<uint16_t>(pack_16(a.type, u, 0.0f));
+    }
+}
+__device__ __forceinline__ void store_hidden(const Q8Args &a, size_t row, int n, const float (&v)[4])
+{
+    f16x4 o;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = static_cast<_Float16>(v[c]);
+    *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(a.y) + row * a.h + n) = o;
+}
+__device__ __forceinline__ float row_scale(const Q8Args &a, int row)
+{
+    return a.xs[a.row_src != nullptr ? a.row_src[row] / a.row_div : row];
+}
+// scales of columns n .. n + 3, of the last column past it
+__device__ __forceinline__ void column_scales(const float *__restrict__ p, int n, int N, float (&s)[4])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[c] = p[min(n + c, N - 1)];
+}
+
+// ---------------------------------------------------------------- few rows per expert
+// Four wavefronts share out the depth of a tile of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes; each
+// takes its stages through LDS of its own, PD of them on their way, so nothing is waited for but its own loads; the whole
+// numbers are added up through LDS at the end.
+template <bool PAIR, int RT, int PD>
+__global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
+{
+    constexpr int NT = PAIR ? 2 : 1, WAVES = 4, STAGE = (NT + RT) * 2048, LOADS = (NT + RT) * 2;
+    const Tiles<16 * RT, 16 * NT> tiles(a.offsets, a.E, a.tiles);
+    const WorkItem item = tiles[blockIdx.x];
+    if (item.expert < 0) return;
+    extern __shared__ __attribute__((aligned(16))) char q8_lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, oct = lane >> 4;
+    char *const mine = q8_lds + wave * (STAGE * PD);
+    const uint32_t dest = lds_address(mine);
+    const int rows = item.row1 - item.row0, n0 = item.n0 / NT, width = PAIR ? a.h : a.N;
+    const unsigned pitch = static_cast<unsigned>(a.K) * 2u;
+    const uint16_t *w0 = a.w + (static_cast<size_t>(item.expert) * a.N + n0) * a.K;
+    __amdgpu_buffer_rsrc_t rsw[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        rsw[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(w0 + static_cast<size_t>(t) * a.h * a.K), 0,
+                                                   static_cast<unsigned>(min(width - n0, 16)) * pitch, 0x00020000);
+    const bool gather = PAIR && a.row_src != nullptr;
+    const __amdgpu_buffer_rsrc_t rsx = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(gather ? a.x : a.x + static_cast<size_t>(item.row0) * a.K), 0,
+        static_cast<unsigned>(gather ? a.a_rows : rows) * pitch, 0x00020000);
+    // a load: eight rows of 128 bytes; lane l lands at row l / 8, place l % 8, where piece place ^ (row / 2 % 8) belongs
+    int wsrc[2], xsrc[2 * RT], piece[2];
+#pragma unroll
+    for (int q = 0; q < 2 * RT; ++q) {
+        const int r = q * 8 + (lane >> 3);
+        if (q < 2) {
+            piece[q] = (lane & 7) ^ ((r >> 1) & 7);
+            wsrc[q] = static_cast<int>(r * pitch) + piece[q] * 16;
+        }
+        const int from = gather ? a.row_src[min(item.row0 + r, item.row1 - 1)] / a.row_div : r;
+        xsrc[q] = r < rows ? static_cast<int>(from * pitch) + piece[q & 1] * 16 : 0x7ffffff0;
+    }
+    const int KT = (a.K + 63) / 64, per = (KT + WAVES - 1) / WAVES;
+    const int s0 = min(wave * per, KT), s1 = min(s0 + per, KT);
+    // (a piece past the row's end: an offset past every resource reads as zeros)
+    auto load = [&](int s, int place) {
+        const uint32_t at = dest + place * STAGE;
+        const int k = s * 128;
+        const bool past0 = s >= s1 || k + piece[0] * 16 >= static_cast<int>(pitch), past1 = s >= s1 || k + piece[1] * 16 >= static_cast<int>(pitch);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            load_to_lds(rsw[t], past0 ? 0x7ffffff0 : wsrc[0], at + t * 2048, k);
+            load_to_lds(rsw[t], past1 ? 0x7ffffff0 : wsrc[1], at + t * 2048 + 1024, k);
+        }
+#pragma unroll
+        for (int q = 0; q < 2 * RT; ++q)
+            load_to_lds(rsx, (q & 1 ? past1 : past0) ? 0x7ffffff0 : xsrc[q], at + NT * 2048 + q * 1024, k);
+    };
+    i32x4 acc[NT][RT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[t][j] = (i32x4){0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < PD; ++p) load(s0 + p, p);
+    int place = 0;
+    for (int s = s0; s < s1; ++s) {
+        MOE_VMCNT((PD - 1) * LOADS);
+        lds_handover();
+        const char *at = mine + place * STAGE;
+        u32x4 w[NT][2], x[RT][2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int f = fr * 128 + (((p * 4 + oct) ^ ((fr >> 1) & 7)) << 4);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[t][p] = *reinterpret_cast<const u32x4 *>(at + t * 2048 + f);
+#pragma unroll
+            for (int j = 0; j < RT; ++j) x[j][p] = *reinterpret_cast<const u32x4 *>(at + NT * 2048 + j * 2048 + f);
+        }
+        MOE_LGKM0();
+        lds_handover();
+        load(s + PD, place);
+        place = place == PD - 1 ? 0 : place + 1;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < RT; ++j)
+                    acc[t][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[t][p]), __builtin_bit_cast(i32x4, x[j][p]),
+                                                                     acc[t][j], 0, 0, 0);
+    }
+    MOE_VMCNT(0);
+    MOE_MATRIX_RESULTS();
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) asm volatile("" : "+v"(acc[t][j]));
+    // sums of the wavefronts: [wave][tile][lane] of four numbers
+    __syncthreads();
+    i32x4 *const sums = reinterpret_cast<i32x4 *>(q8_lds);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) sums[((j * NT + t) * WAVES + wave) * 64 + lane] = acc[t][j];
+    __syncthreads();
+    if (wave >= RT) return;
+    const int j = wave, row = j * 16 + fr, n = n0 + oct * 4;
+    if (row >= rows || n >= width) return;
+    float v[NT][4];
+    const float xs = row_scale(a, item.row0 + row);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        i32x4 s = sums[(j * NT + t) * WAVES * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += sums[((j * NT + t) * WAVES + w) * 64 + lane];
+        float cs[4];
+        column_scales(a.ws + static_cast<size_t>(item.expert) * a.N + t * a.h, n, width, cs);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[t][c] = static_cast<float>(s[c]) * xs * cs[c];
+    }
+    const size_t at = static_cast<size_t>(item.row0 + row);
+    if constexpr (PAIR) {
+        float hidden[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) hidden[c] = activate_by(a.act, v[0][c]) * v[1][c];
+        store_hidden(a, at, n, hidden);
+    } else {
+        finish(a, item.expert, at, n, v[0]);
+    }
+}
+
+// ---------------------------------------------------------------- tiles of 128 x 128
+template <bool PAIR, bool KTAIL, bool DEEP>
+__global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
+{
+    constexpr int BM = 128, BN = 128;
+    constexpr int F16 = kI8Operands;
+    constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = PAIR;
+    constexpr int tile_pitch = 0, pair_at = 0;
+    const uint16_t *const tile_in = nullptr;
+    const uint16_t *const A = a.x, *const W = a.w;
+    const int N = a.N, K = a.K, pair_h = a.h, row_div = a.row_div, a_rows = a.a_rows;
+    const int32_t *const row_src = PAIR ? a.row_src : nullptr;
+    const Tiles<BM, BN> items(a.offsets, a.E, a.tiles);
+#include "gemm_w4_body.inc"
+
+    // the wavefront's 64 rows of 64 columns (of a pair 32 of each), 32 bytes of row padding; 16 rows at a time
+    constexpr int PITCH = 256 + 32;
+    char *const patch = lds + wave * 64 * PITCH;
+    float xs[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) xs[j] = row_scale(a, item.row0 + min(wm * 64 + j * 16 + fr, rows - 1));
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            f32x4 v;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = sum_of(acc[i][j][c]) * xs[j];
+            *reinterpret_cast<f32x4 *>(patch + (j * 16 + fr) * PITCH + (i * 16 + oct * 4) * 4) = v;
+        }
+    lds_handover();
+    const float *ws = a.ws + static_cast<size_t>(item.expert) * N;
+    if constexpr (PAIR) {
+        const int col = lane % 8 * 4, n = n0 / 2 + wn * 32 + col, at = col / 16 * 32 + col % 16;
+        float gs[4], us[4];
+        column_scales(ws, n, a.h, gs);
+        column_scales(ws + a.h, n, a.h, us);
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int row = it * 8 + lane / 8;
+            if (wm * 64 + row >= rows || n >= a.h) continue;
+            const f32x4 g = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4);
+            const f32x4 u = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4 + 64);
+            float v[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = activate_by(a.act, g[c] * gs[c]) * (u[c] * us[c]);
+            store_hidden(a, static_cast<size_t>(item.row0 + wm * 64 + row), n, v);
+        }
+    } else {
+        const int col = lane % 16 * 4, n = n0 + wn * 64 + col;
+        float cs[4];
+        column_scales(ws, n, N, cs);
+        for (int it = 0; it < 16; ++it) {
+            const int row = it * 4 + lane / 16;
+            if (wm * 64 + row >= rows || n >= N) continue;
+            const f32x4 s = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + col * 4);
+            float v[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = s[c] * cs[c];
+            finish(a, item.expert, static_cast<size_t>(item.row0 + wm * 64 + row), n, v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- tiles of 256 columns
+// Both epilogues pass sums through the wavefront's patch (W4Place), 16 rows at a time, without a branch.
+// The linear map; N is a multiple of 4.  Y32: y is fp32.
+template <bool ERF, bool Y32, bool KTAIL, int BM>
+__global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
+{
+    constexpr int TM = W4Place<BM>::TM;
+    const Tiles<BM, 256> items(a.offsets, a.E, a.tiles);
+    const ActForm form(a.act);
+    struct Columns {                       // the tile's rows' scales; a lane's four columns of each half's 64
+        float xs[TM];
+        float ws[2][4], bias[2][4];
+    };
+    w4_run<kI8Operands, KTAIL, BM, 0>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, nullptr, 1, 0,
+        [&](const WorkItem &item, int wn, int) {
+            Columns c;
+            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) c.xs[j] = a.xs[min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1)];
+            const float *ws = a.ws + static_cast<size_t>(item.expert) * a.N;
+            const float *bias = a.bias != nullptr ? a.bias + static_cast<size_t>(item.expert) * a.N : ws;
+            const float with = a.bias != nullptr ? 1.0f : 0.0f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int n = min(item.n0 + wn * 128 + half * 64 + lane % 16 * 4, a.N - 4);
+                const f32x4 s = *reinterpret_cast<const f32x4 *>(ws + n), b = *reinterpret_cast<const f32x4 *>(bias + n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c.ws[half][e] = s[e];
+                    c.bias[half][e] = b[e] * with;
+                }
+            }
+            return c;
+        },
+        [&](auto &acc, const Columns &ahead, const WorkItem &item, const W4Place<BM> &place, auto landed) {
+            const int lane = place.lane, in_row = lane / 16;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int row0 = item.row0 + place.wm * (BM / 2) + j * 16;
+                const unsigned rows = static_cast<unsigned>(min(max(item.row1 - row0, 0), 16));
+                const size_t first = static_cast<size_t>(row0) * a.N;
+                // (a row past the tile's or a column past N lies past the resources, as all do of a residual that is not there)
+                const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
+                    static_cast<char *>(a.y) + first * (Y32 ? 4 : 2), 0, rows * static_cast<unsigned>(a.N) * (Y32 ? 4u : 2u), 0x00020000);
+                const bool wide = a.res == kF32;
+                char *const rbase = static_cast<char *>(const_cast<void *>(a.r)) + first * (wide ? 4 : 2);
+                const unsigned rbytes = a.r != nullptr ? rows * static_cast<unsigned>(a.N) : 0u;
+                const __amdgpu_buffer_rsrc_t r32 = __builtin_amdgcn_make_buffer_rsrc(rbase, 0, wide ? rbytes * 4u : 0u, 0x00020000);
+                const __amdgpu_buffer_rsrc_t r16 = __builtin_amdgcn_make_buffer_rsrc(rbase, 0, wide ? 0u : rbytes * 2u, 0x00020000);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int n = item.n0 + place.wn * 128 + half * 64 + lane % 16 * 4;
+                    lds_handover();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f32x4 v;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) v[c] = sum_of(acc[half * 4 + i][j][c]) * ahead.xs[j];
+                        // (a row's 16-byte pieces XOR-swizzled with the row)
+                        *reinterpret_cast<f32x4 *>(place.patch + place.fr * 256 + (((i * 4 + place.oct) ^ place.fr) << 4)) = v;
+                    }
+                    if (j == 0 && half == 0) landed();
+                    lds_handover();
+                    MOE_SB();
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) {
+                        const int row = it * 4 + in_row, at = n < a.N ? row * a.N + n : 0x1ffffff0;
+                        const f32x4 s = *reinterpret_cast<const f32x4 *>(place.patch + row * 256 + ((lane % 16 ^ row) << 4));
+                        const u32x4 rw = __builtin_amdgcn_raw_buffer_load_b128(r32, at * 4, 0, 0);
+                        const u32x2 rh = __builtin_amdgcn_raw_buffer_load_b64(r16, at * 2, 0, 0);
+                        float v[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            v[c] = activate<ERF>(form, __builtin_fmaf(s[c], ahead.ws[half][c], ahead.bias[half][c]));
+                            v[c] += __uint_as_float(rw[c]) + (a.res == kF16 ? f16_of(rh[c / 2], c % 2) : b16_of(rh[c / 2], c % 2));
+                        }
+                        if constexpr (Y32) {
+                            const u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                            __builtin_amdgcn_raw_buffer_store_b128(o, ry, at * 4, 0, 0);
+                        } else {
+                            const u32x2 h = {pack_16(kF16, v[0], v[1]), pack_16(kF16, v[2], v[3])};
+                            const u32x2 b = {pack_16(kB16, v[0], v[1]), pack_16(kB16, v[2], v[3])};
+                            __builtin_amdgcn_raw_buffer_store_b64(a.type == kF16 ? h : b, ry, at * 2, 0, 0);
+                        }
+                        MOE_SB();
+                    }
+                }
+            }
+        });
+}
+
+// The block's first projections: acc[2 p] and acc[2 p + 1] of a lane are gate and value of the same four columns.
+template <bool ERF, bool KTAIL, int BM>
+__global__ __launch_bounds__(256, 1) void q8_gated_run_kernel(Q8Args a)
+{
+    constexpr int TM = W4Place<BM>::TM;
+    const Tiles<BM, 256> items(a.offsets, a.E, a.tiles);
+    const ActForm form(a.act);
+    struct Scales {
+        float xs[TM];
+        float gs[4][4], us[4][4];
+    };
+    w4_run<kI8Operands, KTAIL, BM, 0, true>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, a.row_src, a.row_div, a.a_rows,
+        [&](const WorkItem &item, int wn, int oct) {
+            Scales c;
+            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
+            const int32_t *src = a.row_src != nullptr ? a.row_src : a.offsets;
+            const int div = a.row_src != nullptr ? a.row_div : 1;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int row = min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1);
+                const int from = src[a.row_src != nullptr ? row : 0] / div;
+                c.xs[j] = a.xs[a.row_src != nullptr ? from : row];
+            }
+            const float *gs = a.ws + static_cast<size_t>(item.expert) * a.N;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int n = min(item.n0 / 2 + wn * 64 + p * 16 + oct * 4, a.h - 4);      // (h is a multiple of 16)
+                const f32x4 g = *reinterpret_cast<const f32x4 *>(gs + n), u = *reinterpret_cast<const f32x4 *>(gs + a.h + n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c.gs[p][e] = g[e];
+                    c.us[p][e] = u[e];
+                }
+            }
+            return c;
+        },
+        [&](auto &acc, const Scales &ahead, const WorkItem &item, const W4Place<BM> &place, auto landed) {
+            const int col = item.n0 / 2 + place.wn * 64 + place.lane % 8 * 8;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int row0 = item.row0 + place.wm * (BM / 2) + j * 16;
+                lds_handover();
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    f16x4 o;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float g = sum_of(acc[2 * p][j][c]) * ahead.xs[j] * ahead.gs[p][c];
+                        const float u = sum_of(acc[2 * p + 1][j][c]) * ahead.xs[j] * ahead.us[p][c];
+                        o[c] = static_cast<_Float16>(activate<ERF>(form, g) * u);
+                    }
+                    *reinterpret_cast<f16x4 *>(place.at(p, 0)) = o;
+                    MOE_SB();
+                }
+                if (j == 0) landed();
+                // 16 rows of 64 columns, eight to a row's line
+                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                    static_cast<uint16_t *>(a.y) + static_cast<size_t>(row0) * a.h, 0,
+                    static_cast<unsigned>(min(max(item.row1 - row0, 0), 16)) * static_cast<unsigned>(a.h) * 2u, 0x00020000);
+                lds_handover();
+                MOE_SB();
+#pragma unroll
+                for (int it = 0; it < 2; ++it) {
+                    const int row = it * 8 + place.lane / 8;
+                    const u32x4 q = *reinterpret_cast<const u32x4 *>(place.patch + row * 256 + ((place.lane % 8 ^ row) << 4));
+                    __builtin_amdgcn_raw_buffer_store_b128(q, rs, col < a.h ? (row * a.h + col) * 2 : 0x7ff00000, 0, 0);
+                }
+                MOE_SB();
+            }
+        },
+        a.h);
+}
+
+// ---------------------------------------------------------------- dispatch
+// codes and scales of the tokens to their slots; a wavefront owns a token
+__global__ __launch_bounds__(256) void q8_scatter_kernel(const u32x4 *__restrict__ x, const float *__restrict__ xs,
+                                                         const int32_t *__restrict__ slot_of, u32x4 *__restrict__ xe,
+                                                         float *__restrict__ xes, int T, int k, int vec, int max_rows)
+{
+    const int lane = lane_id(), t = blockIdx.x * 4 + threadIdx.x / kWave;
+    if (t >= T) return;
+    int slot = lane < k ? slot_of[static_cast<size_t>(t) * k + lane] : -1;
+    if (slot >= max_rows) slot = -1;
+    if (slot >= 0) xes[slot] = xs[t];
+    for (int c = lane; c - lane < vec; c += kWave) {
+        const u32x4 v = x[static_cast<size_t>(t) * vec + min(c, vec - 1)];
+        for (int j = 0; j < k; ++j) {
+            const int to = __shfl(slot, j);
+            if (to >= 0 && c < vec) xe[static_cast<size_t>(to) * vec + c] = v;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host side
+// a kernel of 256 threads that needs more LDS than a launch gets unasked
+template <auto KERNEL>
+void launch_product_kernel(const Q8Args &a, int64_t blocks, size_t lds, int stage, hipStream_t st)
+{
+    static PerDeviceOnce once;
+    once.raise_lds(reinterpret_cast<const void *>(KERNEL), static_cast<int>(lds));
+    hipEvent_t t0 = nullptr, t1 = nullptr;
+    if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
+    hipExtLaunchKernelGGL(KERNEL, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, st, t0, t1, 0, a);
+}
+
+void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scale, const int32_t *rows_end, hipStream_t st)
+{
+    using std::integral_constant;
+    auto with_type = [&](auto ty) {
+        auto launch = [&](auto tpr, auto nv) {
+            constexpr int TPR = decltype(tpr)::value, PER = TPR == kWave ? 4 : 1;
+            const unsigned grid = static_cast<unsigned>(std::min<int64_t>((R + PER - 1) / PER, 1 << 20));
+            hipLaunchKernelGGL((q8_rows_kernel<decltype(ty)::value, TPR, decltype(nv)::value>), dim3(grid), dim3(TPR == kWave ? 256 : TPR),
+                               0, st, x, static_cast<uint32_t *>(q), scale, R, K, rows_end);
+        };
+        if (K <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+        else if (K <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+        else if (K <= 8192) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+        else if (K <= 16384) launch(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+        else launch(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    };
+    if (type == kF32) with_type(integral_constant<int, kF32>{});
+    else if (type == kB16) with_type(integral_constant<int, kB16>{});
+    else with_type(integral_constant<int, kF16>{});
+}
+
+// Tile of a product of `rows` rows of E experts, and whether the kernel for few rows takes it.
+struct Q8Plan {
+    int bm, bn;                            // bm 16 or 32: that kernel
+    bool deep;
+};
+Q8Plan plan_product(int64_t rows, int E, int columns, int K)
+{
+    if (rows <= 32ll * E && rows * ((columns + 127) / 128) <= 4000) return {rows <= 16ll * E ? 16 : 32, 0, false};
+    if (few_long_tiles(rows, E, columns, K)) return {128, 128, true};
+    GemmPlan gp;
+    choose_w4_tile(std::max<int64_t>(rows, 256), E, columns, K, &gp);
+    return {gp.bm, gp.bn, false};
+}
+
+template <bool PAIR>
+moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
+{
+    const int columns = tile_columns(a);
+    Q8Plan plan = plan_product(rows, a.E, columns, a.K);
+    if (!PAIR && plan.bn == 256 && a.N % 4 != 0) plan = {128, 128, false};
+    const int bn = plan.bm <= 32 ? (PAIR ? 32 : 16) : plan.bn;
+    a.tiles = (columns + bn - 1) / bn;
+    const int64_t entries = tile_entries(rows, a.E, plan.bm, a.tiles);
+    if (entries >= 1ll << 30) {
+        set_error("products of %lld rows and %d columns: more than 2^30 tiles", static_cast<long long>(rows), columns);
+        return MOE_EUNSUPPORTED;
+    }
+    a.entries = static_cast<int>(entries);
+    if (plan.bm <= 32) {
+        constexpr int PD = 4;
+        auto stream = [&](auto rt) {
+            constexpr int RT = decltype(rt)::value;
+            launch_product_kernel<q8_stream_kernel<PAIR, RT, PD>>(a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048, stage, st);
+        };
+        if (plan.bm == 16) stream(std::integral_constant<int, 1>{});
+        else stream(std::integral_constant<int, 2>{});
+        return MOE_OK;
+    }
+    auto with_tail = [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if (plan.bn == 128) {
+            if (plan.deep) launch_product_kernel<q8_tile_kernel<PAIR, TAIL, true>>(a, entries, kW4Lds, stage, st);
+            else launch_product_kernel<q8_tile_kernel<PAIR, TAIL, false>>(a, entries, w4_lds(128, 128), stage, st);
+            return;
+        }
+        a.share = w4_run_share(plan.bm, a.K);
+        const int blocks = w4_run_blocks(a.entries, a.share);
+        auto with_rows = [&](auto bm) {
+            constexpr int BM = decltype(bm)::value;
+            auto with_act = [&](auto erf) {
+                constexpr bool ERF = decltype(erf)::value;
+                if constexpr (PAIR) launch_product_kernel<q8_gated_run_kernel<ERF, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
+                else if (a.type == kF32) launch_product_kernel<q8_run_kernel<ERF, true, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
+                else launch_product_kernel<q8_run_kernel<ERF, false, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
+            };
+            if (a.act == MOE_ACT_GELU_ERF) with_act(std::true_type{});
+            else with_act(std::false_type{});
+        };
+        if (plan.bm == 256) with_rows(std::integral_constant<int, 256>{});
+        else with_rows(std::integral_constant<int, 128>{});
+    };
+    if (a.K % 64 == 0 && (plan.bn != 256 || a.K >= 256)) with_tail(std::false_type{});
+    else with_tail(std::true_type{});
+    return MOE_OK;
+}
+
+bool known_type(int type) { return type >= kF32 && type <= kF16; }
+
+moe_status check_rows(const char *call, int64_t R, int K, int type)
+{
+    if (R < 1 || K < 1 || !known_type(type)) {
+        set_error("%s: R and K must be >= 1 and the type 0 (fp32), 1 (bf16) or 2 (fp16)", call);
+        return MOE_EINVAL;
+    }
+    if (K % 16 != 0 || K > kMaxDepth || R > (1ll << 40) / K) {
+        set_error("%s: K = %d must be a multiple of 16 up to %d, and R K at most 2^40", call, K, kMaxDepth);
+        return MOE_EUNSUPPORTED;
+    }
+    return MOE_OK;
+}
+
+moe_status check_q8_block(const moe_shape *s)
+{
+    const moe_status rc = check_layer_shape(s);
+    if (rc != MOE_OK) return rc;
+    if (s->dtype != MOE_BF16) {
+        set_error("moe_gated_ffn_q8: bf16 layers only");
+        return MOE_EUNSUPPORTED;
+    }
+    if (s->d_model % 16 != 0 || s->d_ff % 16 != 0 || s->d_model > kMaxDepth || s->d_ff > kMaxDepth ||
+        2ll * s->d_ff * s->d_model >= (1ll << 31) - (1 << 26) || moe_max_rows(s) >= 1ll << 30) {
+        set_error("moe_gated_ffn_q8: d_model and d_ff multiples of 16 up to %d, 2 d_ff d_model below 2^31 - 2^26, rows below 2^30", kMaxDepth);
+        return MOE_EUNSUPPORTED;
+    }
+    if (tile_entries(moe_max_rows(s), s->E, 128, (std::max(s->d_model, 2 * s->d_ff) + 127) / 128) >= 1ll << 30) {
+        set_error("moe_gated_ffn_q8: more than 2^30 tiles");
+        return MOE_EUNSUPPORTED;
+    }
+    return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+moe_status moe_q8_rows(int64_t R, int32_t K, int32_t type, const void *x, void *q, float *scale, void *stream)
+{
+    const moe_status rc = check_rows("moe_q8_rows", R, K, type);
+    if (rc != MOE_OK) return rc;
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(q);
+    MOE_REQUIRE_PTR(scale);
+    launch_rows(R, K, type, x, q, scale, nullptr, static_cast<hipStream_t>(stream));
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+moe_status moe_q8_values(int64_t R, int32_t K, int32_t type, const void *q, const float *scale, void *x, void *stream)
+{
+    const moe_status rc = check_rows("moe_q8_values", R, K, type);
+    if (rc != MOE_OK) return rc;
+    MOE_REQUIRE_PTR(q);
+    MOE_REQUIRE_PTR(scale);
+    MOE_REQUIRE_PTR(x);
+    const int rows = std::max(1, 1024 / (K / 16));
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((R + rows - 1) / rows, 1 << 20));
+    auto launch = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<const uint32_t *>(q), scale, x, R, K, rows);
+    };
+    if (type == kF32) launch(q8_values_kernel<kF32>);
+    else if (type == kB16) launch(q8_values_kernel<kB16>);
+    else launch(q8_values_kernel<kF16>);
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+moe_status moe_q8_linear(const moe_q8_shape *s, const void *x, const float *x_scale, const int32_t *offsets, const void *w,
+                         const float *w_scale, const float *bias, const void *r, void *y, void *stream)
+{
+    if (s == nullptr) {
+        set_error("moe_q8_linear: shape is NULL");
+        return MOE_EINVAL;
+    }
+    if (s->R < 1 || s->E < 1 || s->N < 1 || s->K < 1 || !known_type(s->res) || !known_type(s->y) || s->act < MOE_ACT_GELU_ERF ||
+        s->act > MOE_ACT_SILU) {
+        set_error("moe_q8_linear: R, E, N, K must be >= 1, res and y 0 (fp32), 1 (bf16) or 2 (fp16), act a moe_act");
+        return MOE_EINVAL;
+    }
+    if (s->E > kMaxExperts || s->N >= 1 << 22 || s->K % 16 != 0 || s->K > kMaxDepth || s->R >= 1 << 30) {
+        set_error("moe_q8_linear: at most %d experts, N below 2^22, K a multiple of 16 up to %d, R below 2^30", kMaxExperts, kMaxDepth);
+        return MOE_EUNSUPPORTED;
+    }
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(x_scale);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(w);
+    MOE_REQUIRE_PTR(w_scale);
+    MOE_OPTIONAL_PTR(bias);
+    MOE_OPTIONAL_PTR(r);
+    MOE_REQUIRE_PTR(y);
+    Q8Args a = {};
+    a.x = static_cast<const uint16_t *>(x);
+    a.xs = x_scale;
+    a.w = static_cast<const uint16_t *>(w);
+    a.ws = w_scale;
+    a.bias = bias;
+    a.r = r;
+    a.y = y;
+    a.offsets = offsets;
+    a.row_div = 1;
+    a.E = s->E;
+    a.N = s->N;
+    a.K = s->K / 2;
+    a.act = s->act;
+    a.res = s->res;
+    a.type = s->y;
+    const moe_status rc = launch_product<false>(a, s->R, -1, static_cast<hipStream_t>(stream));
+    if (rc != MOE_OK) return rc;
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+moe_status moe_dispatch_q8(const moe_shape *s, const void *x, const float *x_scale, const int32_t *expert_idx,
+                           int32_t *counts, int32_t *offsets, int32_t *slot_of, int32_t *src_of, void *xe, float *xe_scale,
+                           void *workspace, void *stream)
+{
+    const moe_status rc = check_layer_shape(s);
+    if (rc != MOE_OK) return rc;
+    if (s->d_model % 16 != 0) {
+        set_error("moe_dispatch_q8: d_model = %d must be a multiple of 16", s->d_model);
+        return MOE_EUNSUPPORTED;
+    }
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(x_scale);
+    MOE_REQUIRE_PTR(expert_idx);
+    MOE_REQUIRE_PTR(counts);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(slot_of);
+    MOE_REQUIRE_PTR(src_of);
+    MOE_OPTIONAL_PTR(xe);
+    MOE_OPTIONAL_PTR(xe_scale);
+    if ((xe == nullptr) != (xe_scale == nullptr)) {
+        set_error("moe_dispatch_q8: xe and xe_scale come together");
+        return MOE_EINVAL;
+    }
+    MOE_REQUIRE_PTR(workspace);
+    Workspace w;
+    layout_workspace(*s, 1, 1, workspace, &w);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    prof_begin(kStagePlan, st);
+    const moe_status plan = launch_plan(*s, expert_idx, counts, offsets, slot_of, src_of, w, false, 0, st);
+    prof_end(kStagePlan, st);
+    if (plan != MOE_OK) return plan;
+    if (xe != nullptr) {
+        hipLaunchKernelGGL(q8_scatter_kernel, dim3(ceil_div(s->T, 4)), dim3(256), 0, st, static_cast<const u32x4 *>(x), x_scale, slot_of,
+                           static_cast<u32x4 *>(xe), xe_scale, s->T, s->k, s->d_model / 16, static_cast<int>(moe_max_rows(s)));
+        MOE_TRY_HIP(hipGetLastError());
+    }
+    return MOE_OK;
+}
+
+size_t moe_gated_q8_workspace_bytes(const moe_shape *s)
+{
+    if (check_q8_block(s) != MOE_OK) return 0;
+    const size_t R = static_cast<size_t>(moe_max_rows(s));
+    return align_up(R * s->d_ff * 2, 256) + align_up(R * s->d_ff, 256) + align_up(R * 4, 256);
+}
+
+moe_status moe_gated_ffn_q8(const moe_shape *s, const void *x, const float *x_scale, const int32_t *src_of,
+                            const int32_t *offsets, const void *q13, const float *scale13, const void *q2,
+                            const float *scale2, void *ye, void *workspace, void *stream)
+{
+    const moe_status rc = check_q8_block(s);
+    if (rc != MOE_OK) return rc;
+    if (src_of != nullptr && static_cast<int64_t>(s->T) * s->d_model >= (1ll << 31) - (1 << 20)) {
+        set_error("moe_gated_ffn_q8: with src_of T d_model has to be below 2^31 - 2^20; moe_dispatch_q8 moves the rows");
+        return MOE_EUNSUPPORTED;
+    }
+    MOE_REQUIRE_PTR(x);
+    MOE_REQUIRE_PTR(x_scale);
+    MOE_OPTIONAL_PTR(src_of);
+    MOE_REQUIRE_PTR(offsets);
+    MOE_REQUIRE_PTR(q13);
+    MOE_REQUIRE_PTR(scale13);
+    MOE_REQUIRE_PTR(q2);
+    MOE_REQUIRE_PTR(scale2);
+    MOE_REQUIRE_PTR(ye);
+    MOE_REQUIRE_PTR(workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const size_t R = static_cast<size_t>(moe_max_rows(s));
+    char *const hidden = static_cast<char *>(workspace), *const codes = hidden + align_up(R * s->d_ff * 2, 256);
+    float *const scales = reinterpret_cast<float *>(codes + align_up(R * s->d_ff, 256));
+    Q8Args a = {};
+    a.x = static_cast<const uint16_t *>(x);
+    a.xs = x_scale;
+    a.w = static_cast<const uint16_t *>(q13);
+    a.ws = scale13;
+    a.y = hidden;
+    a.offsets = offsets;
+    a.row_src = src_of;
+    a.row_div = s->k;
+    a.a_rows = s->T;
+    a.E = s->E;
+    a.N = 2 * s->d_ff;
+    a.K = s->d_model / 2;
+    a.h = s->d_ff;
+    a.act = s->act;
+    const moe_status first = launch_product<true>(a, static_cast<int64_t>(R), kStageGemm1, st);
+    if (first != MOE_OK) return first;
+    launch_rows(static_cast<int64_t>(R), s->d_ff, kF16, hidden, codes, scales, offsets + s->E, st);
+    Q8Args b = {};
+    b.x = reinterpret_cast<const uint16_t *>(codes);
+    b.xs = scales;
+    b.w = static_cast<const uint16_t *>(q2);
+    b.ws = scale2;
+    b.y = ye;
+    b.offsets = offsets;
+    b.row_div = 1;
+    b.E = s->E;
+    b.N = s->d_model;
+    b.K = s->d_ff / 2;
+    b.act = MOE_ACT_IDENTITY;
+    b.type = kF16;
+    const moe_status second = launch_product<false>(b, static_cast<int64_t>(R), kStageGemm2, st);
+    if (second != MOE_OK) return second;
+    MOE_TRY_HIP(hipGetLastError());
+    return MOE_OK;
+}
+
+}  // extern "C"
