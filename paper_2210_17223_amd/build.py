@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe.so")
 SOURCES = ["api.hip", "route.hip", "plan.hip", "rows.hip", "ffn.hip", "sched.hip", "bwd.hip", "offload.hip",
-           "comm.hip", "calib.hip", "norm.hip", "gated.hip", "q4.hip", "q8.hip"]
+           "comm.hip", "calib.hip", "norm.hip", "gated.hip", "q4.hip", "q8.hip", "q8_run.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -78,7 +78,8 @@ struct W4Place {                       // where a wavefront stands in its tile
 // the accumulators, without a branch, acc[i][j][c] = column wn * 128 + i * 16 + oct * 4 + c, row wm * BM / 2 + j * 16 + fr, and calls landed() once, in
 // front of its first store: what the next tile waits for early has to be there before stores stand in front of it.
 // items: the list, or what finds entry b by items[b].  F16 may be kI8Operands (K is then half the depth); PAIR: the tile's columns
-// are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).
+// are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).  Of 8-bit operands, whose tiles have half
+// the stages and more to prepare (scales of rows and columns), prepare is called in front of the tile's first stage instead of behind its last.
 template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, typename Items, typename Prepare, typename Epilogue>
 __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uint16_t *__restrict__ W,
                                        const Items &items, const int32_t *__restrict__ nitems, int entries, int share,
@@ -289,6 +290,12 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         const WorkItem later = next.expert >= 0 ? item_at(b + stride) : next;
         int source = 0;
         if (row_src != nullptr && later.expert >= 0) source = *source_at(later);
+        constexpr bool EARLY = F16 == kI8Operands;
+        auto prepared = [&](auto now) {
+            if constexpr (decltype(now)::value) return prepare(item, wn, oct);
+            else return 0;
+        };
+        const auto early = prepared(integral_constant<bool, EARLY>{});
         stage(std::true_type{}, 2, W_AHEAD, fresh);     // (behind an epilogue: see landed)
         for (int kt = 1; kt < KT; ++kt) {
             if (kt == KT - W_AHEAD) rsw = weights_of(next);
@@ -300,7 +307,7 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
             const int ka = kt + 2, kw = kt + W_AHEAD;
             stage(std::false_type{}, ka < KT ? ka : ka - KT, kw < KT ? kw : kw - KT, true);
         }
-        const auto ahead = prepare(item, wn, oct);
+        const auto late = prepared(integral_constant<bool, !EARLY>{});
         MOE_MATRIX_RESULTS();
         // From here to the last accumulator's use there is no branch: values that cross one leave the AGPRs all at
         // once.  (And no read of an accumulator goes in front of the no-ops.)
@@ -314,6 +321,10 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         asm volatile("" : "+v"(here));
         const W4Place<BM> place{lds + (RING5 ? uf : 3 * (A_UNIT + W_UNIT)) + wave * (W4Place<BM>::UR * 256), here, wm, wn,
                                 here & 15, here >> 4};
+        const auto &ahead = [&]() -> const auto & {
+            if constexpr (EARLY) return early;
+            else return late;
+        }();
         epilogue(acc, ahead, item, place, [&]() {
             MOE_SB();
             MOE_VMCNT(RING5 ? 0 : TN);            // the next tile's first two stages

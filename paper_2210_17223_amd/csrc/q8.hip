@@ -12,6 +12,7 @@
 #include "moe_q8.h"
 #include "gated.h"
 #include "q8.h"
+#include "q8_product.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -21,23 +22,9 @@
 namespace moe {
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
-typedef __attribute__((ext_vector_type(4))) int i32x4;
+#include "q8_product_device.h"
 
-#include "gemm_w4.h"
-#include "gemm_w4_run.h"
-
-enum { kF32 = 0, kB16 = 1, kF16 = 2 };       // element types as in moe_q8_shape
 constexpr int kMaxDepth = 65536;             // values of a row
-
-// one of the two fp16 (bf16) values of a dword.  (By value: a bit cast of a vector's element casts its first one.)
-__device__ __forceinline__ float f16_of(uint32_t w, int i) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[i]); }
-__device__ __forceinline__ float b16_of(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
 
 // ---------------------------------------------------------------- rows to codes and back
 // 16 values of a row as they lie in memory
@@ -110,20 +97,6 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void q8_rows_kernel(const
     }
 }
 
-__device__ __forceinline__ uint32_t pack_16(int type, float lo, float hi)
-{
-    if (type == kF16) {
-        f16x2 h;
-        h[0] = static_cast<_Float16>(lo);
-        h[1] = static_cast<_Float16>(hi);
-        return __builtin_bit_cast(uint32_t, h);
-    }
-    bf16x2 b;
-    b[0] = static_cast<__bf16>(lo);
-    b[1] = static_cast<__bf16>(hi);
-    return __builtin_bit_cast(uint32_t, b);
-}
-
 // A block takes `rows` rows' pieces of 16 codes.
 template <int TYPE>
 __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restrict__ q, const float *__restrict__ scale, void *__restrict__ x,
@@ -154,161 +127,6 @@ __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restri
             }
         }
     }
-}
-
-// ---------------------------------------------------------------- products: what they share
-// K: pairs of codes.  Tiles are found from the experts' offsets.
-struct Q8Args {
-    const uint16_t *x, *w;
-    const float *xs, *ws, *bias;
-    const void *r;
-    void *y;
-    const int32_t *offsets, *row_src;      // row_src: the first product takes row row_src[i] / row_div, of a_rows
-    int row_div, a_rows;
-    int E, N, K;                           // of a pair of projections N = 2 h
-    int h;                                 // else 0
-    int act, res, type;
-    int tiles, entries, share;
-};
-
-// acc columns of a tile: BN packed ones of a pair of projections, sixteen of the first and the same sixteen of the second in turn
-__host__ __device__ inline int tile_columns(const Q8Args &a) { return a.h != 0 ? gated_packed_columns(a.h) : a.N; }
-
-// The tile of block entry b: a panel of kPanel tiles' rows of an expert column by column, then the next; an eighth of all tiles for
-// each XCD.  A wavefront holds the experts' row tiles and their running sum, a lane each.
-constexpr int kPanel = 8;
-template <int BM, int BN>
-struct Tiles {
-    int first, end, row_tiles, sum, per_xcd, total, tiles;
-    __device__ __forceinline__ Tiles(const int32_t *__restrict__ offsets, int E, int column_tiles) : tiles(column_tiles)
-    {
-        const int lane = lane_id(), e = min(lane, E - 1);
-        first = offsets[e];
-        end = lane < E ? offsets[e + 1] : first;
-        row_tiles = end > first ? (end - first + BM - 1) / BM : 0;
-        sum = row_tiles * tiles;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int v = __shfl_up(sum, d);
-            if (lane >= d) sum += v;
-        }
-        total = __builtin_amdgcn_readlane(sum, kWave - 1);
-        per_xcd = (total + 7) / 8;
-    }
-    __device__ __forceinline__ WorkItem operator[](int b) const
-    {
-        const int slot = b / 8, index = b % 8 * per_xcd + slot;
-        if (slot >= per_xcd || index >= total) return WorkItem{-1, 0, 0, 0};
-        const int e = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
-        const int mt = __builtin_amdgcn_readlane(row_tiles, e);
-        const int within = index - (__builtin_amdgcn_readlane(sum, e) - mt * tiles);
-        const int panel = within / (kPanel * tiles), rest = within - panel * (kPanel * tiles), high = min(kPanel, mt - panel * kPanel);
-        const int column = rest / high, row0 = __builtin_amdgcn_readlane(first, e) + (panel * kPanel + rest - column * high) * BM;
-        return WorkItem{e, row0, min(row0 + BM, __builtin_amdgcn_readlane(end, e)), column * BN};
-    }
-};
-inline int64_t tile_entries(int64_t rows, int E, int bm, int tiles)
-{
-    return static_cast<int64_t>(align_up((static_cast<size_t>(rows) / bm + std::min<int64_t>(rows, E)) * tiles, 8));
-}
-
-// All activations but the erf form of the GeLU as factor * v / (1 + 2^-(v (a + b v^2))): silu; its tanh form; relu, whose a is so large
-// that the quotient is 1 or 0 from |v| = 1e-36 on; and identity, 2 v / 2.  An epilogue that holds accumulators takes no branch, and a
-// kernel for each activation is five times the code.  (v^2 is bounded so that 0 v^2 is 0.)
-struct ActForm {
-    float a, b, factor;
-    __device__ __forceinline__ explicit ActForm(int act)
-    {
-        a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : act == MOE_ACT_RELU ? 1e38f : 0.0f;
-        b = act == MOE_ACT_GELU_TANH ? 0.10294324f : 0.0f;
-        factor = act == MOE_ACT_IDENTITY ? 2.0f : 1.0f;
-    }
-    __device__ __forceinline__ float operator()(float v) const
-    {
-        const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
-        const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
-        return v * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
-    }
-};
-template <bool ERF>
-__device__ __forceinline__ float activate(const ActForm &form, float v)
-{
-    if constexpr (ERF) return gelu_erf_fast(v);
-    else return form(v);
-}
-__device__ __forceinline__ float activate_by(int act, float v)
-{
-    switch (act) {
-    case MOE_ACT_GELU_ERF: return gate_value<MOE_ACT_GELU_ERF>(v);
-    case MOE_ACT_GELU_TANH: return gate_value<MOE_ACT_GELU_TANH>(v);
-    case MOE_ACT_RELU: return gate_value<MOE_ACT_RELU>(v);
-    case MOE_ACT_SILU: return gate_value<MOE_ACT_SILU>(v);
-    default: return v;
-    }
-}
-__device__ __forceinline__ float sum_of(float bits) { return static_cast<float>(__builtin_bit_cast(int, bits)); }
-
-__device__ __forceinline__ float load_value(const void *p, int type, size_t at)
-{
-    if (type == kF32) return static_cast<const float *>(p)[at];
-    const uint16_t h = static_cast<const uint16_t *>(p)[at];
-    return type == kB16 ? bf16_to_f32(h) : static_cast<float>(__builtin_bit_cast(_Float16, h));
-}
-// y of columns n .. n + 3 of a row; v: sums times both scales
-__device__ __forceinline__ void finish(const Q8Args &a, int expert, size_t row, int n, float (&v)[4])
-{
-    const size_t at = row * a.N + n;
-    const float *bias = a.bias != nullptr ? a.bias + static_cast<size_t>(expert) * a.N + n : nullptr;
-    if (a.N % 4 == 0) {                    // (whole groups, and their addresses are multiples of the groups' size)
-        if (bias != nullptr) {
-            const f32x4 b = *reinterpret_cast<const f32x4 *>(bias);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] += b[c];
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = activate_by(a.act, v[c]);
-        if (a.r != nullptr) {
-            if (a.res == kF32) {
-                const f32x4 r = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.r) + at);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] += r[c];
-            } else {
-                const u32x2 r = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.r) + at);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] += a.res == kF16 ? f16_of(r[c / 2], c % 2) : b16_of(r[c / 2], c % 2);
-            }
-        }
-        if (a.type == kF32)
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + at) = (f32x4){v[0], v[1], v[2], v[3]};
-        else
-            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + at) = (u32x2){pack_16(a.type, v[0], v[1]), pack_16(a.type, v[2], v[3])};
-        return;
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        if (n + c >= a.N) return;
-        float u = activate_by(a.act, v[c] + (bias != nullptr ? bias[c] : 0.0f));
-        if (a.r != nullptr) u += load_value(a.r, a.res, at + c);
-        if (a.type == kF32) static_cast<float *>(a.y)[at + c] = u;
-        else static_cast<uint16_t *>(a.y)[at + c] = static_cast<uint16_t>(pack_16(a.type, u, 0.0f));
-    }
-}
-__device__ __forceinline__ void store_hidden(const Q8Args &a, size_t row, int n, const float (&v)[4])
-{
-    f16x4 o;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] = static_cast<_Float16>(v[c]);
-    *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(a.y) + row * a.h + n) = o;
-}
-__device__ __forceinline__ float row_scale(const Q8Args &a, int row)
-{
-    return a.xs[a.row_src != nullptr ? a.row_src[row] / a.row_div : row];
-}
-// scales of columns n .. n + 3, of the last column past it
-__device__ __forceinline__ void column_scales(const float *__restrict__ p, int n, int N, float (&s)[4])
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c) s[c] = p[min(n + c, N - 1)];
 }
 
 // ---------------------------------------------------------------- few rows per expert
@@ -427,16 +245,35 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
         float cs[4];
         column_scales(a.ws + static_cast<size_t>(item.expert) * a.N + t * a.h, n, width, cs);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[t][c] = static_cast<float>(s[c]) * xs * cs[c];
+        for (int c = 0; c < 4; ++c) {
+            const float in = static_cast<float>(s[c]) * xs;
+            if constexpr (PAIR) v[t][c] = in * cs[c];
+            else v[t][c] = __builtin_fmaf(in, cs[c], a.bias != nullptr ? a.bias[static_cast<size_t>(item.expert) * a.N + min(n + c, a.N - 1)] : 0.0f);
+        }
     }
     const size_t at = static_cast<size_t>(item.row0 + row);
-    if constexpr (PAIR) {
-        float hidden[4];
+    const ActForm form(a.act);
+    with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto act) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) hidden[c] = activate_by(a.act, v[0][c]) * v[1][c];
-        store_hidden(a, at, n, hidden);
+        for (int c = 0; c < 4; ++c) v[0][c] = activate<decltype(act)::value>(form, v[0][c]) * (PAIR ? v[NT - 1][c] : 1.0f);
+    });
+    if constexpr (PAIR) {
+        store_hidden(a, at, n, v[0]);
+    } else if (a.N % 4 == 0) {
+        uint32_t r[4] = {0, 0, 0, 0};
+        if (a.r != nullptr) load_residual(a, at * a.N + n, r);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[0][c] += a.r != nullptr ? residual(a, r, c) : 0.0f;
+        store_output(a, at * a.N + n, v[0]);
     } else {
-        finish(a, item.expert, at, n, v[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (n + c >= a.N) return;
+            uint32_t r[1] = {0};
+            if (a.r != nullptr) load_residual(a, at * a.N + n + c, r);
+            const float u[1] = {v[0][c] + (a.r != nullptr ? residual(a, r, 0) : 0.0f)};
+            store_output(a, at * a.N + n + c, u);
+        }
     }
 }
 
@@ -453,14 +290,37 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
     const int N = a.N, K = a.K, pair_h = a.h, row_div = a.row_div, a_rows = a.a_rows;
     const int32_t *const row_src = PAIR ? a.row_src : nullptr;
     const Tiles<BM, BN> items(a.offsets, a.E, a.tiles);
+    // scales and biases are on their way through the stages
+    const WorkItem mine = items[blockIdx.x];
+    if (mine.expert < 0) return;
+    constexpr int TM_ = BM / 32;
+    const int l = lane_id(), wm_ = threadIdx.x / kWave & 1, wn_ = threadIdx.x / (2 * kWave);
+    int source[TM_];
+    float xs[TM_];
+#pragma unroll
+    for (int j = 0; j < TM_; ++j) {
+        source[j] = min(mine.row0 + wm_ * 64 + j * 16 + (l & 15), mine.row1 - 1);
+        if (row_src != nullptr) source[j] = row_src[source[j]];
+        else xs[j] = a.xs[source[j]];
+    }
+    // a lane's columns on the way out: four of the wavefront's 64, or one where rows are no multiples of four columns; of a pair four
+    const bool fours = PAIR || N % 4 == 0;
+    const int col = PAIR ? l % 8 * 4 : fours ? l % 16 * 4 : l, width = PAIR ? pair_h : N;
+    const int n = PAIR ? mine.n0 / 2 + wn_ * 32 + col : mine.n0 + wn_ * 64 + col;
+    const float *const ws = a.ws + static_cast<size_t>(mine.expert) * N;
+    const float *const other = PAIR ? ws + pair_h : a.bias != nullptr ? a.bias + static_cast<size_t>(mine.expert) * N : nullptr;
+    float cs[4], cb[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // (cb: of a pair the second's scales)
+    column_scales(ws, n, width, cs);
+    if (other != nullptr) column_scales(other, n, width, cb);
 #include "gemm_w4_body.inc"
 
-    // the wavefront's 64 rows of 64 columns (of a pair 32 of each), 32 bytes of row padding; 16 rows at a time
+    // the wavefront's 64 rows of 64 columns (of a pair 32 of each), 32 bytes of row padding
     constexpr int PITCH = 256 + 32;
     char *const patch = lds + wave * 64 * PITCH;
-    float xs[TM];
+    if (row_src != nullptr) {
 #pragma unroll
-    for (int j = 0; j < TM; ++j) xs[j] = row_scale(a, item.row0 + min(wm * 64 + j * 16 + fr, rows - 1));
+        for (int j = 0; j < TM; ++j) xs[j] = a.xs[source[j] / row_div];
+    }
 #pragma unroll
     for (int j = 0; j < TM; ++j)
 #pragma unroll
@@ -471,201 +331,65 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
             *reinterpret_cast<f32x4 *>(patch + (j * 16 + fr) * PITCH + (i * 16 + oct * 4) * 4) = v;
         }
     lds_handover();
-    const float *ws = a.ws + static_cast<size_t>(item.expert) * N;
-    if constexpr (PAIR) {
-        const int col = lane % 8 * 4, n = n0 / 2 + wn * 32 + col, at = col / 16 * 32 + col % 16;
-        float gs[4], us[4];
-        column_scales(ws, n, a.h, gs);
-        column_scales(ws + a.h, n, a.h, us);
-#pragma unroll
-        for (int it = 0; it < 8; ++it) {
-            const int row = it * 8 + lane / 8;
-            if (wm * 64 + row >= rows || n >= a.h) continue;
-            const f32x4 g = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4);
-            const f32x4 u = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4 + 64);
-            float v[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = activate_by(a.act, g[c] * gs[c]) * (u[c] * us[c]);
-            store_hidden(a, static_cast<size_t>(item.row0 + wm * 64 + row), n, v);
-        }
-    } else {
-        const int col = lane % 16 * 4, n = n0 + wn * 64 + col;
-        float cs[4];
-        column_scales(ws, n, N, cs);
-        for (int it = 0; it < 16; ++it) {
-            const int row = it * 4 + lane / 16;
-            if (wm * 64 + row >= rows || n >= N) continue;
-            const f32x4 s = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + col * 4);
-            float v[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = s[c] * cs[c];
-            finish(a, item.expert, static_cast<size_t>(item.row0 + wm * 64 + row), n, v);
-        }
-    }
-}
-
-// ---------------------------------------------------------------- tiles of 256 columns
-// Both epilogues pass sums through the wavefront's patch (W4Place), 16 rows at a time, without a branch.
-// The linear map; N is a multiple of 4.  Y32: y is fp32.
-template <bool ERF, bool Y32, bool KTAIL, int BM>
-__global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
-{
-    constexpr int TM = W4Place<BM>::TM;
-    const Tiles<BM, 256> items(a.offsets, a.E, a.tiles);
     const ActForm form(a.act);
-    struct Columns {                       // the tile's rows' scales; a lane's four columns of each half's 64
-        float xs[TM];
-        float ws[2][4], bias[2][4];
-    };
-    w4_run<kI8Operands, KTAIL, BM, 0>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, nullptr, 1, 0,
-        [&](const WorkItem &item, int wn, int) {
-            Columns c;
-            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
+    const int left = rows - wm * 64;                      // of the wavefront's rows
+    const size_t row0 = static_cast<size_t>(item.row0) + wm * 64;
+    with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto actc) {
+        constexpr int ACT = decltype(actc)::value;
+        if constexpr (PAIR) {
+            const int at = col / 16 * 32 + col % 16;
+            if (n >= width) return;
 #pragma unroll
-            for (int j = 0; j < TM; ++j) c.xs[j] = a.xs[min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1)];
-            const float *ws = a.ws + static_cast<size_t>(item.expert) * a.N;
-            const float *bias = a.bias != nullptr ? a.bias + static_cast<size_t>(item.expert) * a.N : ws;
-            const float with = a.bias != nullptr ? 1.0f : 0.0f;
+            for (int it = 0; it < 8; ++it) {
+                const int row = it * 8 + lane / 8;
+                const f32x4 g = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4);
+                const f32x4 u = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + at * 4 + 64);
+                float v[4];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int n = min(item.n0 + wn * 128 + half * 64 + lane % 16 * 4, a.N - 4);
-                const f32x4 s = *reinterpret_cast<const f32x4 *>(ws + n), b = *reinterpret_cast<const f32x4 *>(bias + n);
+                for (int c = 0; c < 4; ++c) v[c] = activate<ACT>(form, g[c] * cs[c]) * (u[c] * cb[c]);
+                if (row < left) store_hidden(a, row0 + row, n, v);
+            }
+        } else if (fours) {
+            if (n >= width) return;
+            // eight rows' residuals are on their way together
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    c.ws[half][e] = s[e];
-                    c.bias[half][e] = b[e] * with;
+            for (int part = 0; part < 2; ++part) {
+                uint32_t r[8][4];
+                if (a.r != nullptr) {
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) load_residual(a, (row0 + min((part * 8 + it) * 4 + lane / 16, max(left - 1, 0))) * N + n, r[it]);
                 }
-            }
-            return c;
-        },
-        [&](auto &acc, const Columns &ahead, const WorkItem &item, const W4Place<BM> &place, auto landed) {
-            const int lane = place.lane, in_row = lane / 16;
 #pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                const int row0 = item.row0 + place.wm * (BM / 2) + j * 16;
-                const unsigned rows = static_cast<unsigned>(min(max(item.row1 - row0, 0), 16));
-                const size_t first = static_cast<size_t>(row0) * a.N;
-                // (a row past the tile's or a column past N lies past the resources, as all do of a residual that is not there)
-                const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
-                    static_cast<char *>(a.y) + first * (Y32 ? 4 : 2), 0, rows * static_cast<unsigned>(a.N) * (Y32 ? 4u : 2u), 0x00020000);
-                const bool wide = a.res == kF32;
-                char *const rbase = static_cast<char *>(const_cast<void *>(a.r)) + first * (wide ? 4 : 2);
-                const unsigned rbytes = a.r != nullptr ? rows * static_cast<unsigned>(a.N) : 0u;
-                const __amdgpu_buffer_rsrc_t r32 = __builtin_amdgcn_make_buffer_rsrc(rbase, 0, wide ? rbytes * 4u : 0u, 0x00020000);
-                const __amdgpu_buffer_rsrc_t r16 = __builtin_amdgcn_make_buffer_rsrc(rbase, 0, wide ? 0u : rbytes * 2u, 0x00020000);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int n = item.n0 + place.wn * 128 + half * 64 + lane % 16 * 4;
-                    lds_handover();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f32x4 v;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) v[c] = sum_of(acc[half * 4 + i][j][c]) * ahead.xs[j];
-                        // (a row's 16-byte pieces XOR-swizzled with the row)
-                        *reinterpret_cast<f32x4 *>(place.patch + place.fr * 256 + (((i * 4 + place.oct) ^ place.fr) << 4)) = v;
-                    }
-                    if (j == 0 && half == 0) landed();
-                    lds_handover();
-                    MOE_SB();
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int row = it * 4 + in_row, at = n < a.N ? row * a.N + n : 0x1ffffff0;
-                        const f32x4 s = *reinterpret_cast<const f32x4 *>(place.patch + row * 256 + ((lane % 16 ^ row) << 4));
-                        const u32x4 rw = __builtin_amdgcn_raw_buffer_load_b128(r32, at * 4, 0, 0);
-                        const u32x2 rh = __builtin_amdgcn_raw_buffer_load_b64(r16, at * 2, 0, 0);
-                        float v[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            v[c] = activate<ERF>(form, __builtin_fmaf(s[c], ahead.ws[half][c], ahead.bias[half][c]));
-                            v[c] += __uint_as_float(rw[c]) + (a.res == kF16 ? f16_of(rh[c / 2], c % 2) : b16_of(rh[c / 2], c % 2));
-                        }
-                        if constexpr (Y32) {
-                            const u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                            __builtin_amdgcn_raw_buffer_store_b128(o, ry, at * 4, 0, 0);
-                        } else {
-                            const u32x2 h = {pack_16(kF16, v[0], v[1]), pack_16(kF16, v[2], v[3])};
-                            const u32x2 b = {pack_16(kB16, v[0], v[1]), pack_16(kB16, v[2], v[3])};
-                            __builtin_amdgcn_raw_buffer_store_b64(a.type == kF16 ? h : b, ry, at * 2, 0, 0);
-                        }
-                        MOE_SB();
-                    }
-                }
-            }
-        });
-}
-
-// The block's first projections: acc[2 p] and acc[2 p + 1] of a lane are gate and value of the same four columns.
-template <bool ERF, bool KTAIL, int BM>
-__global__ __launch_bounds__(256, 1) void q8_gated_run_kernel(Q8Args a)
-{
-    constexpr int TM = W4Place<BM>::TM;
-    const Tiles<BM, 256> items(a.offsets, a.E, a.tiles);
-    const ActForm form(a.act);
-    struct Scales {
-        float xs[TM];
-        float gs[4][4], us[4][4];
-    };
-    w4_run<kI8Operands, KTAIL, BM, 0, true>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, a.row_src, a.row_div, a.a_rows,
-        [&](const WorkItem &item, int wn, int oct) {
-            Scales c;
-            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
-            const int32_t *src = a.row_src != nullptr ? a.row_src : a.offsets;
-            const int div = a.row_src != nullptr ? a.row_div : 1;
-#pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                const int row = min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1);
-                const int from = src[a.row_src != nullptr ? row : 0] / div;
-                c.xs[j] = a.xs[a.row_src != nullptr ? from : row];
-            }
-            const float *gs = a.ws + static_cast<size_t>(item.expert) * a.N;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int n = min(item.n0 / 2 + wn * 64 + p * 16 + oct * 4, a.h - 4);      // (h is a multiple of 16)
-                const f32x4 g = *reinterpret_cast<const f32x4 *>(gs + n), u = *reinterpret_cast<const f32x4 *>(gs + a.h + n);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    c.gs[p][e] = g[e];
-                    c.us[p][e] = u[e];
-                }
-            }
-            return c;
-        },
-        [&](auto &acc, const Scales &ahead, const WorkItem &item, const W4Place<BM> &place, auto landed) {
-            const int col = item.n0 / 2 + place.wn * 64 + place.lane % 8 * 8;
-#pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                const int row0 = item.row0 + place.wm * (BM / 2) + j * 16;
-                lds_handover();
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    f16x4 o;
+                for (int it = 0; it < 8; ++it) {
+                    const int row = (part * 8 + it) * 4 + lane / 16;
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + col * 4);
+                    float v[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const float g = sum_of(acc[2 * p][j][c]) * ahead.xs[j] * ahead.gs[p][c];
-                        const float u = sum_of(acc[2 * p + 1][j][c]) * ahead.xs[j] * ahead.us[p][c];
-                        o[c] = static_cast<_Float16>(activate<ERF>(form, g) * u);
+                        v[c] = activate<ACT>(form, __builtin_fmaf(s[c], cs[c], cb[c]));
+                        if (a.r != nullptr) v[c] += residual(a, r[it], c);
                     }
-                    *reinterpret_cast<f16x4 *>(place.at(p, 0)) = o;
-                    MOE_SB();
+                    if (row < left) store_output(a, (row0 + row) * N + n, v);
                 }
-                if (j == 0) landed();
-                // 16 rows of 64 columns, eight to a row's line
-                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-                    static_cast<uint16_t *>(a.y) + static_cast<size_t>(row0) * a.h, 0,
-                    static_cast<unsigned>(min(max(item.row1 - row0, 0), 16)) * static_cast<unsigned>(a.h) * 2u, 0x00020000);
-                lds_handover();
-                MOE_SB();
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {
-                    const int row = it * 8 + place.lane / 8;
-                    const u32x4 q = *reinterpret_cast<const u32x4 *>(place.patch + row * 256 + ((place.lane % 8 ^ row) << 4));
-                    __builtin_amdgcn_raw_buffer_store_b128(q, rs, col < a.h ? (row * a.h + col) * 2 : 0x7ff00000, 0, 0);
-                }
-                MOE_SB();
             }
-        },
-        a.h);
+        } else {
+            if (n >= width) return;
+            for (int row = 0; row < min(left, 64); row += 8) {
+                uint32_t r[8][1];
+                if (a.r != nullptr) {
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) load_residual(a, (row0 + min(row + it, left - 1)) * N + n, r[it]);
+                }
+#pragma unroll
+                for (int it = 0; it < 8; ++it) {
+                    const float s = *reinterpret_cast<const float *>(patch + (row + it) * PITCH + col * 4);
+                    float v[1] = {activate<ACT>(form, __builtin_fmaf(s, cs[0], cb[0]))};
+                    if (a.r != nullptr) v[0] += residual(a, r[it], 0);
+                    if (row + it < left) store_output(a, (row0 + row + it) * N + n, v);
+                }
+            }
+        }
+    });
 }
 
 // ---------------------------------------------------------------- dispatch
@@ -689,17 +413,6 @@ __global__ __launch_bounds__(256) void q8_scatter_kernel(const u32x4 *__restrict
 }
 
 // ---------------------------------------------------------------- host side
-// a kernel of 256 threads that needs more LDS than a launch gets unasked
-template <auto KERNEL>
-void launch_product_kernel(const Q8Args &a, int64_t blocks, size_t lds, int stage, hipStream_t st)
-{
-    static PerDeviceOnce once;
-    once.raise_lds(reinterpret_cast<const void *>(KERNEL), static_cast<int>(lds));
-    hipEvent_t t0 = nullptr, t1 = nullptr;
-    if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
-    hipExtLaunchKernelGGL(KERNEL, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, st, t0, t1, 0, a);
-}
-
 void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scale, const int32_t *rows_end, hipStream_t st)
 {
     using std::integral_constant;
@@ -732,7 +445,8 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     if (few_long_tiles(rows, E, columns, K)) return {128, 128, true};
     GemmPlan gp;
     choose_w4_tile(std::max<int64_t>(rows, 256), E, columns, K, &gp);
-    return {gp.bm, gp.bn, false};
+    if (gp.bm == 256) return {256, 256, false};
+    return {128, 128, false};
 }
 
 template <bool PAIR>
@@ -759,30 +473,16 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
         else stream(std::integral_constant<int, 2>{});
         return MOE_OK;
     }
+    if (plan.bn == 256) {
+        launch_q8_run(PAIR, a, entries, stage, st);
+        return MOE_OK;
+    }
     auto with_tail = [&](auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
-        if (plan.bn == 128) {
-            if (plan.deep) launch_product_kernel<q8_tile_kernel<PAIR, TAIL, true>>(a, entries, kW4Lds, stage, st);
-            else launch_product_kernel<q8_tile_kernel<PAIR, TAIL, false>>(a, entries, w4_lds(128, 128), stage, st);
-            return;
-        }
-        a.share = w4_run_share(plan.bm, a.K);
-        const int blocks = w4_run_blocks(a.entries, a.share);
-        auto with_rows = [&](auto bm) {
-            constexpr int BM = decltype(bm)::value;
-            auto with_act = [&](auto erf) {
-                constexpr bool ERF = decltype(erf)::value;
-                if constexpr (PAIR) launch_product_kernel<q8_gated_run_kernel<ERF, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
-                else if (a.type == kF32) launch_product_kernel<q8_run_kernel<ERF, true, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
-                else launch_product_kernel<q8_run_kernel<ERF, false, TAIL, BM>>(a, blocks, kW4RunLds, stage, st);
-            };
-            if (a.act == MOE_ACT_GELU_ERF) with_act(std::true_type{});
-            else with_act(std::false_type{});
-        };
-        if (plan.bm == 256) with_rows(std::integral_constant<int, 256>{});
-        else with_rows(std::integral_constant<int, 128>{});
+        if (plan.deep) launch_product_kernel<q8_tile_kernel<PAIR, TAIL, true>>(a, entries, kW4Lds, stage, st);
+        else launch_product_kernel<q8_tile_kernel<PAIR, TAIL, false>>(a, entries, w4_lds(128, 128), stage, st);
     };
-    if (a.K % 64 == 0 && (plan.bn != 256 || a.K >= 256)) with_tail(std::false_type{});
+    if (a.K % 64 == 0) with_tail(std::false_type{});
     else with_tail(std::true_type{});
     return MOE_OK;
 }
@@ -872,8 +572,8 @@ moe_status moe_q8_linear(const moe_q8_shape *s, const void *x, const float *x_sc
         set_error("moe_q8_linear: R, E, N, K must be >= 1, res and y 0 (fp32), 1 (bf16) or 2 (fp16), act a moe_act");
         return MOE_EINVAL;
     }
-    if (s->E > kMaxExperts || s->N >= 1 << 22 || s->K % 16 != 0 || s->K > kMaxDepth || s->R >= 1 << 30) {
-        set_error("moe_q8_linear: at most %d experts, N below 2^22, K a multiple of 16 up to %d, R below 2^30", kMaxExperts, kMaxDepth);
+    if (s->E > kMaxExperts || s->N >= 1 << 21 || s->K % 16 != 0 || s->K > kMaxDepth || s->R >= 1 << 30) {
+        set_error("moe_q8_linear: at most %d experts, N below 2^21, K a multiple of 16 up to %d, R below 2^30", kMaxExperts, kMaxDepth);
         return MOE_EUNSUPPORTED;
     }
     MOE_REQUIRE_PTR(x);

@@ -1,0 +1,25 @@
+// A product of rows and weights in 8 bits: its arguments, and the launch of the kernel for large tiles.
+#pragma once
+
+#include "common.h"
+
+namespace moe {
+
+// K: pairs of codes, the "16-bit values" of the expert FFN's loops.  Tiles are found from the experts' offsets.
+struct Q8Args {
+    const uint16_t *x, *w;
+    const float *xs, *ws, *bias;
+    const void *r;
+    void *y;
+    const int32_t *offsets, *row_src;      // row_src: the first product takes row row_src[i] / row_div, of a_rows
+    int row_div, a_rows;
+    int E, N, K;                           // of a pair of projections N = 2 h
+    int h;                                 // else 0
+    int act, res, type;
+    int tiles, entries, share;
+};
+
+// q8_run.hip: tiles of 256 x 256; pair: the first projections, else the linear map, N a multiple of 4.
+void launch_q8_run(bool pair, const Q8Args &a, int64_t blocks, int stage, hipStream_t st);
+
+}  // namespace moe

@@ -1,0 +1,176 @@
+// What the kernels of 8-bit products share.  Included inside the translation unit's own namespace.
+#pragma once
+
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+#include "gemm_w4.h"
+
+enum { kF32 = 0, kB16 = 1, kF16 = 2 };       // element types as in moe_q8_shape
+
+// one of the two fp16 (bf16) values of a dword.  (By value: a bit cast of a vector's element casts its first one.)
+__device__ __forceinline__ float f16_of(uint32_t w, int i) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[i]); }
+__device__ __forceinline__ float b16_of(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
+
+__device__ __forceinline__ uint32_t pack_16(int type, float lo, float hi)
+{
+    if (type == kF16) {
+        f16x2 h;
+        h[0] = static_cast<_Float16>(lo);
+        h[1] = static_cast<_Float16>(hi);
+        return __builtin_bit_cast(uint32_t, h);
+    }
+    bf16x2 b;
+    b[0] = static_cast<__bf16>(lo);
+    b[1] = static_cast<__bf16>(hi);
+    return __builtin_bit_cast(uint32_t, b);
+}
+
+// acc columns of a tile: BN packed ones of a pair of projections, sixteen of the first and the same sixteen of the second in turn
+__host__ __device__ inline int tile_columns(const Q8Args &a) { return a.h != 0 ? gated_packed_columns(a.h) : a.N; }
+
+// The tile of block entry b: a panel of kPanel tiles' rows of an expert column by column, then the next; an eighth of all tiles for
+// each XCD.  A wavefront holds the experts' row tiles and their running sum, a lane each.
+constexpr int kPanel = 8;
+template <int BM, int BN>
+struct Tiles {
+    int first, end, row_tiles, sum, per_xcd, total, tiles;
+    __device__ __forceinline__ Tiles(const int32_t *__restrict__ offsets, int E, int column_tiles) : tiles(column_tiles)
+    {
+        const int lane = lane_id(), e = min(lane, E - 1);
+        first = offsets[e];
+        end = lane < E ? offsets[e + 1] : first;
+        row_tiles = end > first ? (end - first + BM - 1) / BM : 0;
+        sum = row_tiles * tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        total = __builtin_amdgcn_readlane(sum, kWave - 1);
+        per_xcd = (total + 7) / 8;
+    }
+    __device__ __forceinline__ WorkItem operator[](int b) const
+    {
+        const int slot = b / 8, index = b % 8 * per_xcd + slot;
+        if (slot >= per_xcd || index >= total) return WorkItem{-1, 0, 0, 0};
+        const int e = __builtin_amdgcn_readfirstlane(__popcll(__ballot(sum <= index)));
+        const int mt = __builtin_amdgcn_readlane(row_tiles, e);
+        const int within = index - (__builtin_amdgcn_readlane(sum, e) - mt * tiles);
+        const int panel = within / (kPanel * tiles), rest = within - panel * (kPanel * tiles), high = min(kPanel, mt - panel * kPanel);
+        const int column = rest / high, row0 = __builtin_amdgcn_readlane(first, e) + (panel * kPanel + rest - column * high) * BM;
+        return WorkItem{e, row0, min(row0 + BM, __builtin_amdgcn_readlane(end, e)), column * BN};
+    }
+};
+inline int64_t tile_entries(int64_t rows, int E, int bm, int tiles)
+{
+    return static_cast<int64_t>(align_up((static_cast<size_t>(rows) / bm + std::min<int64_t>(rows, E)) * tiles, 8));
+}
+
+// All activations but the erf form of the GeLU as factor * v / (1 + 2^-(v (a + b v^2))): silu; its tanh form; relu, whose a is so large
+// that the quotient is 1 or 0 from |v| = 1e-36 on; and identity, 2 v / 2.  An epilogue that holds accumulators takes no branch, and a
+// kernel for each activation is five times the code.  (v^2 is bounded so that 0 v^2 is 0.)
+struct ActForm {
+    float a, b, factor;
+    __device__ __forceinline__ explicit ActForm(int act)
+    {
+        a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : act == MOE_ACT_RELU ? 1e38f : 0.0f;
+        b = act == MOE_ACT_GELU_TANH ? 0.10294324f : 0.0f;
+        factor = act == MOE_ACT_IDENTITY ? 2.0f : 1.0f;
+    }
+    __device__ __forceinline__ float operator()(float v) const
+    {
+        const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
+        const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
+        return v * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
+    }
+};
+// The activation in every kernel (FORM: by its form), so that all give the same bits.
+enum { kForm = 8 };
+template <int ACT>
+__device__ __forceinline__ float activate(const ActForm &form, float v)
+{
+    if constexpr (ACT == kForm) return form(v);
+    else return gate_value<ACT>(v);
+}
+// f(integral_constant of GELU_ERF, of `plain`, or of kForm)
+template <int PLAIN, typename F>
+__host__ __device__ __forceinline__ void with_activation(int act, F f)
+{
+    if (act == MOE_ACT_GELU_ERF) f(std::integral_constant<int, MOE_ACT_GELU_ERF>{});
+    else if (act == PLAIN) f(std::integral_constant<int, PLAIN>{});
+    else f(std::integral_constant<int, kForm>{});
+}
+__device__ __forceinline__ float sum_of(float bits) { return static_cast<float>(__builtin_bit_cast(int, bits)); }
+
+// N consecutive values of r, and of y, from `at` on: one or four (at a multiple of four)
+template <int N>
+__device__ __forceinline__ void load_residual(const Q8Args &a, size_t at, uint32_t (&raw)[N])
+{
+    if (a.res == kF32) {
+        if constexpr (N == 4) {
+            const u32x4 r = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.r) + at);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) raw[c] = r[c];
+        } else {
+            raw[0] = static_cast<const uint32_t *>(a.r)[at];
+        }
+    } else if constexpr (N == 4) {
+        const u32x2 r = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.r) + at);
+        raw[0] = r[0], raw[1] = r[1];
+    } else {
+        raw[0] = static_cast<const uint16_t *>(a.r)[at];
+    }
+}
+template <int N>
+__device__ __forceinline__ float residual(const Q8Args &a, const uint32_t (&raw)[N], int c)
+{
+    if (a.res == kF32) return __uint_as_float(raw[c]);
+    return a.res == kF16 ? f16_of(raw[c / 2], c % 2) : b16_of(raw[c / 2], c % 2);
+}
+template <int N>
+__device__ __forceinline__ void store_output(const Q8Args &a, size_t at, const float (&v)[N])
+{
+    if constexpr (N == 4) {
+        if (a.type == kF32)
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + at) = (f32x4){v[0], v[1], v[2], v[3]};
+        else
+            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + at) = (u32x2){pack_16(a.type, v[0], v[1]), pack_16(a.type, v[2], v[3])};
+    } else {
+        if (a.type == kF32) static_cast<float *>(a.y)[at] = v[0];
+        else static_cast<uint16_t *>(a.y)[at] = static_cast<uint16_t>(pack_16(a.type, v[0], 0.0f));
+    }
+}
+__device__ __forceinline__ void store_hidden(const Q8Args &a, size_t row, int n, const float (&v)[4])
+{
+    f16x4 o;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = static_cast<_Float16>(v[c]);
+    *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(a.y) + row * a.h + n) = o;
+}
+__device__ __forceinline__ float row_scale(const Q8Args &a, int row)
+{
+    return a.xs[a.row_src != nullptr ? a.row_src[row] / a.row_div : row];
+}
+// scales of columns n .. n + 3, of the last column past it
+__device__ __forceinline__ void column_scales(const float *__restrict__ p, int n, int N, float (&s)[4])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[c] = p[min(n + c, N - 1)];
+}
+
+// a kernel of 256 threads that needs more LDS than a launch gets unasked
+template <auto KERNEL>
+void launch_product_kernel(const Q8Args &a, int64_t blocks, size_t lds, int stage, hipStream_t st)
+{
+    static PerDeviceOnce once;
+    once.raise_lds(reinterpret_cast<const void *>(KERNEL), static_cast<int>(lds));
+    hipEvent_t t0 = nullptr, t1 = nullptr;
+    if (stage >= 0) prof_kernel_events(stage, &t0, &t1);
+    hipExtLaunchKernelGGL(KERNEL, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, st, t0, t1, 0, a);
+}

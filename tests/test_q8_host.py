@@ -24,7 +24,7 @@ def linear(args=None, **kw):
     (dict(R=0), 1, ">= 1"), (dict(E=0), 1, ">= 1"), (dict(N=0), 1, ">= 1"), (dict(K=0), 1, ">= 1"), (dict(R=-5), 1, ">= 1"),
     (dict(act_number=5), 1, "moe_act"), (dict(act_number=-1), 1, "moe_act"), (dict(res_number=3), 1, "res and y"),
     (dict(y_number=-1), 1, "res and y"), (dict(K=120), 2, "multiple of 16"), (dict(K=65552), 2, "65536"), (dict(E=65), 2, "at most 64"),
-    (dict(N=1 << 22), 2, "2^22"), (dict(R=1 << 30), 2, "2^30"), (dict(R=(1 << 30) - 1, N=(1 << 22) - 1), 2, "tiles"),
+    (dict(N=1 << 21), 2, "2^21"), (dict(R=1 << 30), 2, "2^30"), (dict(R=(1 << 30) - 1, N=(1 << 21) - 1), 2, "tiles"),
 ])
 def test_linear_refuses_bad_shapes(kw, status, frag):
     assert linear(**kw) == status and frag in moe.moe_last_error()
