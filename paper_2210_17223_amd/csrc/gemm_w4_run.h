@@ -29,18 +29,18 @@
 constexpr size_t kW4RunLds = 160 * 1024;
 // tiles of a block's share (a stage of 128 x 256 takes half as long as one of 256 x 256)
 inline int w4_run_share(int bm, int K) { return std::max(1, kRunStages * 256 / bm / std::max((K + 63) / 64, 4)); }
-// blocks of a launch: blocks 256 g .. 256 g + 255 take the entries from 256 g * share on, each every 256th
-inline int w4_run_blocks(int entries, int share)
+// blocks of a launch: blocks 256 g .. 256 g + 255 take the entries from 256 g * share on, each every 256th (units: how many run at once)
+inline int w4_run_blocks(int entries, int share, int units = kRunUnits)
 {
-    const int whole = (entries - 1) / (kRunUnits * share);
-    return whole * kRunUnits + std::min(entries - whole * kRunUnits * share, kRunUnits);
+    const int64_t whole = (entries - 1) / (static_cast<int64_t>(units) * share);
+    return static_cast<int>(whole * units + std::min<int64_t>(entries - whole * units * share, units));
 }
 
-template <int BM>
+template <int BM, int BN = 256>
 struct W4Place {                       // where a wavefront stands in its tile
     char *patch;                       // its quarter of the free LDS: UR rows of 256 bytes
     int lane, wm, wn, fr, oct;
-    static constexpr int UR = BM / 8, TM = BM / 32, TN = 8;
+    static constexpr int UR = BM / 8, TM = BM / 32, TN = BN / 32;
     // a lane's four values of column block i (16 columns) of a row block, as 16-bit values, the patch's 16 rows `part`
     __device__ __forceinline__ char *at(int i, int part) const
     {
@@ -80,17 +80,18 @@ struct W4Place {                       // where a wavefront stands in its tile
 // items: the list, or what finds entry b by items[b].  F16 may be kI8Operands (K is then half the depth); PAIR: the tile's columns
 // are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).  Of 8-bit operands, whose tiles have half
 // the stages and more to prepare (scales of rows and columns), prepare is called in front of the tile's first stage instead of behind its last.
-template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, typename Items, typename Prepare, typename Epilogue>
+// BN: 256, or 128 with BM 128: the ring of five units of 16 KiB, two blocks to a compute unit, 4 KiB of LDS for a wavefront's way out.
+template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, int BN = 256, typename Items, typename Prepare, typename Epilogue>
 __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uint16_t *__restrict__ W,
                                        const Items &items, const int32_t *__restrict__ nitems, int entries, int share,
                                        int N, int K, const int32_t *__restrict__ row_src, int row_div, int a_rows,
                                        Prepare prepare, Epilogue epilogue, int pair_h = 0)
 {
-    constexpr int TM = BM / 32, TN = 8, BK = 64;
-    constexpr bool RING5 = BM == 256;
-    constexpr int A_UNIT = BM * 128, W_UNIT = 256 * 128;
+    constexpr int TM = BM / 32, TN = BN / 32, BK = 64;
+    constexpr bool RING5 = BM == BN;
+    constexpr int A_UNIT = BM * 128, W_UNIT = BN * 128;
     constexpr int AR = BM / 4;                    // rows of A that a wavefront loads
-    constexpr int stride = kRunUnits;
+    constexpr int stride = BN == 256 ? kRunUnits : 2 * kRunUnits;      // (blocks that run at once)
     int b = blockIdx.x / stride * stride * share + blockIdx.x % stride;
     const int stop = min(entries, b + share * stride);
     auto item_at = [&](int b) {
@@ -126,16 +127,16 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
     };
     auto weights_of = [&](const WorkItem &t) {
         const uint16_t *at = t.expert < 0 ? W : W + (static_cast<size_t>(t.expert) * N + (PAIR ? t.n0 / 2 : t.n0)) * K;
-        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(PAIR ? N - t.n0 / 2 : min(N - t.n0, 256));     // (a tile's: 256 K values fit)
+        const unsigned n = t.expert < 0 ? 0u : static_cast<unsigned>(PAIR ? N - t.n0 / 2 : min(N - t.n0, BN));     // (a tile's: 256 K values fit)
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(at), 0, n * static_cast<unsigned>(K) * 2u, 0x00020000);
     };
-    // load q of this wavefront's TM (TN) of a unit: rows wave * AR (64) + 8 q .. + 7, eight 16-byte pieces
+    // load q of this wavefront's TM (TN) of a unit: rows wave * AR (BN / 4) + 8 q .. + 7, eight 16-byte pieces
     // each; lane l lands at row l / 8, place l % 8, where piece place ^ (row / 2 % 8) belongs
     int w_src[TN], a_src[TM], a_next[TM];
     int first_col[2];                             // KTAIL: the piece's first column in its stage (q even / odd)
 #pragma unroll
     for (int q = 0; q < TN; ++q) {
-        const int r = wave * 64 + q * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
+        const int r = wave * (BN / 4) + q * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
         // (of a pair, columns past pair_h are of its other half or past it: not stored)
         w_src[q] = ((PAIR ? r / 32 * 16 + r % 16 + (r / 16 % 2) * pair_h : r) * K + piece * 8) * 2;
         if (q < 2) first_col[q] = piece * 8;
@@ -262,7 +263,11 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         step(integral_constant<int, 0>{}, first, [&](auto mc) {
             constexpr int m = decltype(mc)::value;
             if constexpr (m < NR && m % 2 == 0) read(integral_constant<int, 1>{}, integral_constant<int, m / 2>{}, w0, a0);
-            if constexpr (m >= NR && m % A_GAP == 0 && !(ABL & 4)) load_a((m - NR) / A_GAP, uf, ka);
+            if constexpr (NR < TM * TN) {
+                if constexpr (m >= NR && m % A_GAP == 0 && !(ABL & 4)) load_a((m - NR) / A_GAP, uf, ka);
+            } else {
+                if constexpr (m % 4 == 1 && !(ABL & 4)) load_a(m / 4, uf, ka);
+            }
         });
         MOE_LGKM0();
         if (wait) MOE_VMCNT(RING5 ? TM : TM + TN);
@@ -319,8 +324,8 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         }
         int here = lane;               // (so that the epilogue's addresses are not kept through the stages)
         asm volatile("" : "+v"(here));
-        const W4Place<BM> place{lds + (RING5 ? uf : 3 * (A_UNIT + W_UNIT)) + wave * (W4Place<BM>::UR * 256), here, wm, wn,
-                                here & 15, here >> 4};
+        const W4Place<BM, BN> place{lds + (RING5 ? uf : 3 * (A_UNIT + W_UNIT)) + wave * (W4Place<BM, BN>::UR * 256), here, wm, wn,
+                                    here & 15, here >> 4};
         const auto &ahead = [&]() -> const auto & {
             if constexpr (EARLY) return early;
             else return late;

@@ -23,6 +23,7 @@ namespace moe {
 namespace {
 
 #include "q8_product_device.h"
+#include "gemm_w4_run.h"
 
 constexpr int kMaxDepth = 65536;             // values of a row
 
@@ -260,28 +261,31 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
     if constexpr (PAIR) {
         store_hidden(a, at, n, v[0]);
     } else if (a.N % 4 == 0) {
-        uint32_t r[4] = {0, 0, 0, 0};
-        if (a.r != nullptr) load_residual(a, at * a.N + n, r);
+        const WayOut<4> out(a, item.row0, item.row1, n);
+        typename WayOut<4>::Residual r;
+        out.ask(row, r);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[0][c] += a.r != nullptr ? residual(a, r, c) : 0.0f;
-        store_output(a, at * a.N + n, v[0]);
+        for (int c = 0; c < 4; ++c) v[0][c] += out.value(r, c);
+        out.leave(row, v[0]);
     } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            if (n + c >= a.N) return;
-            uint32_t r[1] = {0};
-            if (a.r != nullptr) load_residual(a, at * a.N + n + c, r);
-            const float u[1] = {v[0][c] + (a.r != nullptr ? residual(a, r, 0) : 0.0f)};
-            store_output(a, at * a.N + n + c, u);
+            const WayOut<1> out(a, item.row0, item.row1, n + c);
+            typename WayOut<1>::Residual r;
+            out.ask(row, r);
+            const float u[1] = {v[0][c] + out.value(r, 0)};
+            out.leave(row, u);
         }
     }
 }
 
-// ---------------------------------------------------------------- tiles of 128 x 128
-template <bool PAIR, bool KTAIL, bool DEEP>
-__global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
+// ---------------------------------------------------------------- tiles of 128 x 128, one for a block
+// Few rows and a long depth: five stages on their way, one block to a compute unit, bound by the weights' arrival.
+template <bool PAIR, bool KTAIL>
+__global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 {
     constexpr int BM = 128, BN = 128;
+    constexpr bool DEEP = true;
     constexpr int F16 = kI8Operands;
     constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = PAIR;
     constexpr int tile_pitch = 0, pair_at = 0;
@@ -332,6 +336,34 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
         }
     lds_handover();
     const ActForm form(a.act);
+    // sixteen rows' residuals are on their way together
+    auto leave_sums = [&](auto perc, auto actc) {
+        constexpr int PER = decltype(perc)::value, ROWS = PER;
+        const WayOut<PER> out(a, item.row0 + wm * 64, item.row1, n);
+        typename WayOut<PER>::Residual r[16 / ROWS];
+#pragma unroll 1
+        for (int row0 = 0; row0 < 64; row0 += 16) {
+            const int in = PER == 4 ? lane / 16 : 0;
+#pragma unroll
+            for (int it = 0; it < 16 / ROWS; ++it) out.ask(row0 + it * ROWS + in, r[it]);
+#pragma unroll
+            for (int it = 0; it < 16 / ROWS; ++it) {
+                const char *const at = patch + (row0 + it * ROWS + in) * PITCH + col * 4;
+                float v[PER];
+                if constexpr (PER == 4) {
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(at);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[c] = s[c];
+                } else {
+                    v[0] = *reinterpret_cast<const float *>(at);
+                }
+#pragma unroll
+                for (int c = 0; c < PER; ++c)
+                    v[c] = activate<decltype(actc)::value>(form, __builtin_fmaf(v[c], cs[c], cb[c])) + out.value(r[it], c);
+                out.leave(row0 + it * ROWS + in, v);
+            }
+        }
+    };
     const int left = rows - wm * 64;                      // of the wavefront's rows
     const size_t row0 = static_cast<size_t>(item.row0) + wm * 64;
     with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto actc) {
@@ -350,46 +382,159 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void q8_tile_kernel(Q8Args a)
                 if (row < left) store_hidden(a, row0 + row, n, v);
             }
         } else if (fours) {
-            if (n >= width) return;
-            // eight rows' residuals are on their way together
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                uint32_t r[8][4];
-                if (a.r != nullptr) {
-#pragma unroll
-                    for (int it = 0; it < 8; ++it) load_residual(a, (row0 + min((part * 8 + it) * 4 + lane / 16, max(left - 1, 0))) * N + n, r[it]);
-                }
-#pragma unroll
-                for (int it = 0; it < 8; ++it) {
-                    const int row = (part * 8 + it) * 4 + lane / 16;
-                    const f32x4 s = *reinterpret_cast<const f32x4 *>(patch + row * PITCH + col * 4);
-                    float v[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        v[c] = activate<ACT>(form, __builtin_fmaf(s[c], cs[c], cb[c]));
-                        if (a.r != nullptr) v[c] += residual(a, r[it], c);
-                    }
-                    if (row < left) store_output(a, (row0 + row) * N + n, v);
-                }
-            }
+            leave_sums(std::integral_constant<int, 4>{}, actc);
         } else {
-            if (n >= width) return;
-            for (int row = 0; row < min(left, 64); row += 8) {
-                uint32_t r[8][1];
-                if (a.r != nullptr) {
-#pragma unroll
-                    for (int it = 0; it < 8; ++it) load_residual(a, (row0 + min(row + it, left - 1)) * N + n, r[it]);
-                }
-#pragma unroll
-                for (int it = 0; it < 8; ++it) {
-                    const float s = *reinterpret_cast<const float *>(patch + (row + it) * PITCH + col * 4);
-                    float v[1] = {activate<ACT>(form, __builtin_fmaf(s, cs[0], cb[0]))};
-                    if (a.r != nullptr) v[0] += residual(a, r[it], 0);
-                    if (row + it < left) store_output(a, (row0 + row + it) * N + n, v);
-                }
-            }
+            leave_sums(std::integral_constant<int, 1>{}, actc);
         }
     });
+}
+
+// ---------------------------------------------------------------- tiles of 128 x 128, a share of them for a block
+// As the kernels of q8_run.hip, two blocks to a compute unit: products of a short depth, whose tiles are mostly beginnings and ends.
+// WHOLE: N is a multiple of four, and a lane takes four columns of a row on the way out; else one, of 64.
+template <bool WHOLE, bool KTAIL>
+__global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
+{
+    constexpr int BM = 128, BN = 128, TM = 4;
+    const Tiles<BM, BN> items(a.offsets, a.E, a.tiles);
+    const ActForm form(a.act);
+    struct Columns {
+        float xs[TM];
+        float ws[4], bias[4];
+    };
+    w4_run<kI8Operands, KTAIL, BM, 0, false, BN>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, nullptr, 1, 0,
+        [&](const WorkItem &item, int wn, int) {
+            Columns c;
+            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) c.xs[j] = a.xs[min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1)];
+            const size_t first = static_cast<size_t>(item.expert) * a.N;
+            const int n = item.n0 + wn * 64 + (WHOLE ? lane % 16 * 4 : lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c.bias[e] = 0.0f;
+            column_scales(a.ws + first, n, a.N, c.ws);
+            if (a.bias != nullptr) column_scales(a.bias + first, n, a.N, c.bias);
+            return c;
+        },
+        [&](auto &acc, const Columns &ahead, const WorkItem &item, const W4Place<BM, BN> &place, auto landed) {
+            const int lane = place.lane;
+            constexpr int PER = WHOLE ? 4 : 1, ROWS = PER;      // columns of a lane, rows of a step
+            const WayOut<PER> out(a, item.row0 + place.wm * (BM / 2), item.row1, item.n0 + place.wn * 64 + (WHOLE ? lane % 16 * 4 : lane));
+            const int in = WHOLE ? lane / 16 : 0;
+            // (sixteen rows' residuals are on their way from the step before, of single columns, which are more, from the step's start)
+            constexpr int TURNS = WHOLE ? 2 : 1;
+            typename WayOut<PER>::Residual r[TURNS][16 / ROWS];
+            auto ask = [&](int j) {
+#pragma unroll
+                for (int it = 0; it < 16 / ROWS; ++it) out.ask(j * 16 + it * ROWS + in, r[j % TURNS][it]);
+            };
+            if constexpr (WHOLE) ask(0);
+            static_for<TM>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                lds_handover();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 v;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[c] = sum_of(acc[i][j][c]) * ahead.xs[j];
+                    // (a row's 16-byte pieces XOR-swizzled with the row)
+                    *reinterpret_cast<f32x4 *>(place.patch + place.fr * 256 + (((i * 4 + place.oct) ^ place.fr) << 4)) = v;
+                }
+                MOE_SB();
+                if constexpr (j == 0) landed();
+                if constexpr (!WHOLE) ask(j);
+                else if constexpr (j + 1 < TM) ask(j + 1);
+                lds_handover();
+                MOE_SB();
+                with_activation<MOE_ACT_IDENTITY>(a.act, [&](auto act) {
+#pragma unroll
+                    for (int it = 0; it < 16 / ROWS; ++it) {
+                        const int row = it * ROWS + in;
+                        float v[PER];
+                        if constexpr (WHOLE) {
+                            const f32x4 s = *reinterpret_cast<const f32x4 *>(place.patch + row * 256 + ((lane % 16 ^ row) << 4));
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) v[c] = s[c];
+                        } else {
+                            v[0] = *reinterpret_cast<const float *>(place.patch + row * 256 + ((lane / 4 ^ row) << 4) + lane % 4 * 4);
+                        }
+#pragma unroll
+                        for (int c = 0; c < PER; ++c)
+                            v[c] = activate<decltype(act)::value>(form, __builtin_fmaf(v[c], ahead.ws[c], ahead.bias[c])) + out.value(r[j % TURNS][it], c);
+                        out.leave(j * 16 + row, v);
+                    }
+                });
+            });
+        });
+}
+
+// The block's first projections.
+template <bool KTAIL>
+__global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
+{
+    constexpr int BM = 128, BN = 128, TM = 4;
+    const Tiles<BM, BN> items(a.offsets, a.E, a.tiles);
+    const ActForm form(a.act);
+    struct Scales {
+        float xs[TM];
+        float gs[2][4], us[2][4];
+    };
+    w4_run<kI8Operands, KTAIL, BM, 0, true, BN>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, a.row_src, a.row_div, a.a_rows,
+        [&](const WorkItem &item, int wn, int oct) {
+            Scales c;
+            const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
+            int from[TM];
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                from[j] = min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1);
+                if (a.row_src != nullptr) from[j] = a.row_src[from[j]];
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j) c.xs[j] = a.xs[a.row_src != nullptr ? from[j] / a.row_div : from[j]];
+            const float *gs = a.ws + static_cast<size_t>(item.expert) * a.N;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int n = min(item.n0 / 2 + wn * 32 + p * 16 + oct * 4, a.h - 4);      // (h is a multiple of 16)
+                const f32x4 g = *reinterpret_cast<const f32x4 *>(gs + n), u = *reinterpret_cast<const f32x4 *>(gs + a.h + n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c.gs[p][e] = g[e];
+                    c.us[p][e] = u[e];
+                }
+            }
+            return c;
+        },
+        [&](auto &acc, const Scales &ahead, const WorkItem &item, const W4Place<BM, BN> &place, auto landed) {
+            const int lane = place.lane, row0 = item.row0 + place.wm * (BM / 2), left = item.row1 - row0;
+            const int col = item.n0 / 2 + place.wn * 32 + lane % 4 * 8;
+            static_for<TM>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                lds_handover();
+                with_activation<MOE_ACT_SILU>(a.act, [&](auto act) {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        f16x4 o;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float g = sum_of(acc[2 * p][j][c]) * ahead.xs[j] * ahead.gs[p][c];
+                            const float u = sum_of(acc[2 * p + 1][j][c]) * ahead.xs[j] * ahead.us[p][c];
+                            o[c] = static_cast<_Float16>(activate<decltype(act)::value>(form, g) * u);
+                        }
+                        *reinterpret_cast<f16x4 *>(place.at(p, 0)) = o;
+                    }
+                });
+                MOE_SB();
+                if constexpr (j == 0) landed();
+                lds_handover();
+                MOE_SB();
+                // 16 rows of 32 columns, four lanes to a row
+                const int row = lane / 4;
+                const u32x4 q = *reinterpret_cast<const u32x4 *>(place.patch + row * 256 + ((lane % 4 ^ row) << 4));
+                if (j * 16 + row < left && col < a.h)
+                    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.y) + static_cast<size_t>(row0 + j * 16 + row) * a.h + col) = q;
+            });
+        },
+        a.h);
 }
 
 // ---------------------------------------------------------------- dispatch
@@ -479,10 +624,19 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
     }
     auto with_tail = [&](auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
-        if (plan.deep) launch_product_kernel<q8_tile_kernel<PAIR, TAIL, true>>(a, entries, kW4Lds, stage, st);
-        else launch_product_kernel<q8_tile_kernel<PAIR, TAIL, false>>(a, entries, w4_lds(128, 128), stage, st);
+        if (plan.deep) {
+            launch_product_kernel<q8_tile_kernel<PAIR, TAIL>>(a, entries, kW4Lds, stage, st);
+            return;
+        }
+        constexpr int units = 2 * kRunUnits;
+        a.share = std::max(1, std::min(w4_run_share(128, a.K), parts_of(a.entries, units)));
+        const int blocks = w4_run_blocks(a.entries, a.share, units);
+        if constexpr (PAIR) launch_product_kernel<q8_gated_small_run_kernel<TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
+        else if (a.N % 4 == 0) launch_product_kernel<q8_small_run_kernel<true, TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
+        else launch_product_kernel<q8_small_run_kernel<false, TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
     };
-    if (a.K % 64 == 0) with_tail(std::false_type{});
+    // (the forms without a tail take their depth in whole stages, those that run on four of them at least)
+    if (a.K % 64 == 0 && (plan.deep || a.K >= 256)) with_tail(std::false_type{});
     else with_tail(std::true_type{});
     return MOE_OK;
 }

@@ -108,44 +108,66 @@ __host__ __device__ __forceinline__ void with_activation(int act, F f)
 }
 __device__ __forceinline__ float sum_of(float bits) { return static_cast<float>(__builtin_bit_cast(int, bits)); }
 
-// N consecutive values of r, and of y, from `at` on: one or four (at a multiple of four)
-template <int N>
-__device__ __forceinline__ void load_residual(const Q8Args &a, size_t at, uint32_t (&raw)[N])
-{
-    if (a.res == kF32) {
-        if constexpr (N == 4) {
-            const u32x4 r = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.r) + at);
+// The way of a wavefront's sums to y: rows row0 .. row1 - 1, of each a lane's columns n .. n + PER - 1 (four where N is a multiple of four,
+// else one).  No branch on types: each of r's and y's two sizes has a buffer resource of its own, the one that is not theirs is empty,
+// and what is asked of it or left to it takes no way to memory; so do a row past the last and a column past N.
+template <int PER>
+struct WayOut {
+    static_assert(PER == 1 || PER == 4, "one column, or four");
+    struct Residual {
+        uint32_t wide[PER], half[(PER + 1) / 2];
+    };
+    __amdgpu_buffer_rsrc_t y32, y16, r32, r16;
+    int pitch, column;
+    bool r_wide, r_f16, y_f16;
+    __device__ __forceinline__ WayOut(const Q8Args &a, int row0, int row1, int n) : pitch(a.N), column(n < a.N ? n : 0x1ff00000)
+    {
+        const size_t first = static_cast<size_t>(row0) * a.N;
+        const unsigned values = static_cast<unsigned>(max(row1 - row0, 0)) * static_cast<unsigned>(a.N);
+        auto resource = [&](const void *p, unsigned size, bool used) {
+            return __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(const_cast<void *>(p)) + first * size, 0, used ? values * size : 0u, 0x00020000);
+        };
+        r_wide = a.res == kF32;
+        r_f16 = a.res == kF16;
+        y_f16 = a.type == kF16;
+        y32 = resource(a.y, 4, a.type == kF32);
+        y16 = resource(a.y, 2, a.type != kF32);
+        r32 = resource(a.r, 4, a.r != nullptr && r_wide);
+        r16 = resource(a.r, 2, a.r != nullptr && !r_wide);
+    }
+    __device__ __forceinline__ int at(int row) const { return column == 0x1ff00000 ? column : row * pitch + column; }
+    __device__ __forceinline__ void ask(int row, Residual &r) const
+    {
+        if constexpr (PER == 4) {
+            const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r32, at(row) * 4, 0, 0);
+            const u32x2 h = __builtin_amdgcn_raw_buffer_load_b64(r16, at(row) * 2, 0, 0);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) raw[c] = r[c];
+            for (int c = 0; c < 4; ++c) r.wide[c] = w[c];
+            r.half[0] = h[0], r.half[1] = h[1];
         } else {
-            raw[0] = static_cast<const uint32_t *>(a.r)[at];
+            r.wide[0] = __builtin_amdgcn_raw_buffer_load_b32(r32, at(row) * 4, 0, 0);
+            r.half[0] = __builtin_amdgcn_raw_buffer_load_b16(r16, at(row) * 2, 0, 0);
         }
-    } else if constexpr (N == 4) {
-        const u32x2 r = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.r) + at);
-        raw[0] = r[0], raw[1] = r[1];
-    } else {
-        raw[0] = static_cast<const uint16_t *>(a.r)[at];
     }
-}
-template <int N>
-__device__ __forceinline__ float residual(const Q8Args &a, const uint32_t (&raw)[N], int c)
-{
-    if (a.res == kF32) return __uint_as_float(raw[c]);
-    return a.res == kF16 ? f16_of(raw[c / 2], c % 2) : b16_of(raw[c / 2], c % 2);
-}
-template <int N>
-__device__ __forceinline__ void store_output(const Q8Args &a, size_t at, const float (&v)[N])
-{
-    if constexpr (N == 4) {
-        if (a.type == kF32)
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + at) = (f32x4){v[0], v[1], v[2], v[3]};
-        else
-            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.y) + at) = (u32x2){pack_16(a.type, v[0], v[1]), pack_16(a.type, v[2], v[3])};
-    } else {
-        if (a.type == kF32) static_cast<float *>(a.y)[at] = v[0];
-        else static_cast<uint16_t *>(a.y)[at] = static_cast<uint16_t>(pack_16(a.type, v[0], 0.0f));
+    __device__ __forceinline__ float value(const Residual &r, int c) const
+    {
+        const float half = r_f16 ? f16_of(r.half[c / 2], c % 2) : b16_of(r.half[c / 2], c % 2);
+        return r_wide ? __uint_as_float(r.wide[c]) : half;
     }
-}
+    __device__ __forceinline__ void leave(int row, const float (&v)[PER]) const
+    {
+        if constexpr (PER == 4) {
+            const u32x4 w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            const u32x2 h = {pack_16(kF16, v[0], v[1]), pack_16(kF16, v[2], v[3])}, b = {pack_16(kB16, v[0], v[1]), pack_16(kB16, v[2], v[3])};
+            __builtin_amdgcn_raw_buffer_store_b128(w, y32, at(row) * 4, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b64(y_f16 ? h : b, y16, at(row) * 2, 0, 0);
+        } else {
+            const uint16_t h = static_cast<uint16_t>(y_f16 ? pack_16(kF16, v[0], 0.0f) : pack_16(kB16, v[0], 0.0f));
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), y32, at(row) * 4, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b16(h, y16, at(row) * 2, 0, 0);
+        }
+    }
+};
 __device__ __forceinline__ void store_hidden(const Q8Args &a, size_t row, int n, const float (&v)[4])
 {
     f16x4 o;
