@@ -587,7 +587,7 @@ struct Q8Plan {
 Q8Plan plan_product(int64_t rows, int E, int columns, int K)
 {
     if (rows <= 32ll * E && rows * ((columns + 127) / 128) <= 4000) return {rows <= 16ll * E ? 16 : 32, 0, false};
-    if (few_long_tiles(rows, E, columns, K)) return {128, 128, true};
+    if (K >= 320 && (rows / 128 + E) * ((columns + 127) / 128) <= 256) return {128, 128, true};
     GemmPlan gp;
     choose_w4_tile(std::max<int64_t>(rows, 256), E, columns, K, &gp);
     if (gp.bm == 256) return {256, 256, false};
@@ -609,9 +609,8 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
     }
     a.entries = static_cast<int>(entries);
     if (plan.bm <= 32) {
-        constexpr int PD = 4;
         auto stream = [&](auto rt) {
-            constexpr int RT = decltype(rt)::value;
+            constexpr int RT = decltype(rt)::value, PD = PAIR ? (RT == 1 ? 2 : 2) : RT == 1 ? 3 : 2;
             launch_product_kernel<q8_stream_kernel<PAIR, RT, PD>>(a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048, stage, st);
         };
         if (plan.bm == 16) stream(std::integral_constant<int, 1>{});
