@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256, BM + BN == 256 && !DEEP ? 2 : 1) void bwd_gemm
     constexpr bool F16 = false;
     const int32_t *const row_src = nullptr;      // packed rows
     constexpr int row_div = 1, a_rows = 0;
-    constexpr bool TILE_IN = EPI == 2, TILE_PAIR = false, W_PAIR = false;
+    constexpr bool TILE_IN = EPI == 2, TILE_PAIR = false, W_PAIR = false, W_ONCE = false;
     constexpr int pair_at = 0, pair_h = 0;
     const int tile_pitch = N;
     const uint16_t *const tile_in = reinterpret_cast<const uint16_t *>(Pbuf);

@@ -624,7 +624,7 @@ __device__ __forceinline__ void w4_gemm_tile(
     const int32_t *__restrict__ row_src, int row_div, int a_rows)
 {
     constexpr int BM = 128, BN = 128;
-    constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = false;
+    constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = false, W_ONCE = false;
     constexpr int tile_pitch = 0, pair_at = 0, pair_h = 0;
     const uint16_t *const tile_in = nullptr;
 #include "gemm_w4_body.inc"

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void gated_tile_kernel(
     const WorkItem *__restrict__ items, int N, int K, int h)
 {
     constexpr int BM = 128, BN = 128;
-    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false, W_PAIR = false;
+    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false, W_PAIR = false, W_ONCE = false;
     constexpr int tile_pitch = 0, pair_at = 0, row_div = 1, a_rows = 0, pair_h = 0;
     const uint16_t *const tile_in = nullptr;
     const int32_t *const row_src = nullptr;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(256, BM == 128 ? 2 : 1) void gated_dh_kernel(
     const WorkItem *__restrict__ items, int N, int K)
 {
     constexpr int BN = BM;
-    constexpr bool F16 = false, TILE_IN = true, TILE_PAIR = true, DEEP = false, W_PAIR = false;
+    constexpr bool F16 = false, TILE_IN = true, TILE_PAIR = true, DEEP = false, W_PAIR = false, W_ONCE = false;
     constexpr int row_div = 1, a_rows = 0, pair_h = 0;
     const int32_t *const row_src = nullptr;
     const uint16_t *const tile_in = pre;
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(256, DEEP ? 1 : 2) void rows_bf16_tile_kernel(
     int N, int K)
 {
     constexpr int BM = 128, BN = 128;
-    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false, W_PAIR = false;
+    constexpr bool F16 = false, TILE_IN = false, TILE_PAIR = false, W_PAIR = false, W_ONCE = false;
     constexpr int tile_pitch = 0, pair_at = 0, row_div = 1, a_rows = 0, pair_h = 0;
     const uint16_t *const tile_in = nullptr;
     const int32_t *const row_src = nullptr;

@@ -81,7 +81,10 @@ struct W4Place {                       // where a wavefront stands in its tile
 // are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).  Of 8-bit operands, whose tiles have half
 // the stages and more to prepare (scales of rows and columns), prepare is called in front of the tile's first stage instead of behind its last.
 // BN: 256, or 128 with BM 128: the ring of five units of 16 KiB, two blocks to a compute unit, 4 KiB of LDS for a wavefront's way out.
-template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, int BN = 256, typename Items, typename Prepare, typename Epilogue>
+// ONCE: few rows, whose weights are read once: past the caches' lines, and from another place of the depth in every block (of
+// whole numbers, whose sums are exact in any order): rows of weights are often a power of two bytes apart, and blocks that walk them in step
+// ask few of the memory channels at a time.  Else 8-bit operands' blocks do so by their XCD, whose L2 they share.
+template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, int BN = 256, bool ONCE = false, typename Items, typename Prepare, typename Epilogue>
 __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uint16_t *__restrict__ W,
                                        const Items &items, const int32_t *__restrict__ nitems, int entries, int share,
                                        int N, int K, const int32_t *__restrict__ row_src, int row_div, int a_rows,
@@ -167,8 +170,17 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         if constexpr (KTAIL) return k * BK + first_col[q & 1] < K ? src : 0x7ffffff0;
         else return src;
     };
-    auto load_a = [&](int q, int unit, int k) { load_to_lds(rsa, piece_of(a_src[q], q, k), a_dest + unit + q * 1024, k * (BK * 2)); };
-    auto load_w = [&](int q, int unit, int k) { load_to_lds(rsw, piece_of(w_src[q], q, k), w_dest + unit + q * 1024, k * (BK * 2)); };
+    constexpr bool TURNED = F16 == kI8Operands;
+    const int k_first = __builtin_amdgcn_readfirstlane(
+        !TURNED || row_src != nullptr ? 0 : ONCE ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(KT)) : static_cast<int>(blockIdx.x % 8u) * KT / 8);
+    auto turned = [&](int k) {
+        if constexpr (TURNED) return k + k_first < KT ? k + k_first : k + k_first - KT;
+        else return k;
+    };
+    auto load_a = [&](int q, int unit, int k) { load_to_lds(rsa, piece_of(a_src[q], q, turned(k)), a_dest + unit + q * 1024, turned(k) * (BK * 2)); };
+    auto load_w = [&](int q, int unit, int k) {
+        load_to_lds_as<ONCE>(rsw, piece_of(w_src[q], q, turned(k)), w_dest + unit + q * 1024, turned(k) * (BK * 2));
+    };
 
     // RING5: A and W of this stage, A and W of the next, and the free unit; else the A and W units of
     // this stage, the next and the one after it (uf: its A unit)

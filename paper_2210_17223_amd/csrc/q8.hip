@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restri
 // Four wavefronts share out the depth of a tile of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes; each
 // takes its stages through LDS of its own, PD of them on their way, so nothing is waited for but its own loads; the whole
 // numbers are added up through LDS at the end.
-template <bool PAIR, int RT, int PD>
+template <bool PAIR, int RT, int PD, bool ONCE>
 __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
 {
     constexpr int NT = PAIR ? 2 : 1, WAVES = 4, STAGE = (NT + RT) * 2048, LOADS = (NT + RT) * 2;
@@ -178,8 +178,8 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
         const bool past0 = s >= s1 || k + piece[0] * 16 >= static_cast<int>(pitch), past1 = s >= s1 || k + piece[1] * 16 >= static_cast<int>(pitch);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            load_to_lds(rsw[t], past0 ? 0x7ffffff0 : wsrc[0], at + t * 2048, k);
-            load_to_lds(rsw[t], past1 ? 0x7ffffff0 : wsrc[1], at + t * 2048 + 1024, k);
+            load_to_lds_as<ONCE>(rsw[t], past0 ? 0x7ffffff0 : wsrc[0], at + t * 2048, k);
+            load_to_lds_as<ONCE>(rsw[t], past1 ? 0x7ffffff0 : wsrc[1], at + t * 2048 + 1024, k);
         }
 #pragma unroll
         for (int q = 0; q < 2 * RT; ++q)
@@ -281,13 +281,13 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
 
 // ---------------------------------------------------------------- tiles of 128 x 128, one for a block
 // Few rows and a long depth: five stages on their way, one block to a compute unit, bound by the weights' arrival.
-template <bool PAIR, bool KTAIL>
+template <bool PAIR, bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 {
     constexpr int BM = 128, BN = 128;
     constexpr bool DEEP = true;
     constexpr int F16 = kI8Operands;
-    constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = PAIR;
+    constexpr bool TILE_IN = false, TILE_PAIR = false, W_PAIR = PAIR, W_ONCE = ONCE;
     constexpr int tile_pitch = 0, pair_at = 0;
     const uint16_t *const tile_in = nullptr;
     const uint16_t *const A = a.x, *const W = a.w;
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 // ---------------------------------------------------------------- tiles of 128 x 128, a share of them for a block
 // As the kernels of q8_run.hip, two blocks to a compute unit: products of a short depth, whose tiles are mostly beginnings and ends.
 // WHOLE: N is a multiple of four, and a lane takes four columns of a row on the way out; else one, of 64.
-template <bool WHOLE, bool KTAIL>
+template <bool WHOLE, bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
 {
     constexpr int BM = 128, BN = 128, TM = 4;
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
         float xs[TM];
         float ws[4], bias[4];
     };
-    w4_run<kI8Operands, KTAIL, BM, 0, false, BN>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, nullptr, 1, 0,
+    w4_run<kI8Operands, KTAIL, BM, 0, false, BN, ONCE>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, nullptr, 1, 0,
         [&](const WorkItem &item, int wn, int) {
             Columns c;
             const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
@@ -469,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
 }
 
 // The block's first projections.
-template <bool KTAIL>
+template <bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
 {
     constexpr int BM = 128, BN = 128, TM = 4;
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
         float xs[TM];
         float gs[2][4], us[2][4];
     };
-    w4_run<kI8Operands, KTAIL, BM, 0, true, BN>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, a.row_src, a.row_div, a.a_rows,
+    w4_run<kI8Operands, KTAIL, BM, 0, true, BN, ONCE>(a.x, a.w, items, nullptr, a.entries, a.share, a.N, a.K, a.row_src, a.row_div, a.a_rows,
         [&](const WorkItem &item, int wn, int oct) {
             Scales c;
             const int lane = lane_id(), wm = threadIdx.x / kWave & 1;
@@ -594,6 +594,8 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     return {128, 128, false};
 }
 
+constexpr int64_t kKeptBytes = 64 << 20;
+
 template <bool PAIR>
 moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
 {
@@ -608,35 +610,44 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
         return MOE_EUNSUPPORTED;
     }
     a.entries = static_cast<int>(entries);
+    // Weights that one tile of rows reads, and more of them than stay in the last level of cache until the next call.
+    const bool once = rows <= static_cast<int64_t>(plan.bm) * a.E && 2ll * a.E * a.N * a.K > kKeptBytes;
     if (plan.bm <= 32) {
-        auto stream = [&](auto rt) {
-            constexpr int RT = decltype(rt)::value, PD = PAIR ? (RT == 1 ? 2 : 2) : RT == 1 ? 3 : 2;
-            launch_product_kernel<q8_stream_kernel<PAIR, RT, PD>>(a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048, stage, st);
+        auto stream = [&](auto rt, auto once) {
+            constexpr int RT = decltype(rt)::value, PD = PAIR ? 2 : RT == 1 ? 3 : 2;
+            launch_product_kernel<q8_stream_kernel<PAIR, RT, PD, decltype(once)::value>>(a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048,
+                                                                                        stage, st);
         };
-        if (plan.bm == 16) stream(std::integral_constant<int, 1>{});
-        else stream(std::integral_constant<int, 2>{});
+        using std::integral_constant;
+        if (plan.bm == 16 && once) stream(integral_constant<int, 1>{}, std::true_type{});
+        else if (plan.bm == 16) stream(integral_constant<int, 1>{}, std::false_type{});
+        else if (once) stream(integral_constant<int, 2>{}, std::true_type{});
+        else stream(integral_constant<int, 2>{}, std::false_type{});
         return MOE_OK;
     }
     if (plan.bn == 256) {
         launch_q8_run(PAIR, a, entries, stage, st);
         return MOE_OK;
     }
-    auto with_tail = [&](auto tail) {
-        constexpr bool TAIL = decltype(tail)::value;
+    auto with_tail = [&](auto tail, auto oncec) {
+        constexpr bool TAIL = decltype(tail)::value, ONCE = decltype(oncec)::value;
         if (plan.deep) {
-            launch_product_kernel<q8_tile_kernel<PAIR, TAIL>>(a, entries, kW4Lds, stage, st);
+            launch_product_kernel<q8_tile_kernel<PAIR, TAIL, ONCE>>(a, entries, kW4Lds, stage, st);
             return;
         }
         constexpr int units = 2 * kRunUnits;
         a.share = std::max(1, std::min(w4_run_share(128, a.K), parts_of(a.entries, units)));
         const int blocks = w4_run_blocks(a.entries, a.share, units);
-        if constexpr (PAIR) launch_product_kernel<q8_gated_small_run_kernel<TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
-        else if (a.N % 4 == 0) launch_product_kernel<q8_small_run_kernel<true, TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
-        else launch_product_kernel<q8_small_run_kernel<false, TAIL>>(a, blocks, w4_lds(128, 128), stage, st);
+        if constexpr (PAIR) launch_product_kernel<q8_gated_small_run_kernel<TAIL, ONCE>>(a, blocks, w4_lds(128, 128), stage, st);
+        else if (a.N % 4 == 0) launch_product_kernel<q8_small_run_kernel<true, TAIL, ONCE>>(a, blocks, w4_lds(128, 128), stage, st);
+        else launch_product_kernel<q8_small_run_kernel<false, TAIL, ONCE>>(a, blocks, w4_lds(128, 128), stage, st);
     };
     // (the forms without a tail take their depth in whole stages, those that run on four of them at least)
-    if (a.K % 64 == 0 && (plan.deep || a.K >= 256)) with_tail(std::false_type{});
-    else with_tail(std::true_type{});
+    const bool whole = a.K % 64 == 0 && (plan.deep || a.K >= 256);
+    if (whole && once) with_tail(std::false_type{}, std::true_type{});
+    else if (whole) with_tail(std::false_type{}, std::false_type{});
+    else if (once) with_tail(std::true_type{}, std::true_type{});
+    else with_tail(std::true_type{}, std::false_type{});
     return MOE_OK;
 }
 
