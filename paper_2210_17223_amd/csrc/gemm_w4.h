@@ -123,7 +123,7 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rs, int voff,
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds_as(__amdgpu_buffer_rsrc_t rs, int voff, uint32_t at, int soff)
 {
-    if constexpr (!ONCE) return load_to_lds(rs, voff, at, soff);
+    if constexpr (!ONCE) load_to_lds(rs, voff, at, soff);
 #if defined(__HIP_DEVICE_COMPILE__)
     else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen nt lds"
                  ::"v"(voff), "s"(rs), "s"(at), "s"(soff) : "memory", "m0");

@@ -171,8 +171,10 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         else return src;
     };
     constexpr bool TURNED = F16 == kI8Operands;
-    const int k_first = __builtin_amdgcn_readfirstlane(
-        !TURNED || row_src != nullptr ? 0 : ONCE ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(KT)) : static_cast<int>(blockIdx.x % 8u) * KT / 8);
+    int k_first = 0;
+    if constexpr (TURNED)
+        k_first = __builtin_amdgcn_readfirstlane(
+            row_src != nullptr ? 0 : ONCE ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(KT)) : static_cast<int>(blockIdx.x % 8u) * KT / 8);
     auto turned = [&](int k) {
         if constexpr (TURNED) return k + k_first < KT ? k + k_first : k + k_first - KT;
         else return k;

@@ -40,16 +40,18 @@ template <int TY, int VEC>
 struct Piece {
     static constexpr int W = TY == kF32 ? VEC : VEC / 2;
     uint32_t w[W];
+    template <bool NT = false>
     __device__ __forceinline__ void load(const void *row, int col)
     {
+        auto from = [](const auto *q) { return NT ? __builtin_nontemporal_load(q) : *q; };
         const char *p = static_cast<const char *>(row) + static_cast<size_t>(col) * (TY == kF32 ? 4 : 2);
         if constexpr (W == 2) {
-            const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+            const u32x2 v = from(reinterpret_cast<const u32x2 *>(p));
             w[0] = v[0], w[1] = v[1];
         } else {
 #pragma unroll
             for (int q = 0; q < W / 4; ++q) {
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 16 * q);
+                const u32x4 v = from(reinterpret_cast<const u32x4 *>(p + 16 * q));
 #pragma unroll
                 for (int c = 0; c < 4; ++c) w[4 * q + c] = v[c];
             }
@@ -78,23 +80,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 }
 
 // v to columns col .. col + VEC - 1 of a row, fp32 or rounded to bf16
-template <int VEC>
+template <int VEC, bool NT = false>
 __device__ __forceinline__ void store_row(void *row, bool f32, int col, const float (&v)[VEC])
 {
+    auto to = [](auto *q, auto x) { if constexpr (NT) __builtin_nontemporal_store(x, q); else *q = x; };
     if (f32) {
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q)
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(row) + col + 4 * q) =
-                (f32x4){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            to(reinterpret_cast<f32x4 *>(static_cast<float *>(row) + col + 4 * q), (f32x4){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
     } else {
         uint32_t w[VEC / 2];
 #pragma unroll
         for (int c = 0; c < VEC / 2; ++c) w[c] = pack_bf16(v[2 * c], v[2 * c + 1]);
         uint16_t *p = static_cast<uint16_t *>(row) + col;
         if constexpr (VEC == 8)
-            *reinterpret_cast<u32x4 *>(p) = (u32x4){w[0], w[1], w[2], w[3]};
+            to(reinterpret_cast<u32x4 *>(p), (u32x4){w[0], w[1], w[2], w[3]});
         else
-            *reinterpret_cast<u32x2 *>(p) = (u32x2){w[0], w[1]};
+            to(reinterpret_cast<u32x2 *>(p), (u32x2){w[0], w[1]});
     }
 }
 
@@ -159,9 +161,11 @@ struct NormArgs {
 
 constexpr int row_vec(int res, int z) { return res == kB16 && z != kF32 ? 8 : 4; }
 
-// Forward.  Columns of thread t: (v TPR + t) VEC .. + VEC - 1.  Q8: next leaves in 8 bits too, or only so.
-template <int RES, int Z, int TPR, int EPT, bool Q8 = false>
-__global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(NormArgs a)
+// Forward.  Columns of thread t: (v TPR + t) VEC .. + VEC - 1.  Q8: next leaves in 8 bits too, or only so; and what is read or written
+// once goes past the caches, where the codes then stay for the product that reads them (32768 rows of 2048, fp32 x, fp16 z, 0.87 GB: 168 us,
+// 5.2 TB/s, instead of 188).
+template <int RES, int Z, int TPR, int EPT, bool Q8>
+__device__ __forceinline__ void norm_forward(const NormArgs &a)
 {
     constexpr bool AFTER = Z >= 0;
     constexpr int ZT = AFTER ? Z : kF32, VEC = row_vec(RES, Z), NV = EPT / VEC;
@@ -187,11 +191,11 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
     auto fetch = [&](int i) {
         const char *x = static_cast<const char *>(a.x) + static_cast<size_t>(i) * d * RB;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) xr[v].load(x, col[v]);
+        for (int v = 0; v < NV; ++v) xr[v].template load<Q8>(x, col[v]);
         if constexpr (AFTER) {
             const char *z = static_cast<const char *>(a.z) + static_cast<size_t>(i) * d * ZB;
 #pragma unroll
-            for (int v = 0; v < NV; ++v) zr[v].load(z, col[v]);
+            for (int v = 0; v < NV; ++v) zr[v].template load<Q8>(z, col[v]);
         }
     };
     fetch(i0);
@@ -273,7 +277,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
                     if constexpr (RES == kB16) x[v][e] = __uint_as_float(pack_bf16(0.0f, x[v][e]));
                     x[v][e] = in[v] ? x[v][e] : 0.0f;
                 }
-                if (in[v]) store_row<VEC>(r, RES == kF32, col[v], x[v]);
+                if (in[v]) store_row<VEC, Q8>(r, RES == kF32, col[v], x[v]);
             }
         }
         norm(x);
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
         for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[v][e] = __builtin_fmaf(x[v][e], wn[v][e], bn[v][e]);
-            if (in[v] && (!Q8 || a.next != nullptr)) store_row<VEC>(next, a.next_f32, col[v], x[v]);
+            if (in[v] && (!Q8 || a.next != nullptr)) store_row<VEC, Q8>(next, a.next_f32, col[v], x[v]);
         }
         if constexpr (Q8) {
             uint32_t most = 0;
@@ -314,6 +318,17 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(
             if (t == 0) a.q_scale[i] = row.scale;
         }
     }
+}
+
+template <int RES, int Z, int TPR, int EPT>
+__global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_forward_kernel(NormArgs a)
+{
+    norm_forward<RES, Z, TPR, EPT, false>(a);
+}
+template <int RES, int Z, int TPR, int EPT>
+__global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void norm_q8_kernel(NormArgs a)
+{
+    norm_forward<RES, Z, TPR, EPT, true>(a);
 }
 
 // Rows of a run's partial sums: dw_next, db_next; behind a block also dw, db and what the run adds to the gradient
@@ -669,23 +684,38 @@ NormArgs norm_args(const moe_norm_shape &n)
 moe_status launch_norm_forward(const moe_norm_shape &n, NormArgs a, bool after, hipStream_t st)
 {
     with_types(n, after, [&](auto res, auto z) {
-        auto launch = [&](auto tpr, auto ept, int most) {
-            constexpr int TPR = decltype(tpr)::value;
+        using std::integral_constant;
+        constexpr int RES = decltype(res)::value, Z = decltype(z)::value, VEC = row_vec(RES, Z);
+        auto launch = [&](auto q8, auto tpr, auto ept, int most) {
+            constexpr int TPR = decltype(tpr)::value, EPT = decltype(ept)::value;
             a.per_run = parts_of(n.T, std::min(n.T, most));
             const int runs = parts_of(n.T, a.per_run);
-            auto run = [&](auto q8) {
-                hipLaunchKernelGGL((norm_forward_kernel<decltype(res)::value, decltype(z)::value, TPR, decltype(ept)::value, decltype(q8)::value>),
-                                   dim3(TPR == kWave ? ceil_div(runs, 4) : runs), dim3(TPR == kWave ? 256 : TPR), 0, st, a);
-            };
-            if (a.q != nullptr) run(std::true_type{});
-            else run(std::false_type{});
+            const dim3 grid(TPR == kWave ? ceil_div(runs, 4) : runs), block(TPR == kWave ? 256 : TPR);
+            if constexpr (decltype(q8)::value) hipLaunchKernelGGL((norm_q8_kernel<RES, Z, TPR, EPT>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((norm_forward_kernel<RES, Z, TPR, EPT>), grid, block, 0, st, a);
         };
-        using std::integral_constant;
-        if (n.d <= 512) launch(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 256 * 16);
-        else if (n.d <= 2048) launch(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 256 * 6);
-        else if (n.d <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 16>{}, 256 * 4);
-        else if (n.d <= 8192) launch(integral_constant<int, 512>{}, integral_constant<int, 16>{}, 256 * 2);
-        else launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 256);
+        auto plain = [&](auto tpr, auto ept, int most) { launch(std::false_type{}, tpr, ept, most); };
+        auto q8 = [&](auto tpr, auto ept, int most) { launch(std::true_type{}, tpr, ept, most); };
+        if (a.q == nullptr) {
+            if (n.d <= 512) plain(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 256 * 16);
+            else if (n.d <= 2048) plain(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 256 * 6);
+            else if (n.d <= 4096) plain(integral_constant<int, 256>{}, integral_constant<int, 16>{}, 256 * 4);
+            else if (n.d <= 8192) plain(integral_constant<int, 512>{}, integral_constant<int, 16>{}, 256 * 2);
+            else plain(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 256);
+            return;
+        }
+        // In 8 bits: few rows with as few columns per thread as there are, since a row's chain of sums is what takes the time (32 rows of
+        // 4096, fp32, 256 threads of sixteen columns 6.7 us, 1024 of four 5.3); many rows with eight, of which a thread's 90 to 124
+        // registers leave room for sixteen wavefronts on a unit.
+        const bool few = n.T <= 1024 && VEC == 4;
+        if (n.d <= 512) q8(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 256 * 16);
+        else if (few && n.d <= 1024) q8(integral_constant<int, 256>{}, integral_constant<int, VEC>{}, 1024);
+        else if (few && n.d <= 2048) q8(integral_constant<int, 512>{}, integral_constant<int, VEC>{}, 1024);
+        else if (few && n.d <= 4096) q8(integral_constant<int, 1024>{}, integral_constant<int, VEC>{}, 1024);
+        else if (n.d <= 2048) q8(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 256 * 4);
+        else if (n.d <= 4096) q8(integral_constant<int, 512>{}, integral_constant<int, 8>{}, 256 * 2);
+        else if (n.d <= 8192) q8(integral_constant<int, 1024>{}, integral_constant<int, 8>{}, 256);
+        else q8(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 256);
     });
     MOE_TRY_HIP(hipGetLastError());
     return MOE_OK;

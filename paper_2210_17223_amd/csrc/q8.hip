@@ -568,7 +568,9 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
             hipLaunchKernelGGL((q8_rows_kernel<decltype(ty)::value, TPR, decltype(nv)::value>), dim3(grid), dim3(TPR == kWave ? 256 : TPR),
                                0, st, x, static_cast<uint32_t *>(q), scale, R, K, rows_end);
         };
-        if (K <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+        // many rows: a wavefront each, as far as its registers go
+        if (R >= 2048 && K > 1024 && K <= 2048) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+        else if (K <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 1>{});
         else if (K <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
         else if (K <= 8192) launch(integral_constant<int, 256>{}, integral_constant<int, 2>{});
         else if (K <= 16384) launch(integral_constant<int, 512>{}, integral_constant<int, 2>{});
