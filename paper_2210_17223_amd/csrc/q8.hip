@@ -15,6 +15,7 @@
 #include "q8_product.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include <hip/hip_ext.h>
@@ -131,18 +132,22 @@ __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restri
 }
 
 // ---------------------------------------------------------------- few rows per expert
-// Four wavefronts share out the depth of a tile of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes; each
-// takes its stages through LDS of its own, PD of them on their way, so nothing is waited for but its own loads; the whole
-// numbers are added up through LDS at the end.
-template <bool PAIR, int RT, int PD, bool ONCE>
+// A wavefront multiplies tiles of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes, which go through LDS of its
+// own, PD of them on their way, so that nothing is waited for but its own loads.  Of a long depth a block's four wavefronts share out the
+// stages of one tile (SPLIT), and the whole numbers are added up through LDS at the end; of a short one each has a tile, four side by side.
+template <bool PAIR, int RT, int PD, bool ONCE, bool SPLIT>
 __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
 {
     constexpr int NT = PAIR ? 2 : 1, WAVES = 4, STAGE = (NT + RT) * 2048, LOADS = (NT + RT) * 2;
-    const Tiles<16 * RT, 16 * NT> tiles(a.offsets, a.E, a.tiles);
-    const WorkItem item = tiles[blockIdx.x];
+    const Tiles<16 * RT, (SPLIT ? 16 : 64) * NT> tiles(a.offsets, a.E, a.tiles);
+    WorkItem item = tiles[blockIdx.x];
     if (item.expert < 0) return;
     extern __shared__ __attribute__((aligned(16))) char q8_lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, oct = lane >> 4;
+    if constexpr (!SPLIT) {
+        item.n0 += wave * (16 * NT);
+        if (item.n0 / NT >= (PAIR ? a.h : a.N)) return;         // (no wavefront waits for another)
+    }
     char *const mine = q8_lds + wave * (STAGE * PD);
     const uint32_t dest = lds_address(mine);
     const int rows = item.row1 - item.row0, n0 = item.n0 / NT, width = PAIR ? a.h : a.N;
@@ -169,8 +174,8 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
         const int from = gather ? a.row_src[min(item.row0 + r, item.row1 - 1)] / a.row_div : r;
         xsrc[q] = r < rows ? static_cast<int>(from * pitch) + piece[q & 1] * 16 : 0x7ffffff0;
     }
-    const int KT = (a.K + 63) / 64, per = (KT + WAVES - 1) / WAVES;
-    const int s0 = min(wave * per, KT), s1 = min(s0 + per, KT);
+    const int KT = (a.K + 63) / 64, per = SPLIT ? (KT + WAVES - 1) / WAVES : KT;
+    const int s0 = SPLIT ? min(wave * per, KT) : 0, s1 = min(s0 + per, KT);
     // (a piece past the row's end: an offset past every resource reads as zeros)
     auto load = [&](int s, int place) {
         const uint32_t at = dest + place * STAGE;
@@ -225,24 +230,33 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int j = 0; j < RT; ++j) asm volatile("" : "+v"(acc[t][j]));
-    // sums of the wavefronts: [wave][tile][lane] of four numbers
-    __syncthreads();
-    i32x4 *const sums = reinterpret_cast<i32x4 *>(q8_lds);
+    if constexpr (SPLIT) {
+        // sums of the wavefronts: [wave][tile][lane] of four numbers
+        __syncthreads();
+        i32x4 *const sums = reinterpret_cast<i32x4 *>(q8_lds);
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int j = 0; j < RT; ++j) sums[((j * NT + t) * WAVES + wave) * 64 + lane] = acc[t][j];
-    __syncthreads();
-    if (wave >= RT) return;
-    const int j = wave, row = j * 16 + fr, n = n0 + oct * 4;
-    if (row >= rows || n >= width) return;
+            for (int j = 0; j < RT; ++j) sums[((j * NT + t) * WAVES + wave) * 64 + lane] = acc[t][j];
+        __syncthreads();
+        if (wave >= RT) return;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            i32x4 s = sums[(wave * NT + t) * WAVES * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) s += sums[((wave * NT + t) * WAVES + w) * 64 + lane];
+            acc[t][0] = s;
+        }
+    }
+#pragma unroll
+    for (int jj = 0; jj < (SPLIT ? 1 : RT); ++jj) {
+    const int j = SPLIT ? wave : jj, row = j * 16 + fr, n = n0 + oct * 4;
+    if (row >= rows || n >= width) continue;
     float v[NT][4];
     const float xs = row_scale(a, item.row0 + row);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        i32x4 s = sums[(j * NT + t) * WAVES * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += sums[((j * NT + t) * WAVES + w) * 64 + lane];
+        const i32x4 s = acc[t][jj];
         float cs[4];
         column_scales(a.ws + static_cast<size_t>(item.expert) * a.N + t * a.h, n, width, cs);
 #pragma unroll
@@ -276,6 +290,7 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
             const float u[1] = {v[0][c] + out.value(r, 0)};
             out.leave(row, u);
         }
+    }
     }
 }
 
@@ -581,21 +596,38 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
     else with_type(integral_constant<int, kF16>{});
 }
 
-// Tile of a product of `rows` rows of E experts, and whether the kernel for few rows takes it.
+// The kernel of a product of `rows` rows of E experts, by what each would take.
 struct Q8Plan {
-    int bm, bn;                            // bm 16 or 32: that kernel
-    bool deep;
+    int bm, bn;                            // tile; bm 16 or 32: the kernel for few rows
+    bool deep, split;
 };
 Q8Plan plan_product(int64_t rows, int E, int columns, int K)
 {
-    if (rows <= 32ll * E && rows * ((columns + 127) / 128) <= 4000) return {rows <= 16ll * E ? 16 : 32, 0, false};
-    if (K >= 320 && (rows / 128 + E) * ((columns + 127) / 128) <= 256) return {128, 128, true};
-    GemmPlan gp;
-    choose_w4_tile(std::max<int64_t>(rows, 256), E, columns, K, &gp);
-    if (gp.bm == 256) return {256, 256, false};
-    return {128, 128, false};
+    const double depth = 2.0 * K, stages = (K + 63) / 64, used = static_cast<double>(std::min<int64_t>(rows, E));
+    const double weights = used * columns * depth;                      // bytes
+    // row tiles: one of every expert while they are a good deal emptier than a tile, else half of one too many
+    auto row_tiles = [&](int bm) { return rows * 8 <= static_cast<int64_t>(bm) * E * 3 ? used : std::max(used, static_cast<double>(rows) / bm + E / 2.0); };
+    auto rounds = [](double tiles, double at_once) { return tiles > 3.0 * at_once ? tiles / at_once : std::ceil(tiles / at_once); };
+    Q8Plan best{0, 0, false, false};
+    double least = 1e30;
+    auto offer = [&](double us, Q8Plan p) {
+        if (us < least) {
+            least = us;
+            best = p;
+        }
+    };
+    for (int bm : {16, 32}) {
+        const double groups = row_tiles(bm) * ((columns + 15) / 16), bytes = groups * (16 + bm) * depth;
+        offer(4.0 + std::max({weights / 6.2e6, bytes / 16e6, groups / 768 * 4.5}), {bm, 0, false, true});
+        offer(4.0 + std::max({weights / 6.2e6, bytes / 16e6, groups / 4 / 768 * (2.0 + 0.5 * stages), 0.6 * stages}), {bm, 0, false, false});
+    }
+    const double t128 = row_tiles(128) * ((columns + 127) / 128), t256 = row_tiles(256) * ((columns + 255) / 256);
+    const double one = 6.0 + stages * 0.45, more = rounds(t128, 256) * (stages * 0.5 + 9.0);
+    if (K >= 320) offer(std::max(6.0 + weights / 6.4e6, t128 <= 256 ? one : more), {128, 128, true, false});
+    offer(6.0 + std::max({weights / 6e6, rounds(t128, 512) * stages * 0.5, t128 * stages * 32768 / 10.5e6}), {128, 128, false, false});
+    offer(4.0 + std::max(weights / 6e6, rounds(t256, 256) * (stages * 1.15 + 9.0)), {256, 256, false, false});
+    return best;
 }
-
 constexpr int64_t kKeptBytes = 64 << 20;
 
 template <bool PAIR>
@@ -603,8 +635,8 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
 {
     const int columns = tile_columns(a);
     Q8Plan plan = plan_product(rows, a.E, columns, a.K);
-    if (!PAIR && plan.bn == 256 && a.N % 4 != 0) plan = {128, 128, false};
-    const int bn = plan.bm <= 32 ? (PAIR ? 32 : 16) : plan.bn;
+    if (!PAIR && plan.bn == 256 && a.N % 4 != 0) plan = {128, 128, false, false};
+    const int bn = plan.bm <= 32 ? (PAIR ? 2 : 1) * (plan.split ? 16 : 64) : plan.bn;
     a.tiles = (columns + bn - 1) / bn;
     const int64_t entries = tile_entries(rows, a.E, plan.bm, a.tiles);
     if (entries >= 1ll << 30) {
@@ -615,16 +647,22 @@ moe_status launch_product(Q8Args a, int64_t rows, int stage, hipStream_t st)
     // Weights that one tile of rows reads, and more of them than stay in the last level of cache until the next call.
     const bool once = rows <= static_cast<int64_t>(plan.bm) * a.E && 2ll * a.E * a.N * a.K > kKeptBytes;
     if (plan.bm <= 32) {
-        auto stream = [&](auto rt, auto once) {
-            constexpr int RT = decltype(rt)::value, PD = PAIR ? 2 : RT == 1 ? 3 : 2;
-            launch_product_kernel<q8_stream_kernel<PAIR, RT, PD, decltype(once)::value>>(a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048,
-                                                                                        stage, st);
-        };
         using std::integral_constant;
-        if (plan.bm == 16 && once) stream(integral_constant<int, 1>{}, std::true_type{});
-        else if (plan.bm == 16) stream(integral_constant<int, 1>{}, std::false_type{});
-        else if (once) stream(integral_constant<int, 2>{}, std::true_type{});
-        else stream(integral_constant<int, 2>{}, std::false_type{});
+        auto stream = [&](auto rt, auto once, auto split) {
+            constexpr int RT = decltype(rt)::value, PD = PAIR ? 2 : RT == 1 ? 3 : 2;
+            launch_product_kernel<q8_stream_kernel<PAIR, RT, PD, decltype(once)::value, decltype(split)::value>>(
+                a, entries, static_cast<size_t>(4) * PD * ((PAIR ? 2 : 1) + RT) * 2048, stage, st);
+        };
+        auto with_split = [&](auto rt, auto oncec) {
+            if (plan.split) stream(rt, oncec, std::true_type{});
+            else stream(rt, oncec, std::false_type{});
+        };
+        auto with_once = [&](auto rt) {
+            if (once) with_split(rt, std::true_type{});
+            else with_split(rt, std::false_type{});
+        };
+        if (plan.bm == 16) with_once(integral_constant<int, 1>{});
+        else with_once(integral_constant<int, 2>{});
         return MOE_OK;
     }
     if (plan.bn == 256) {

@@ -291,7 +291,9 @@ def test_rows_taken_where_they_are_and_rows_moved_give_the_same_bits(T, k, E, d,
 @pytest.mark.parametrize("kind,res,z,bias,gate_tokens", [("rms", "f32", "f16", False, 0), ("layer", "bf16", "bf16", True, 2),
                                                          ("rms", "bf16", "f32", False, 3), ("layer", "f32", "f32", True, 0)])
 def test_norms_write_the_codes_of_their_fp32_rows(T, d, kind, res, z, bias, gate_tokens):
-    """next in fp32 is what the codes are of; r and next are the bits of the calls without codes."""
+    """next in fp32 is what the codes are of, whether it is wanted or not.  r and next against 64 bits: a row's mean and mean square are sums in
+    at most 16 + 10 + 4 steps, 2^-19 of the sums of magnitudes, and so is a factor's; of a hat, whose root mean square is one, 2^-18 (1 + |hat|)
+    with the roundings of its products; r once more rounded to its type."""
     g = gen(T + d)
     n = moe.NormShape.make(T, d, kind=kind, dtype="f32", res=res, z=z, scale=0.7, gate_tokens=gate_tokens)
     x, zz = normal(g, T, d, std=2.0).to(n.res_torch_dtype), normal(g, T, d).to(n.z_torch_dtype)
@@ -299,20 +301,32 @@ def test_norms_write_the_codes_of_their_fp32_rows(T, d, kind, res, z, bias, gate
     w, wn, b, bn = vec(), vec(), vec() if bias else None, vec() if bias else None
     gate = normal(g, n.gates, d, std=0.3) + 0.5
     new = lambda dtype, *s: torch.empty(*s, dtype=dtype, device=DEV)  # noqa: E731
+
+    def hat(v):
+        v = v.double()
+        v = v - v.mean(1, keepdim=True) if kind == "layer" else v
+        return v * torch.rsqrt(v.square().mean(1, keepdim=True) + 1e-5)
+
     for after in (True, False):
-        r = [new(n.res_torch_dtype, T, d) for _ in range(3)]
-        nx = [new(torch.float32, T, d) for _ in range(2)]
+        r = [new(n.res_torch_dtype, T, d) for _ in range(2)]
+        nx = new(torch.float32, T, d)
         q, s = [new(torch.int8, T, d) for _ in range(2)], [new(torch.float32, T) for _ in range(2)]
         if after:
-            moe.moe_norm_after(n, x, zz, w, b, gate, r[0], wn, bn, nx[0])
-            moe.moe_norm_after_q8(n, x, zz, w, b, gate, r[1], wn, bn, nx[1], q[0], s[0])
-            moe.moe_norm_after_q8(n, x, zz, w, b, gate, r[2], wn, bn, None, q[1], s[1])
-            assert torch.equal(r[0], r[1]) and torch.equal(r[0], r[2])
+            moe.moe_norm_after_q8(n, x, zz, w, b, gate, r[0], wn, bn, nx, q[0], s[0])
+            moe.moe_norm_after_q8(n, x, zz, w, b, gate, r[1], wn, bn, None, q[1], s[1])
+            assert torch.equal(r[0], r[1])
+            zh, gt = hat(zz), 0.7 * gate[torch.arange(T, device=DEV) // (gate_tokens or T)].double()
+            want = x.double() + gt * (zh * w + (0 if b is None else b.double()))
+            room = 2.0 ** -18 * (1 + zh.abs()) * (gt * w).abs() + 2.0 ** -23 * (x.double().abs() + want.abs()) + 2.0 ** -22
+            assert bool(((r[0].double() - want).abs() <= room + (EPS["bf16"] * 1.01 * want.abs() if res == "bf16" else 0)).all())
+            rh = hat(r[0])
         else:
-            moe.moe_norm_before(n, x, wn, bn, nx[0])
-            moe.moe_norm_before_q8(n, x, wn, bn, nx[1], q[0], s[0])
+            moe.moe_norm_before_q8(n, x, wn, bn, nx, q[0], s[0])
             moe.moe_norm_before_q8(n, x, wn, bn, None, q[1], s[1])
-        code, scale = held(nx[0])
-        assert torch.equal(nx[0], nx[1])
+            rh = hat(x)
+        want = rh * wn + (0 if bn is None else bn.double())
+        room = 2.0 ** -18 * (1 + rh.abs()) * wn.abs() + 2.0 ** -23 * want.abs() + 2.0 ** -22
+        assert bool(((nx.double() - want).abs() <= room).all())
+        code, scale = held(nx)
         for k in range(2):
             assert torch.equal(q[k], code) and torch.equal(s[k], scale)
