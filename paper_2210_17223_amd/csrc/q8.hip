@@ -176,10 +176,13 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
     }
     const int KT = (a.K + 63) / 64, per = SPLIT ? (KT + WAVES - 1) / WAVES : KT;
     const int s0 = SPLIT ? min(wave * per, KT) : 0, s1 = min(s0 + per, KT);
+    // Every block begins elsewhere in its stages: whole numbers' sums are exact in any order, rows of weights are often a power of two bytes
+    // apart, and blocks that walk them in step ask few of the memory channels at a time.
+    const int turn = __builtin_amdgcn_readfirstlane(s1 > s0 ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(s1 - s0)) : 0);
     // (a piece past the row's end: an offset past every resource reads as zeros)
     auto load = [&](int s, int place) {
         const uint32_t at = dest + place * STAGE;
-        const int k = s * 128;
+        const int k = (s + turn < s1 ? s + turn : s + turn - (s1 - s0)) * 128;
         const bool past0 = s >= s1 || k + piece[0] * 16 >= static_cast<int>(pitch), past1 = s >= s1 || k + piece[1] * 16 >= static_cast<int>(pitch);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -596,7 +599,7 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
     else with_type(integral_constant<int, kF16>{});
 }
 
-// The kernel of a product of `rows` rows of E experts, by what each would take.
+// The kernel of a product of `rows` rows of E experts, by what each would take, us.
 struct Q8Plan {
     int bm, bn;                            // tile; bm 16 or 32: the kernel for few rows
     bool deep, split;
@@ -605,8 +608,13 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
 {
     const double depth = 2.0 * K, stages = (K + 63) / 64, used = static_cast<double>(std::min<int64_t>(rows, E));
     const double weights = used * columns * depth;                      // bytes
-    // row tiles: one of every expert while they are a good deal emptier than a tile, else half of one too many
-    auto row_tiles = [&](int bm) { return rows * 8 <= static_cast<int64_t>(bm) * E * 3 ? used : std::max(used, static_cast<double>(rows) / bm + E / 2.0); };
+    // tiles of bm rows: one of every expert while they are a good deal emptier than a tile, else half of one too many
+    auto few = [&](int bm) { return rows * 8 <= static_cast<int64_t>(bm) * E * 3; };
+    auto row_tiles = [&](int bm) {
+        if (E == 1) return static_cast<double>((rows + bm - 1) / bm);
+        return few(bm) ? used : std::max(used, static_cast<double>(rows) / bm + E / 2.0);
+    };
+    // how often `tiles` go round a chip that holds at_once of them (many: the shares even out)
     auto rounds = [](double tiles, double at_once) { return tiles > 3.0 * at_once ? tiles / at_once : std::ceil(tiles / at_once); };
     Q8Plan best{0, 0, false, false};
     double least = 1e30;
@@ -618,16 +626,17 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     };
     for (int bm : {16, 32}) {
         const double groups = row_tiles(bm) * ((columns + 15) / 16), bytes = groups * (16 + bm) * depth;
-        offer(4.0 + std::max({weights / 6.2e6, bytes / 16e6, groups / 768 * 4.5}), {bm, 0, false, true});
-        offer(4.0 + std::max({weights / 6.2e6, bytes / 16e6, groups / 4 / 768 * (2.0 + 0.5 * stages), 0.6 * stages}), {bm, 0, false, false});
+        offer(4.0 + std::max({weights / 5.8e6, bytes / 14.5e6, groups / 768 * 4.5, 0.42 / 4 * stages}), {bm, 0, false, true});
+        offer(4.0 + std::max({weights / 6.9e6, bytes / 19.5e6, groups / 3072 * (2.5 + 0.7 * stages), 0.42 * stages}), {bm, 0, false, false});
     }
     const double t128 = row_tiles(128) * ((columns + 127) / 128), t256 = row_tiles(256) * ((columns + 255) / 256);
-    const double one = 6.0 + stages * 0.45, more = rounds(t128, 256) * (stages * 0.5 + 9.0);
-    if (K >= 320) offer(std::max(6.0 + weights / 6.4e6, t128 <= 256 ? one : more), {128, 128, true, false});
-    offer(6.0 + std::max({weights / 6e6, rounds(t128, 512) * stages * 0.5, t128 * stages * 32768 / 10.5e6}), {128, 128, false, false});
-    offer(4.0 + std::max(weights / 6e6, rounds(t256, 256) * (stages * 1.15 + 9.0)), {256, 256, false, false});
+    const double deep = (E == 1 || few(128) ? row_tiles(128) : static_cast<double>(rows) / 128 + E) * ((columns + 127) / 128);
+    if (K >= 320) offer(std::max(6.0 + weights / 6.4e6, deep <= 256 ? 6.0 + 0.45 * stages : rounds(deep, 256) * (9.0 + 0.5 * stages)), {128, 128, true, false});
+    offer(std::max(6.0 + weights / 6e6, t128 <= 256 ? 8.0 + 0.42 * stages : 3.0 + rounds(t128, 512) * (8.0 + stages)), {128, 128, false, false});
+    offer(std::max(6.0 + weights / 6e6, 4.0 + rounds(t256, 256) * (8.0 + 1.3 * stages)), {256, 256, false, false});
     return best;
 }
+
 constexpr int64_t kKeptBytes = 64 << 20;
 
 template <bool PAIR>
