@@ -63,9 +63,17 @@ typedef struct {
  *   w, w_scale         the experts' matrices
  *   bias               fp32 [E, N] or NULL
  *   r                  [R, N] or NULL; it may be y where their types are the same
- * Rows of y at or beyond offsets[E] are left as they are. */
+ * N below 2^21.  The same bits whichever kernel a shape's size chooses.  Rows of y at or beyond offsets[E] are left as they are. */
 moe_status moe_q8_linear(const moe_q8_shape *s, const void *x, const float *x_scale, const int32_t *offsets, const void *w,
                          const float *w_scale, const float *bias, const void *r, void *y, void *stream);
+
+/* Which kernel moe_q8_linear launches for the shape, and moe_gated_ffn_q8 for its product `which` (0: first projections; 1: second), written
+ * to name (host, len bytes, always terminated) as "<kernel> <tile rows>x<tile columns>", with " split" behind it where a block shares out
+ * a tile's depth, " deep" where five stages of loads are on their way, " once" where the weights go past the caches and " tail" where the
+ * depth is not taken in whole stages of 128, so that a measurement or a test can say which kernel it ran.  MOE_EINVAL for a null name,
+ * len == 0 or another which; else as the call that launches it. */
+moe_status moe_q8_linear_kernel(const moe_q8_shape *s, char *name, size_t len);
+moe_status moe_gated_q8_kernel(const moe_shape *s, int32_t which, char *name, size_t len);
 
 /* moe_dispatch of rows in 8 bits: x [T, d_model] with x_scale [T] to xe [moe_max_rows, d_model] with xe_scale
  * [moe_max_rows].  xe and xe_scale may both be NULL: only counts, offsets, slot_of and src_of are wanted, for the

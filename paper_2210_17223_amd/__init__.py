@@ -27,13 +27,13 @@ from .gated_binding import (Q4Shape, moe_gated_backward_workspace_bytes, moe_gat
                             moe_gated_workspace_bytes, moe_pack_gated_weights, moe_q4_linear)
 from .norm_binding import (NormShape, moe_norm_after, moe_norm_after_backward, moe_norm_before,
                            moe_norm_before_backward, moe_norm_workspace_bytes)
-from .q8_binding import (Q8Shape, moe_dispatch_q8, moe_gated_ffn_q8, moe_gated_q8_workspace_bytes, moe_norm_after_q8,
-                         moe_norm_before_q8, moe_q8_linear, moe_q8_rows, moe_q8_values)
+from .q8_binding import (Q8Shape, moe_dispatch_q8, moe_gated_ffn_q8, moe_gated_q8_kernel, moe_gated_q8_workspace_bytes,
+                         moe_norm_after_q8, moe_norm_before_q8, moe_q8_linear, moe_q8_linear_kernel, moe_q8_rows, moe_q8_values)
 from . import comm_binding as comm
 from .comm_binding import moe_layer_padded, moe_padded_workspace_bytes
 
 __all__ = ["Q8Shape", "moe_dispatch_q8", "moe_gated_ffn_q8", "moe_gated_q8_workspace_bytes", "moe_norm_after_q8", "moe_norm_before_q8",
-           "moe_q8_linear", "moe_q8_rows", "moe_q8_values", "Q4Shape", "moe_gated_kept_workspace_bytes", "moe_gated_kept_backward_workspace_bytes", "moe_gated_gemm_kernel", "moe_gated_ffn_q4", "moe_gated_q4_workspace_bytes", "moe_q4_linear", "moe_gated_backward_workspace_bytes", "moe_gated_ffn", "moe_gated_ffn_backward", "moe_gated_packed_bytes",
+           "moe_q8_linear", "moe_q8_linear_kernel", "moe_gated_q8_kernel", "moe_q8_rows", "moe_q8_values", "Q4Shape", "moe_gated_kept_workspace_bytes", "moe_gated_kept_backward_workspace_bytes", "moe_gated_gemm_kernel", "moe_gated_ffn_q4", "moe_gated_q4_workspace_bytes", "moe_q4_linear", "moe_gated_backward_workspace_bytes", "moe_gated_ffn", "moe_gated_ffn_backward", "moe_gated_packed_bytes",
            "moe_gated_workspace_bytes", "moe_pack_gated_weights", "NormShape", "moe_norm_after", "moe_norm_after_backward", "moe_norm_before",
            "moe_norm_before_backward", "moe_norm_workspace_bytes",
            "comm", "moe_layer_padded", "moe_padded_workspace_bytes", "moe_expert_ffn_offloaded", "moe_offload_staging_bytes", "moe_offload_workspace_bytes",

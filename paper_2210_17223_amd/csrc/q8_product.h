@@ -20,6 +20,7 @@ struct Q8Args {
 };
 
 // q8_run.hip: tiles of 256 x 256; pair: the first projections, else the linear map, N a multiple of 4.
-void launch_q8_run(bool pair, const Q8Args &a, int64_t blocks, int stage, hipStream_t st);
+// whole: the depth is taken in whole stages of 64, four at least.
+void launch_q8_run(bool pair, const Q8Args &a, int64_t entries, bool whole, int stage, hipStream_t st);
 
 }  // namespace moe

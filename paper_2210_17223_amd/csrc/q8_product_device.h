@@ -17,12 +17,19 @@ enum { kF32 = 0, kB16 = 1, kF16 = 2 };       // element types as in moe_q8_shape
 __device__ __forceinline__ float f16_of(uint32_t w, int i) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[i]); }
 __device__ __forceinline__ float b16_of(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
 
+// v as it is in fp32, rounded to fp16: the compiler may not fold the product or sum before it into one instruction that rounds once, in
+// some kernels and not in others.
+__device__ __forceinline__ _Float16 to_f16(float v)
+{
+    asm("" : "+v"(v));
+    return static_cast<_Float16>(v);
+}
 __device__ __forceinline__ uint32_t pack_16(int type, float lo, float hi)
 {
     if (type == kF16) {
         f16x2 h;
-        h[0] = static_cast<_Float16>(lo);
-        h[1] = static_cast<_Float16>(hi);
+        h[0] = to_f16(lo);
+        h[1] = to_f16(hi);
         return __builtin_bit_cast(uint32_t, h);
     }
     bf16x2 b;
@@ -85,6 +92,8 @@ struct ActForm {
     }
     __device__ __forceinline__ float operator()(float v) const
     {
+#pragma clang fp contract(off)
+        // (the last product is rounded before a residual is added to it, in every kernel)
         const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
         const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
         return v * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
@@ -172,7 +181,7 @@ __device__ __forceinline__ void store_hidden(const Q8Args &a, size_t row, int n,
 {
     f16x4 o;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] = static_cast<_Float16>(v[c]);
+    for (int c = 0; c < 4; ++c) o[c] = to_f16(v[c]);
     *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(a.y) + row * a.h + n) = o;
 }
 __device__ __forceinline__ float row_scale(const Q8Args &a, int row)

@@ -37,7 +37,6 @@ __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
             for (int j = 0; j < TM; ++j) c.xs[j] = a.xs[min(item.row0 + wm * (BM / 2) + j * 16 + (lane & 15), item.row1 - 1)];
             const float *ws = a.ws + static_cast<size_t>(item.expert) * a.N;
             const float *bias = a.bias != nullptr ? a.bias + static_cast<size_t>(item.expert) * a.N : ws;
-            const float with = a.bias != nullptr ? 1.0f : 0.0f;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int n = min(item.n0 + wn * 128 + half * 64 + lane % 16 * 4, a.N - 4);
@@ -45,7 +44,7 @@ __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     c.ws[half][e] = s[e];
-                    c.bias[half][e] = b[e] * with;
+                    c.bias[half][e] = a.bias != nullptr ? b[e] : 0.0f;
                 }
             }
             return c;
@@ -177,7 +176,7 @@ __global__ __launch_bounds__(256, 1) void q8_gated_run_kernel(Q8Args a)
                     for (int c = 0; c < 4; ++c) {
                         const float g = sum_of(acc[2 * p][j][c]) * ahead.xs[j] * ahead.gs[p][c];
                         const float u = sum_of(acc[2 * p + 1][j][c]) * ahead.xs[j] * ahead.us[p][c];
-                        o[c] = static_cast<_Float16>(activate<ACT>(form, g) * u);
+                        o[c] = to_f16(activate<ACT>(form, g) * u);
                         if constexpr (ACT == kForm) MOE_SB();      // (four at a time spill registers)
                     }
                     *reinterpret_cast<f16x4 *>(place.at(p, 0)) = o;
@@ -202,7 +201,7 @@ __global__ __launch_bounds__(256, 1) void q8_gated_run_kernel(Q8Args a)
 
 }  // namespace
 
-void launch_q8_run(bool pair, const Q8Args &args, int64_t entries, int stage, hipStream_t st)
+void launch_q8_run(bool pair, const Q8Args &args, int64_t entries, bool whole, int stage, hipStream_t st)
 {
     Q8Args a = args;
     a.share = w4_run_share(BM, a.K);
@@ -223,8 +222,7 @@ void launch_q8_run(bool pair, const Q8Args &args, int64_t entries, int stage, hi
             else launch_product_kernel<q8_run_kernel<ACT, false, false, TAIL>>(a, blocks, kW4RunLds, stage, st);
         });
     };
-    // (the form without a tail takes its depth in whole stages, four of them at least)
-    if (a.K % 64 == 0 && a.K >= 256) with_tail(std::false_type{});
+    if (whole) with_tail(std::false_type{});
     else with_tail(std::true_type{});
 }
 

@@ -45,6 +45,9 @@ def _lib():
             getattr(L, "moe_" + name).argtypes = [C.POINTER(shape)] + [vp] * pointers
         for name in ("q8_rows", "q8_values", "norm_before_q8", "norm_after_q8", "q8_linear", "dispatch_q8", "gated_ffn_q8"):
             getattr(L, "moe_" + name).restype = C.c_int
+        L.moe_q8_linear_kernel.argtypes = [C.POINTER(Q8Shape), C.c_char_p, C.c_size_t]
+        L.moe_gated_q8_kernel.argtypes = [C.POINTER(Shape), i32, C.c_char_p, C.c_size_t]
+        L.moe_q8_linear_kernel.restype = L.moe_gated_q8_kernel.restype = C.c_int
         L.moe_gated_q8_workspace_bytes.restype = C.c_size_t
         L.moe_gated_q8_workspace_bytes.argtypes = [C.POINTER(Shape)]
         _ready = True
@@ -94,6 +97,20 @@ def moe_q8_linear(s: Q8Shape, x, x_scale, offsets, w, w_scale, bias, r, y, strea
         C.byref(s), arg(x, I8, s.R * s.K, "x"), arg(x_scale, F32, s.R, "x_scale"), arg(offsets, I32, s.E + 1, "offsets"),
         arg(w, I8, s.E * s.N * s.K, "w"), arg(w_scale, F32, s.E * s.N, "w_scale"), opt(bias, F32, s.E * s.N, "bias"),
         opt(r, _TORCH.get(s.res), s.R * s.N, "r"), arg(y, _TORCH.get(s.y), s.R * s.N, "y"), raw_stream(stream, x)))
+
+
+def moe_q8_linear_kernel(s: Q8Shape) -> str:
+    """Name, tile and form of the kernel that moe_q8_linear launches."""
+    buf = C.create_string_buffer(96)
+    _check(_lib().moe_q8_linear_kernel(C.byref(s), buf, C.sizeof(buf)))
+    return buf.value.decode()
+
+
+def moe_gated_q8_kernel(s: Shape, which: int) -> str:
+    """The same of moe_gated_ffn_q8's products (0: first projections, 1: second)."""
+    buf = C.create_string_buffer(96)
+    _check(_lib().moe_gated_q8_kernel(C.byref(s), int(which), buf, C.sizeof(buf)))
+    return buf.value.decode()
 
 
 def moe_dispatch_q8(s: Shape, x, x_scale, expert_idx, counts, offsets, slot_of, src_of, xe, xe_scale, workspace,

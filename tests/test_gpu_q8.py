@@ -136,22 +136,33 @@ def test_values_are_codes_times_scales(R, K, dtype):
 
 
 # ---------------------------------------------------------------------------- linear map
-# R counts by expert, N, K: every kernel and form, in the order of q8.hip
+# every kernel and form: (rows by expert, N, K)
 LINEAR = {
-    "few, one row": ([1], 64, 4096), "few, depth below a stage": ([3, 0, 2], 48, 16), "few, uneven": ([0, 17, 1, 31, 0], 100, 1040),
-    "few, odd width": ([5, 16], 37, 272), "few, 32 rows": ([32], 96, 640), "few, wide": ([9], 5001, 128),
-    "tiles": ([200, 0, 130], 256, 512), "tiles, tail": ([300], 132, 1008), "tiles, one stage": ([150], 300, 128),
-    "tiles, odd width": ([129, 260], 131, 272), "tiles, width 3": ([500], 3, 64),
-    "deep": ([100, 60], 384, 4096), "deep, tail": ([140], 388, 4080),
-    "wide": ([700, 1, 900], 2048, 1024), "wide, tail": ([2600], 1028, 656), "wide, odd width": ([2600], 1027, 640),
-    "128 x 256": ([2100, 1900], 2052, 6144 + 16), "128 x 256, whole": ([4100], 2048, 6400),
-    "256 x 256": ([3000, 5, 2500], 4096, 2176), "256 x 256, short": ([9000], 4096, 256),
+    "q8_stream_kernel 16x16 split": [([1], 64, 16), ([0, 17, 1, 31, 0], 100, 1040), ([5, 16], 37, 272), ([1], 4096, 4096), ([20], 1101, 65536)],
+    "q8_stream_kernel 16x16 split once": [([0, 2, 0], 4100, 6160), ([1], 16385, 4112)],
+    "q8_stream_kernel 16x16": [([1, 0, 3, 1, 0], 256, 16), ([9], 5001, 128)],
+    "q8_stream_kernel 16x16 once": [([0, 2, 0, 0, 0, 17, 0, 1], 16388, 512), ([1, 0, 0, 0, 0, 0, 0, 0], 16385, 528)],
+    "q8_stream_kernel 32x16 split": [([0, 33, 3], 68, 16), ([70, 1, 49], 65, 144)],
+    "q8_stream_kernel 32x16": [([900, 0, 377], 68, 16), ([500, 1, 96, 31, 0, 300, 200, 100], 65, 48)],
+    "q8_stream_kernel 32x16 once": [([33, 1, 0, 32, 9, 0, 5, 3], 4100, 2048), ([0, 87, 0, 0, 0, 0, 0, 0], 4097, 2064)],
+    "q8_tile_kernel 128x128 deep": [([700, 1, 900], 2048, 1024), ([2600], 1027, 640)],
+    "q8_tile_kernel 128x128 deep tail": [([2600], 1028, 656), ([800, 0, 700], 1001, 1040)],
+    "q8_tile_kernel 128x128 deep once": [([100, 1, 0, 130, 20, 17, 15, 5], 2052, 4096), ([33], 16385, 4096)],
+    "q8_tile_kernel 128x128 deep once tail": [([100, 1, 0, 130, 20, 17, 25, 17], 2048, 4112), ([33], 16385, 4112)],
+    "q8_small_run_kernel 128x128": [([3000, 51, 3100], 260, 512), ([2000, 0, 4496], 257, 512)],
+    "q8_small_run_kernel 128x128 tail": [([4000, 51, 3100], 260, 144), ([7199, 0, 0], 257, 144), ([0, 4000, 5000], 517, 16)],
+    "q8_small_run_kernel 128x128 once": [([128, 1, 0, 130, 100, 40, 40, 5], 4100, 2048), ([64, 40, 0, 200, 100, 47, 10, 10], 4097, 2048)],
+    "q8_small_run_kernel 128x128 once tail": [([128, 1, 0, 130, 100, 40, 41, 5], 4096, 2064), ([64, 40, 0, 200, 100, 49, 10, 10], 4097, 2064)],
+    "q8_run_kernel 256x256": [([3000, 5, 2500], 4096, 2176), ([8000, 0, 126], 1004, 512)],
+    "q8_run_kernel 256x256 tail": [([9000], 4096, 256), ([100, 0, 200, 1, 22, 100, 50, 50], 8192, 16), ([2100, 1900], 2052, 6160)],
 }
+LINEAR = {f"{name} {i}": case + (name,) for name, cases in LINEAR.items() for i, case in enumerate(cases)}
 
 
 def linear_case(name, seed=0, spare=0):
-    counts, N, K = LINEAR[name]
+    counts, N, K, kernel = LINEAR[name]
     g, E, R = gen(seed), len(counts), sum(counts) + spare
+    assert moe.moe_q8_linear_kernel(moe.Q8Shape.make(R, E, N, K)) == kernel
     x, w = codes(g, R, K), codes(g, E, N, K)
     return dict(R=R, E=E, N=N, K=K, x=x, w=w, xs=scales(g, R, of=1 / 73), ws=scales(g, E, N, of=1 / (73 * math.sqrt(K))),
                 offsets=offsets_of(counts), g=g, rows=sum(counts))
@@ -171,8 +182,7 @@ def test_sums_are_exact(name):
     assert torch.equal(y, want)
 
 
-@pytest.mark.parametrize("name", ["few, uneven", "few, odd width", "tiles, tail", "tiles, odd width", "deep", "wide", "wide, tail",
-                                  "128 x 256", "256 x 256"])
+@pytest.mark.parametrize("name", [n for n in LINEAR if " once" not in n or n.endswith(" 1")])
 @pytest.mark.parametrize("act,res,out,in_place", [
     ("identity", "", "bf16", False), ("silu", "f32", "f32", True), ("gelu", "bf16", "bf16", True), ("gelu_tanh", "f16", "f32", False),
     ("relu", "f32", "f16", False), ("gelu", "f16", "f16", True), ("identity", "bf16", "f32", False)])
@@ -200,18 +210,121 @@ def test_epilogue(name, act, res, out, in_place):
     assert float(over.max()) <= 0, (float(over.max()), int((over > 0).sum()))
 
 
+def test_the_same_bits_from_every_kernel():
+    """A row's output depends on the row, its expert and the map, not on how many others come with it."""
+    g = gen(9)
+    R, E, N, K = 6000, 3, 1027 + 1, 1040
+    x, w, xs, ws = codes(g, R, K), codes(g, E, N, K), scales(g, R, of=1 / 73), scales(g, E, N, of=1 / 2000)
+    bias, r = normal(g, E, N, std=0.5), normal(g, R, N)
+    for act, out in (("gelu", "f32"), ("silu", "f32"), ("identity", "f32"), ("identity", "f16"), ("relu", "bf16"), ("gelu_tanh", "f16")):
+        all_y, names = torch.empty(R, N, dtype=TYPES[out], device=DEV), set()
+        for counts in ([R, 0, 0], [1500, 0, 0], [400, 0, 0], [40, 0, 0], [3, 0, 0]):
+            n = sum(counts)
+            s = moe.Q8Shape.make(n, E, N, K, act=act, y=out)
+            names.add(moe.moe_q8_linear_kernel(s).split(" ")[0] + moe.moe_q8_linear_kernel(s)[-5:])
+            y = torch.empty(n, N, dtype=TYPES[out], device=DEV)
+            plain = out == "f16" and act == "identity"
+            moe.moe_q8_linear(s, x[:n], xs[:n], offsets_of(counts), w, ws, None if plain else bias, None if plain else r[:n].contiguous(), y)
+            if n == R:
+                all_y.copy_(y)
+            assert torch.equal(y, all_y[:n]), (act, n)
+        assert len(names) >= 3, names
+
+
+def test_no_rows_at_all():
+    """Every expert empty: nothing is read of the rows, and no output is written."""
+    g = gen(2)
+    x, w, xs, ws = codes(g, 4, 64), codes(g, 2, 96, 64), scales(g, 4), scales(g, 2, 96)
+    y = torch.full((4, 96), 7.0, device=DEV)
+    off = torch.zeros(3, dtype=torch.int32, device=DEV)
+    moe.moe_q8_linear(moe.Q8Shape.make(4, 2, 96, 64, y="f32"), x, xs, off, w, ws, None, None, y)
+    s = moe.Shape.make(4, 64, 2, 48, 1, 4, act="silu")
+    ye, wsp = torch.full((4, 64), 7.0, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q8(s, x, xs, None, off, w, ws, codes(g, 2, 64, 48), scales(g, 2, 64), ye, wsp)
+    assert bool((y == 7.0).all()) and bool((ye == 7.0).all())
+
+
+def test_codes_of_minus_128_and_the_longest_rows():
+    """The largest sums there are, 65536 (-128) (-128) = 2^30, and sums that cancel."""
+    K, N = 65536, 48
+    x, w = torch.full((3, K), -128, dtype=torch.int8, device=DEV), torch.full((1, N, K), -128, dtype=torch.int8, device=DEV)
+    x[1, K // 2:] = 127
+    x[2] = 127
+    one = torch.ones(3, device=DEV)
+    y = torch.empty(3, N, device=DEV)
+    moe.moe_q8_linear(moe.Q8Shape.make(3, 1, N, K, y="f32"), x, one, offsets_of([3]), w, torch.ones(1, N, device=DEV), None, None, y)
+    want = torch.tensor([K * 16384, K // 2 * (16384 - 128 * 127), -K * 128 * 127], dtype=torch.float64, device=DEV).float()
+    assert torch.equal(y, want[:, None].expand(3, N))
+
+
+def test_a_row_that_is_not_finite_spoils_no_other():
+    g = gen(4)
+    x = normal(g, 300, 512)
+    x[7, 3], x[200, 0] = math.nan, math.inf
+    q, s = torch.empty(300, 512, dtype=torch.int8, device=DEV), torch.empty(300, device=DEV)
+    moe.moe_q8_rows(x, q, s)
+    w, ws, off = codes(g, 1, 192, 512), scales(g, 1, 192), offsets_of([300])
+    y = torch.empty(300, 192, device=DEV)
+    moe.moe_q8_linear(moe.Q8Shape.make(300, 1, 192, 512, y="f32"), q, s, off, w, ws, None, None, y)
+    rows = torch.isnan(y)
+    assert rows.all(1).nonzero().flatten().tolist() == [7, 200] and rows.any(1).sum() == 2
+    sh = moe.Shape.make(300, 512, 1, 96, 1, 300, act="silu")
+    ye, wsp = torch.empty(300, 512, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(sh), dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q8(sh, q, s, None, off, w, ws * 1e-3, codes(g, 1, 512, 96), scales(g, 1, 512), ye, wsp)
+    assert torch.isnan(ye).all(1).nonzero().flatten().tolist() == [7, 200] and int(torch.isnan(ye).any(1).sum()) == 2
+
+
+@pytest.mark.parametrize("R,N,K,out", [(530000, 64, 4096, "f32"), (70000, 32768, 128, "f16")])
+def test_rows_and_outputs_past_32_bit_offsets(R, N, K, out):
+    """Rows of more than 2^31 bytes, and an output of more than 2^31 values: the last tile's, and some between."""
+    g = gen(R)
+    x, w = torch.zeros(R, K, dtype=torch.int8, device=DEV), codes(g, 1, N, K)
+    at = torch.tensor([0, 1, R // 2, R - 129, R - 2, R - 1], device=DEV)
+    x[at] = codes(g, len(at), K)
+    xs, ws = torch.ones(R, device=DEV), scales(g, 1, N, of=1 / (73 * 73 * math.sqrt(K)))
+    y = torch.empty(R, N, dtype=TYPES[out], device=DEV)
+    moe.moe_q8_linear(moe.Q8Shape.make(R, 1, N, K, y=out), x, xs, offsets_of([R]), w, ws, None, None, y)
+    want = ((x[at].double() @ w[0].double().T).float() * ws[0]).to(TYPES[out])
+    assert torch.equal(y[at], want)
+    assert not bool(y[2:R // 2:1001].any()) and not bool(y[R // 2 + 1:R - 129:1003].any())
+    del y
+    if K >= 4096:
+        v, q, s = torch.empty(R, K, dtype=torch.float16, device=DEV), torch.empty_like(x), torch.empty(R, device=DEV)
+        moe.moe_q8_values(x, xs, v)
+        assert torch.equal(v[at], x[at].half())
+        moe.moe_q8_rows(v, q, s)
+        code, scale = held(v[at])
+        assert torch.equal(q[at], code) and torch.equal(s[at], scale)
+
+
 # ---------------------------------------------------------------------------- gated block
+# every kernel and form of the first projections: (rows by expert, d_model, d_ff)
 GATED = {
-    "one row": ([1], 256, 512), "few, uneven": ([0, 17, 1, 14, 0], 272, 144), "few, 32 rows": ([32, 3], 1040, 528),
-    "tiles": ([200, 0, 130], 512, 384), "tiles, tail": ([300, 1], 1008, 208), "deep": ([100, 60], 4096, 320),
-    "wide": ([700, 1, 900], 1024, 1024), "wide, tail": ([2600], 656, 1040), "256 x 256": ([3000, 5, 2500], 2176, 2048),
-    "256 x 256, tail": ([9000], 304, 1552),
+    "q8_stream_kernel 16x32 split": [([1], 256, 512), ([0, 17, 1, 12, 0], 272, 144), ([1, 0, 0], 16, 64)],
+    "q8_stream_kernel 16x32 split once": [([0, 1, 0, 2, 0, 0, 1, 0], 4112, 1024)],
+    "q8_stream_kernel 16x32": [([0, 2, 1], 16, 256), ([1, 0, 3, 0, 2], 640, 1040)],
+    "q8_stream_kernel 16x32 once": [([0, 2, 0, 0, 0, 1, 0, 2], 2064, 2048)],
+    "q8_stream_kernel 32x32 split": [([20, 0, 5], 16, 64), ([32, 3], 1040, 528)],
+    "q8_stream_kernel 32x32": [([200, 0, 130], 512, 384), ([500, 0, 258, 0, 0, 0, 0, 0], 16, 64)],
+    "q8_stream_kernel 32x32 once": [([33, 1, 0, 60, 40, 0, 9, 3], 4112, 1024)],
+    "q8_tile_kernel 128x128 deep": [([700, 1, 900], 1024, 1024), ([8000, 0, 738], 640, 64)],
+    "q8_tile_kernel 128x128 deep tail": [([8000, 0, 600, 0, 79], 656, 64)],
+    "q8_tile_kernel 128x128 deep once": [([100, 1, 0, 130, 20, 17, 15, 6], 4224, 1024)],
+    "q8_tile_kernel 128x128 deep once tail": [([100, 1, 0, 130, 20, 17, 16, 6], 4112, 1024)],
+    "q8_gated_small_run_kernel 128x128": [([2000, 1, 1288], 512, 256)],
+    "q8_gated_small_run_kernel 128x128 tail": [([2600], 656, 1040), ([900, 0, 113], 16, 1024)],
+    "q8_gated_small_run_kernel 128x128 once": [([100, 0, 200, 10, 60, 10, 5, 10], 2176, 2048)],
+    "q8_gated_small_run_kernel 128x128 once tail": [([100, 0, 200, 10, 60, 10, 1, 10], 2064, 2048)],
+    "q8_gated_run_kernel 256x256": [([3000, 5, 2500], 2176, 2048), ([4000, 0, 131], 512, 1024)],
+    "q8_gated_run_kernel 256x256 tail": [([9000], 304, 1552), ([100, 0, 200, 1, 15, 100, 50, 50], 16, 4096)],
 }
+GATED = {f"{name} {i}": case + (name,) for name, cases in GATED.items() for i, case in enumerate(cases)}
 
 
 def gated_case(name, seed=0, spare=0):
-    counts, d, h = GATED[name]
+    counts, d, h, kernel = GATED[name]
     g, E, R = gen(seed), len(counts), sum(counts) + spare
+    assert moe.moe_gated_q8_kernel(moe.Shape.make(R, d, E, h, 1, R), 0) == kernel
     return dict(R=R, rows=sum(counts), E=E, d=d, h=h, x=codes(g, R, d), xs=scales(g, R, of=1 / 73), offsets=offsets_of(counts),
                 q13=codes(g, E, 2 * h, d), s13=scales(g, E, 2 * h, of=1 / (73 * math.sqrt(d))), q2=codes(g, E, d, h),
                 s2=scales(g, E, d, of=1 / (73 * math.sqrt(h))))
@@ -253,14 +366,19 @@ def test_gated_block(name, act):
         assert float(off.max()) <= 0.14 * rms
 
 
-@pytest.mark.parametrize("T,k,E,d,h,capacity", [(5, 2, 8, 256, 512, 5), (700, 2, 4, 384, 272, 250), (3000, 3, 5, 272, 528, 3000),
-                                                (9000, 1, 2, 1024, 1040, 9000)])
-def test_rows_taken_where_they_are_and_rows_moved_give_the_same_bits(T, k, E, d, h, capacity):
+@pytest.mark.parametrize("kernel,T,k,E,d,h,capacity", [
+    ("q8_stream_kernel 16x32 split", 5, 2, 8, 1024, 256, 5), ("q8_stream_kernel 32x32", 700, 2, 4, 384, 272, 250),
+    ("q8_stream_kernel 16x32 once", 4, 2, 8, 2064, 2048, 4), ("q8_tile_kernel 128x128 deep tail", 2170, 4, 5, 656, 64, 2170),
+    ("q8_tile_kernel 128x128 deep once", 289, 1, 8, 4224, 1024, 200), ("q8_gated_small_run_kernel 128x128", 1644, 2, 3, 512, 256, 1644),
+    ("q8_gated_small_run_kernel 128x128 tail", 338, 3, 3, 16, 1024, 338), ("q8_gated_run_kernel 256x256 tail", 3000, 3, 5, 272, 1552, 2500),
+    ("q8_gated_run_kernel 256x256", 9000, 1, 2, 1024, 1040, 9000)])
+def test_rows_taken_where_they_are_and_rows_moved_give_the_same_bits(kernel, T, k, E, d, h, capacity):
     g = gen(T)
     x, xs = codes(g, T, d), scales(g, T, of=1 / 73)
     idx = torch.rand(T, E, generator=g, device=DEV).argsort(1)[:, :k].contiguous().int().view(-1)
     s = moe.Shape.make(T, d, E, h, k, capacity, act="silu")
     rows = moe.moe_max_rows(s)
+    assert moe.moe_gated_q8_kernel(s, 0) == kernel
     i32 = lambda n: torch.full((n,), -7, dtype=torch.int32, device=DEV)  # noqa: E731
     plans = [dict(counts=i32(E), offsets=i32(E + 1), slot_of=i32(T * k), src_of=i32(rows)) for _ in range(3)]
     xe, xes = torch.full((rows, d), 5, dtype=torch.int8, device=DEV), torch.full((rows,), -1.0, device=DEV)
@@ -284,6 +402,25 @@ def test_rows_taken_where_they_are_and_rows_moved_give_the_same_bits(T, k, E, d,
     moe.moe_gated_ffn_q8(s, xe, xes, None, plans[0]["offsets"], q13, s13, q2, s2, ye[0], gws)
     moe.moe_gated_ffn_q8(s, x, xs, plans[0]["src_of"], plans[0]["offsets"], q13, s13, q2, s2, ye[1], gws)
     assert torch.equal(ye[0], ye[1]) and bool((ye[0][A:] == 7.0).all())
+
+
+def test_the_blocks_same_bits_from_every_kernel():
+    """As the linear map: a row's output does not depend on how many others come with it."""
+    g = gen(10)
+    R, E, d, h = 6000, 3, 1040, 1552
+    x, xs = codes(g, R, d), scales(g, R, of=1 / 73)
+    q13, s13 = codes(g, E, 2 * h, d), scales(g, E, 2 * h, of=1 / (73 * math.sqrt(d)))
+    q2, s2 = codes(g, E, d, h), scales(g, E, d, of=1 / (73 * math.sqrt(h)))
+    for act in ("silu", "gelu", "gelu_tanh"):
+        all_ye, names = None, set()
+        for n in (R, 1500, 500, 40, 2):
+            s = moe.Shape.make(n, d, E, h, 1, n, act=act)
+            names |= {moe.moe_gated_q8_kernel(s, w).split(" ")[0] for w in (0, 1)}
+            ye, ws = torch.empty(n, d, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+            moe.moe_gated_ffn_q8(s, x[:n], xs[:n], None, offsets_of([n, 0, 0]), q13, s13, q2, s2, ye, ws)
+            all_ye = ye if all_ye is None else all_ye
+            assert torch.equal(ye, all_ye[:n]), (act, n)
+        assert len(names) >= 4, names
 
 
 # ---------------------------------------------------------------------------- norms
@@ -330,3 +467,108 @@ def test_norms_write_the_codes_of_their_fp32_rows(T, d, kind, res, z, bias, gate
         code, scale = held(nx)
         for k in range(2):
             assert torch.equal(q[k], code) and torch.equal(s[k], scale)
+
+
+# ---------------------------------------------------------------------------- together
+class Step:
+    """Between two blocks and through the next one, in 8 bits: norm, a projection, dispatch, gated experts, combine, next norm."""
+
+    def __init__(self, T=37, d=256, h=272, E=5, k=2, N=320, seed=0):
+        g = gen(seed)
+        self.n = moe.NormShape.make(T, d, res="f32", z="f32")
+        self.s = moe.Shape.make(T, d, E, h, k, T, act="silu", renorm_topk=True)
+        self.lin = moe.Q8Shape.make(T, 1, N, d, act="gelu", res="f32", y="f32")
+        new = lambda dtype, *s: torch.empty(*s, dtype=dtype, device=DEV)  # noqa: E731
+        rows, self.T = moe.moe_max_rows(self.s), T
+        self.x, self.w0, self.w1 = normal(g, T, d), normal(g, d, std=0.1) + 1, normal(g, d, std=0.1) + 1
+        self.W, self.Ws = codes(g, 1, N, d), scales(g, 1, N, of=1 / (73 * 16))
+        self.bias, self.res = normal(g, 1, N, std=0.1), normal(g, T, N)
+        self.q13, self.s13 = codes(g, E, 2 * h, d), scales(g, E, 2 * h, of=1 / (73 * 16))
+        self.q2, self.s2 = codes(g, E, d, h), scales(g, E, d, of=1 / (73 * 16))
+        self.Wg = (torch.randn(d, E, generator=g, device=DEV) / 16).bfloat16()
+        self.Wgp = new(torch.float32, moe.moe_packed_gate_bytes(self.s) // 4)
+        moe.moe_pack_gate(self.s, self.Wg, self.Wgp)
+        self.next, self.q, self.qs = new(torch.bfloat16, T, d), new(torch.int8, T, d), new(torch.float32, T)
+        self.y, self.off = new(torch.float32, T, N), offsets_of([T])
+        i32 = lambda n: new(torch.int32, n)  # noqa: E731
+        self.idx, self.gate = i32(T * k), new(torch.float32, T * k)
+        self.plan = [i32(E), i32(E + 1), i32(T * k), i32(rows)]
+        self.pws, self.gws = new(torch.uint8, moe.moe_workspace_bytes(self.s, 1)), new(torch.uint8, moe.moe_gated_q8_workspace_bytes(self.s))
+        self.ye, self.z, self.r, self.out, self.outs = (new(torch.float16, rows, d), new(torch.float32, T, d), new(torch.float32, T, d),
+                                                        new(torch.int8, T, d), new(torch.float32, T))
+
+    def run(self):
+        s = self.s
+        moe.moe_norm_before_q8(self.n, self.x, self.w0, None, self.next, self.q, self.qs)
+        moe.moe_q8_linear(self.lin, self.q, self.qs, self.off, self.W, self.Ws, self.bias, self.res, self.y)
+        moe.moe_route(s, self.next, self.Wgp, None, 0, self.idx, self.gate)
+        moe.moe_dispatch_q8(s, self.q, self.qs, self.idx, *self.plan, None, None, self.pws)
+        moe.moe_gated_ffn_q8(s, self.q, self.qs, self.plan[3], self.plan[1], self.q13, self.s13, self.q2, self.s2, self.ye, self.gws)
+        moe.moe_combine(s, self.ye, self.plan[2], self.gate, self.z, None)
+        moe.moe_norm_after_q8(self.n, self.x, self.z, self.w1, None, None, self.r, self.w0, None, None, self.out, self.outs)
+        return [t.clone() for t in (self.next, self.q, self.qs, self.y, self.z, self.r, self.out, self.outs)]
+
+
+def test_a_step_of_them_together():
+    """The step's block against 64 bits from its own codes and choices, as the tests of its parts bound it."""
+    t = Step()
+    nx, q, qs, y, z, r, out, outs = t.run()
+    code, scale = held(q.double() * qs.double()[:, None])              # (codes reach 127 in every row)
+    assert int(q.abs().max(1).values.min()) == 127
+    v = (q.double() @ t.W[0].double().T) * qs.double()[:, None] * t.Ws[0].double() + t.bias[0].double()
+    assert float((y.double() - act64(v, "gelu") - t.res.double()).abs().max()) < 1e-5
+    want = torch.zeros_like(z, dtype=torch.float64)
+    h = t.s.d_ff
+    for i in range(t.T * t.s.k):
+        token, e = i // t.s.k, int(t.idx[i])
+        both = (t.q13[e].double() @ q[token].double()) * qs[token].double() * t.s13[e].double()
+        H = (act64(both[:h], "silu") * both[h:]).half()
+        hq, hs = held(H[None])
+        want[token] += t.gate[i].double() * (t.q2[e].double() @ hq[0].double()) * hs.double() * t.s2[e].double()
+    rms = float(want.square().mean().sqrt())
+    assert float((z.double() - want).square().mean().sqrt()) <= 2.3e-3 * rms
+    assert torch.equal(outs > 0, torch.ones_like(outs, dtype=torch.bool))
+
+
+def test_steps_captured_and_replayed_beside_eager_ones():
+    """Two graphs with buffers of their own, replayed in turn with the eager step and other streams' work between."""
+    a, b = Step(seed=1), Step(T=200, seed=2)
+    want = [a.run(), b.run()]
+    torch.cuda.synchronize()
+    graphs = []
+    for t in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            t.run()
+        graphs.append(g)
+    side = torch.cuda.Stream()
+    for turn in range(4):
+        for t, g, w in zip((a, b), graphs, want):
+            for out in (t.next, t.q, t.qs, t.y, t.z, t.r, t.out, t.outs, t.ye):
+                out.zero_()
+            g.replay()
+            if turn % 2:
+                torch.cuda.synchronize()
+            got = [v.clone() for v in (t.next, t.q, t.qs, t.y, t.z, t.r, t.out, t.outs)]
+            assert all(torch.equal(x, y) for x, y in zip(got, w)), turn
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            eager = b.run()
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(x, y) for x, y in zip(eager, want[1]))
+
+
+def test_two_streams_at_once():
+    """Calls of one kind in flight on two streams, with workspaces of their own."""
+    steps = [Step(T=3000, seed=3), Step(T=2900, seed=4)]
+    want = [t.run() for t in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+    got = [None, None]
+    for _ in range(3):
+        for i, (t, st) in enumerate(zip(steps, streams)):
+            with torch.cuda.stream(st):
+                got[i] = t.run()
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(g, w))

@@ -95,7 +95,7 @@ def test_gated_block_sizes_and_refusals():
     assert moe.moe_gated_q8_workspace_bytes(s) == rows * 128 * 2 + rows * 128 + -(-rows * 4 // 256) * 256
     for kw, frag in ((dict(dtype="f32"), "bf16"), (dict(d_model=72), "multiples of 16"), (dict(d_ff=72), "multiples of 16"),
                      (dict(d_ff=65552), "65536"), (dict(d_model=32768, d_ff=32768), "2^31"), (dict(E=65), "64"),
-                     (dict(T=(1 << 29) - 1, capacity=1 << 29, d_model=65536, d_ff=16), "2^30 tiles")):
+                     (dict(T=(1 << 29) - 1, capacity=1 << 29, d_model=65536, d_ff=16), "2^23 tiles")):
         assert moe.moe_gated_q8_workspace_bytes(shape(**kw)) == 0 and frag in moe.moe_last_error()
         assert L.moe_gated_ffn_q8(C.byref(shape(**kw)), *[OK] * 10, NULL) in (1, 2)
     assert L.moe_gated_ffn_q8(None, *[OK] * 10, NULL) == 1
@@ -136,3 +136,29 @@ def test_python_calls_check_types_and_sizes():
         moe.moe_q8_rows(torch.zeros(2, 16), torch.zeros(2, 16, dtype=torch.int8), torch.zeros(2))      # (not on a device)
     with pytest.raises(moe.MoeError, match="x: expected"):
         moe.moe_q8_linear(moe.Q8Shape.make(2, 1, 16, 16), torch.zeros(2, 16), None, None, None, None, None, None, None)
+
+
+def test_a_residual_of_another_type_may_not_be_the_output():
+    s = moe.Q8Shape.make(4, 2, 64, 128, res="f32", y="bf16")
+    other = C.c_void_p(8192)
+    assert q8_binding._lib().moe_q8_linear(C.byref(s), *[OK] * 6, other, other, NULL) == 1 and "same" in moe.moe_last_error()
+
+
+def test_kernel_names():
+    name = moe.moe_q8_linear_kernel
+    assert name(moe.Q8Shape.make(1, 1, 4096, 4096)) == "q8_stream_kernel 16x16 split"
+    assert name(moe.Q8Shape.make(16384, 1, 4096, 4096)) == "q8_run_kernel 256x256"
+    assert name(moe.Q8Shape.make(16384, 1, 4097, 4096)) == "q8_small_run_kernel 128x128"            # (its ways out are for four columns)
+    s = moe.Shape.make(2, 4096, 8, 14336, 1, 2, act="silu")
+    assert [moe.moe_gated_q8_kernel(s, w) for w in (0, 1)] == ["q8_stream_kernel 16x32 once", "q8_stream_kernel 16x16 split once"]
+    s = moe.Shape.make(32768, 2048, 32, 8192, 1, 32768, act="silu")
+    assert [moe.moe_gated_q8_kernel(s, w) for w in (0, 1)] == ["q8_gated_run_kernel 256x256", "q8_run_kernel 256x256"]
+    L, buf = q8_binding._lib(), C.create_string_buffer(8)
+    q = moe.Q8Shape.make(1, 1, 64, 64)
+    assert L.moe_q8_linear_kernel(C.byref(q), None, 8) == 1 and L.moe_q8_linear_kernel(C.byref(q), buf, 0) == 1
+    assert L.moe_q8_linear_kernel(None, buf, 8) == 1 and L.moe_gated_q8_kernel(None, 0, buf, 8) == 1
+    assert L.moe_q8_linear_kernel(C.byref(q), buf, 8) == 0 and buf.value == b"q8_stre"
+    for which in (-1, 2):
+        assert L.moe_gated_q8_kernel(C.byref(s), which, buf, 8) == 1
+    with pytest.raises(moe.MoeError):
+        name(moe.Q8Shape.make(1, 1, 64, 72))
