@@ -38,9 +38,6 @@ __device__ __forceinline__ uint32_t pack_16(int type, float lo, float hi)
     return __builtin_bit_cast(uint32_t, b);
 }
 
-// acc columns of a tile: BN packed ones of a pair of projections, sixteen of the first and the same sixteen of the second in turn
-__host__ __device__ inline int tile_columns(const Q8Args &a) { return a.h != 0 ? gated_packed_columns(a.h) : a.N; }
-
 // The tile of block entry b: a panel of kPanel tiles' rows of an expert column by column, then the next; an eighth of all tiles for
 // each XCD.  A wavefront holds the experts' row tiles and their running sum, a lane each.
 constexpr int kPanel = 8;
@@ -83,12 +80,13 @@ inline int64_t tile_entries(int64_t rows, int E, int bm, int tiles)
 // that the quotient is 1 or 0 from |v| = 1e-36 on; and identity, 2 v / 2.  An epilogue that holds accumulators takes no branch, and a
 // kernel for each activation is five times the code.  (v^2 is bounded so that 0 v^2 is 0.)
 struct ActForm {
-    float a, b, factor;
+    float a, b, factor, lowest;
     __device__ __forceinline__ explicit ActForm(int act)
     {
         a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : act == MOE_ACT_RELU ? 1e38f : 0.0f;
         b = act == MOE_ACT_GELU_TANH ? 0.10294324f : 0.0f;
         factor = act == MOE_ACT_IDENTITY ? 2.0f : 1.0f;
+        lowest = act == MOE_ACT_IDENTITY ? -__builtin_inff() : -3.4e38f;
     }
     __device__ __forceinline__ float operator()(float v) const
     {
@@ -96,7 +94,8 @@ struct ActForm {
         // (the last product is rounded before a residual is added to it, in every kernel)
         const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
         const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
-        return v * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
+        // (of -infinity the others' limit is 0)
+        return __builtin_elementwise_maximum(v, lowest) * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
     }
 };
 // The activation in every kernel (FORM: by its form), so that all give the same bits.
@@ -105,6 +104,7 @@ template <int ACT>
 __device__ __forceinline__ float activate(const ActForm &form, float v)
 {
     if constexpr (ACT == kForm) return form(v);
+    else if constexpr (ACT == MOE_ACT_SILU) return gate_value<ACT>(__builtin_elementwise_maximum(v, -3.4e38f));
     else return gate_value<ACT>(v);
 }
 // f(integral_constant of GELU_ERF, of `plain`, or of kForm)

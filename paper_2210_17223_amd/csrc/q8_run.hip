@@ -54,7 +54,8 @@ __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
             const bool wide = a.res == kF32;
             // (a row past the tile's or a column past N lies past the resources; of the residual's two, which are of its two sizes, one is empty)
             const size_t first = static_cast<size_t>(row0) * a.N;
-            const unsigned values = static_cast<unsigned>(max(item.row1 - row0, 0)) * static_cast<unsigned>(a.N);
+            // (the wavefront's 128 rows at most: 2^28 values, so that what lies past N lies past these)
+            const unsigned values = static_cast<unsigned>(min(max(item.row1 - row0, 0), BM / 2)) * static_cast<unsigned>(a.N);
             const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(a.y) + first * (Y32 ? 4 : 2), 0,
                                                                                 values * (Y32 ? 4u : 2u), 0x00020000);
             char *const rbase = static_cast<char *>(const_cast<void *>(a.r)) + first * (wide ? 4 : 2);

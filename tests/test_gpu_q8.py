@@ -274,6 +274,52 @@ def test_a_row_that_is_not_finite_spoils_no_other():
     assert torch.isnan(ye).all(1).nonzero().flatten().tolist() == [7, 200] and int(torch.isnan(ye).any(1).sum()) == 2
 
 
+@pytest.mark.parametrize("name", ["q8_stream_kernel 16x16 split 0", "q8_stream_kernel 32x16 0", "q8_tile_kernel 128x128 deep 1",
+                                  "q8_small_run_kernel 128x128 tail 2", "q8_run_kernel 256x256 1"])
+@pytest.mark.parametrize("act", ["identity", "relu", "silu", "gelu", "gelu_tanh"])
+def test_activations_of_infinities(name, act):
+    """Sums that leave fp32's range are infinite, and the activations take their limits there."""
+    c = linear_case(name)
+    xs = torch.full((c["R"],), 3e38, device=DEV)
+    y = torch.empty(c["R"], c["N"], device=DEV)
+    moe.moe_q8_linear(moe.Q8Shape.make(c["R"], c["E"], c["N"], c["K"], act=act, y="f32"), c["x"], xs, c["offsets"], c["w"],
+                      torch.full_like(c["ws"], 2.0), None, None, y)
+    v = sums(c["x"], c["w"], c["offsets"])
+    assert bool((y[v > 0] == math.inf).all()) and bool((v < 0).any())
+    assert bool((y[v < 0] == -math.inf).all()) if act == "identity" else bool((y[v < 0].abs() < 1e-6).all())
+
+
+@pytest.mark.parametrize("T,d,h", [(3, 64, 64), (300, 512, 256), (9000, 512, 256)])
+def test_gates_of_minus_infinity_are_closed(T, d, h):
+    g = gen(T)
+    x, w = codes(g, T, d).abs().clamp(min=1), codes(g, 1, 2 * h, d)
+    w[:, :h] = -w[:, :h].abs().clamp(min=1)
+    ws = torch.ones(1, 2 * h, device=DEV)
+    ws[:, :h] = 3e38
+    s = moe.Shape.make(T, d, 1, h, 1, T, act="silu")
+    ye, wsp = torch.empty(T, d, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q8(s, x, torch.full((T,), 3.0, device=DEV), None, offsets_of([T]), w, ws, codes(g, 1, d, h), scales(g, 1, d), ye, wsp)
+    assert not bool(ye.any())
+
+
+@pytest.mark.parametrize("res", ["", "f32", "f16"])
+def test_the_most_columns_there_can_be(res):
+    """N near 2^21, no multiple of a tile's columns: what a tile holds past N is neither read nor written."""
+    g = gen(6)
+    R, N, K = 256, (1 << 21) - 4, 16
+    x, w, xs, ws = codes(g, R, K), codes(g, 1, N, K), scales(g, R), scales(g, 1, N)
+    shape = moe.Q8Shape.make(R, 1, N, K, res=res or "f32", y="f32")
+    assert moe.moe_q8_linear_kernel(shape) == "q8_run_kernel 256x256 tail"
+    r = torch.randint(-9, 10, (R, N), generator=g, device=DEV, dtype=torch.int8).to(TYPES[res]) if res else None
+    y = torch.empty(R, N, device=DEV)
+    moe.moe_q8_linear(shape, x, xs, offsets_of([R]), w, ws, None, r, y)
+    for i in range(0, R, 32):
+        want = (x[i:i + 32].float() @ w[0].float().T) * xs[i:i + 32, None] * ws[0]     # (sums below 2^24: exact in fp32)
+        if r is not None:
+            want = want + r[i:i + 32].float()
+        assert torch.equal(y[i:i + 32], want), i
+
+
 @pytest.mark.parametrize("R,N,K,out", [(530000, 64, 4096, "f32"), (70000, 32768, 128, "f16")])
 def test_rows_and_outputs_past_32_bit_offsets(R, N, K, out):
     """Rows of more than 2^31 bytes, and an output of more than 2^31 values: the last tile's, and some between."""
