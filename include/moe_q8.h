@@ -90,7 +90,7 @@ size_t moe_gated_q8_workspace_bytes(const moe_shape *s);
  *   q13 [E, 2 d_ff, d_model]: rows [0, d_ff) are Wg, [d_ff, 2 d_ff) Wu; q2 [E, d_model, d_ff]; each with its scales
  *   x, x_scale   src_of NULL: expert-major, [moe_max_rows, d_model] and [moe_max_rows]; else [T, d_model] and [T], and
  *                slot i takes the row of token src_of[i] / k (src_of as the dispatch wrote it)
- * d_model and d_ff multiples of 16, at most 65536, and 2 d_ff d_model below 2^31; with src_of also T d_model.
+ * d_model and d_ff multiples of 16, at most 65536, and 2 d_ff d_model below 2^31 - 2^26; with src_of T d_model below 2^31 - 2^20.
  * A value of H past 65504 is infinite, and its row then NaN. */
 moe_status moe_gated_ffn_q8(const moe_shape *s, const void *x, const float *x_scale, const int32_t *src_of,
                             const int32_t *offsets, const void *q13, const float *scale13, const void *q2,

@@ -81,9 +81,10 @@ struct W4Place {                       // where a wavefront stands in its tile
 // are sixteen of W's first pair_h rows and the same sixteen of its other pair_h in turn (N = 2 pair_h).  Of 8-bit operands, whose tiles have half
 // the stages and more to prepare (scales of rows and columns), prepare is called in front of the tile's first stage instead of behind its last.
 // BN: 256, or 128 with BM 128: the ring of five units of 16 KiB, two blocks to a compute unit, 4 KiB of LDS for a wavefront's way out.
-// ONCE: few rows, whose weights are read once: past the caches' lines, and from another place of the depth in every block (of
-// whole numbers, whose sums are exact in any order): rows of weights are often a power of two bytes apart, and blocks that walk them in step
-// ask few of the memory channels at a time.  Else 8-bit operands' blocks do so by their XCD, whose L2 they share.
+// ONCE: few rows of 8-bit operands, whose weights are read once: past the caches' lines, and from another place of the depth in every block
+// (of whole numbers, whose sums are exact in any order): rows of weights are often a power of two bytes apart, and blocks that walk them in
+// step ask few of the memory channels at a time.  (Many rows gain nothing from it: 16384 x 4096 x 4096 256 us without, 260 with a place
+// for each XCD.)
 template <int F16, bool KTAIL, int BM, int ABL, bool PAIR = false, int BN = 256, bool ONCE = false, typename Items, typename Prepare, typename Epilogue>
 __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uint16_t *__restrict__ W,
                                        const Items &items, const int32_t *__restrict__ nitems, int entries, int share,
@@ -170,13 +171,10 @@ __device__ __forceinline__ void w4_run(const uint16_t *__restrict__ A, const uin
         if constexpr (KTAIL) return k * BK + first_col[q & 1] < K ? src : 0x7ffffff0;
         else return src;
     };
-    constexpr bool TURNED = F16 == kI8Operands;
     int k_first = 0;
-    if constexpr (TURNED)
-        k_first = __builtin_amdgcn_readfirstlane(
-            row_src != nullptr ? 0 : ONCE ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(KT)) : static_cast<int>(blockIdx.x % 8u) * KT / 8);
+    if constexpr (ONCE) k_first = __builtin_amdgcn_readfirstlane(row_src == nullptr ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(KT)) : 0);
     auto turned = [&](int k) {
-        if constexpr (TURNED) return k + k_first < KT ? k + k_first : k + k_first - KT;
+        if constexpr (ONCE) return k + k_first < KT ? k + k_first : k + k_first - KT;
         else return k;
     };
     auto load_a = [&](int q, int unit, int k) { load_to_lds(rsa, piece_of(a_src[q], q, turned(k)), a_dest + unit + q * 1024, turned(k) * (BK * 2)); };

@@ -57,7 +57,8 @@ struct Sixteen {
 };
 
 // A row is TPR threads' (a wavefront's, or a block's), NV pieces of 16 values each, and stays in registers between the search for
-// its largest magnitude and its codes.  rows_end: NULL, or where the number of rows stands, at most R.
+// its largest magnitude and its codes: read once, written once, bound by memory (fp16 rows: 32768 of 2048 38 us, 5.3 TB/s; 32768 of 8192, a
+// block's hidden rows, 126 us, 6.4 TB/s).  rows_end: NULL, or where the number of rows stands, at most R.
 template <int TYPE, int TPR, int NV>
 __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void q8_rows_kernel(const void *__restrict__ x, uint32_t *__restrict__ q,
                                                                            float *__restrict__ scale, int64_t R, int K,
@@ -100,7 +101,8 @@ __global__ __launch_bounds__(TPR == kWave ? 256 : TPR) void q8_rows_kernel(const
     }
 }
 
-// A block takes `rows` rows' pieces of 16 codes.
+// A block takes `rows` rows' pieces of 16 codes, whichever row they are of.  Bound by memory: 32768 rows of 2048 to fp16, 0.2 GB, 30.6 us,
+// 6.6 TB/s.
 template <int TYPE>
 __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restrict__ q, const float *__restrict__ scale, void *__restrict__ x,
                                                         int64_t R, int K, int rows)
@@ -133,9 +135,13 @@ __global__ __launch_bounds__(256) void q8_values_kernel(const uint32_t *__restri
 }
 
 // ---------------------------------------------------------------- few rows per expert
-// A wavefront multiplies tiles of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes, which go through LDS of its
-// own, PD of them on their way, so that nothing is waited for but its own loads.  Of a long depth a block's four wavefronts share out the
-// stages of one tile (SPLIT), and the whole numbers are added up through LDS at the end; of a short one each has a tile, four side by side.
+// Bound by the weights' arrival.  A wavefront multiplies tiles of 16 columns (of a pair 16 of each) and at most 32 rows in stages of 128 codes,
+// which go through LDS of its own, PD of them on their way, so that nothing is waited for but its own loads.  PD is small, 2 or 3: what is on
+// its way comes from many wavefronts on a unit, and each stage more takes LDS from them (4 and 5 were slower).  Where tiles are few, a block's
+// four wavefronts share out the stages of one tile (SPLIT), and the whole numbers are added up through LDS at the end; else each has a tile, four side by
+// side.  Measured, kernel alone: 1 row, 4096 x 4096, 5.2 us (the latency of a launch and two round trips); 32 rows, 6144 x 4096, 8.3 us, 3.0 TB/s;
+// a block's projections for 64 rows of 8 experts, 4096 to 2 x 14336, 137 us, 6.9 TB/s, and back 74 us, 6.3 TB/s; for 2 rows 35 us,
+// 6.7 TB/s, and back 20.7, 5.7 TB/s.  Reading alone reaches 7.1 TB/s in 2 GB and 6.3 in 128 MB.
 template <bool PAIR, int RT, int PD, bool ONCE, bool SPLIT>
 __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
 {
@@ -178,7 +184,7 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
     const int KT = (a.K + 63) / 64, per = SPLIT ? (KT + WAVES - 1) / WAVES : KT;
     const int s0 = SPLIT ? min(wave * per, KT) : 0, s1 = min(s0 + per, KT);
     // Every block begins elsewhere in its stages: whole numbers' sums are exact in any order, rows of weights are often a power of two bytes
-    // apart, and blocks that walk them in step ask few of the memory channels at a time.
+    // apart, and blocks that walk them in step ask few of the memory channels at a time (1 row, 4096 x 4096: 8.1 -> 5.9 us a pass).
     const int turn = __builtin_amdgcn_readfirstlane(s1 > s0 ? static_cast<int>(blockIdx.x * 5u % static_cast<unsigned>(s1 - s0)) : 0);
     // (a piece past the row's end: an offset past every resource reads as zeros)
     auto load = [&](int s, int place) {
@@ -254,52 +260,55 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
     }
 #pragma unroll
     for (int jj = 0; jj < (SPLIT ? 1 : RT); ++jj) {
-    const int j = SPLIT ? wave : jj, row = j * 16 + fr, n = n0 + oct * 4;
-    if (row >= rows || n >= width) continue;
-    float v[NT][4];
-    const float xs = row_scale(a, item.row0 + row);
+        const int j = SPLIT ? wave : jj, row = j * 16 + fr, n = n0 + oct * 4;
+        if (row >= rows || n >= width) continue;
+        float v[NT][4];
+        const float xs = row_scale(a, item.row0 + row);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const i32x4 s = acc[t][jj];
-        float cs[4];
-        column_scales(a.ws + static_cast<size_t>(item.expert) * a.N + t * a.h, n, width, cs);
+        for (int t = 0; t < NT; ++t) {
+            const i32x4 s = acc[t][jj];
+            float cs[4];
+            column_scales(a.ws + static_cast<size_t>(item.expert) * a.N + t * a.h, n, width, cs);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const float in = static_cast<float>(s[c]) * xs;
-            if constexpr (PAIR) v[t][c] = in * cs[c];
-            else v[t][c] = __builtin_fmaf(in, cs[c], a.bias != nullptr ? a.bias[static_cast<size_t>(item.expert) * a.N + min(n + c, a.N - 1)] : 0.0f);
+            for (int c = 0; c < 4; ++c) {
+                const float in = static_cast<float>(s[c]) * xs;
+                if constexpr (PAIR) v[t][c] = in * cs[c];
+                else v[t][c] = __builtin_fmaf(in, cs[c], a.bias != nullptr ? a.bias[static_cast<size_t>(item.expert) * a.N + min(n + c, a.N - 1)] : 0.0f);
+            }
         }
-    }
-    const size_t at = static_cast<size_t>(item.row0 + row);
-    const ActForm form(a.act);
-    with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto act) {
+        const size_t at = static_cast<size_t>(item.row0 + row);
+        const ActForm form(a.act);
+        with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto act) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[0][c] = activate<decltype(act)::value>(form, v[0][c]) * (PAIR ? v[NT - 1][c] : 1.0f);
-    });
-    if constexpr (PAIR) {
-        store_hidden(a, at, n, v[0]);
-    } else if (a.N % 4 == 0) {
-        const WayOut<4> out(a, item.row0, item.row1, n);
-        typename WayOut<4>::Residual r;
-        out.ask(row, r);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[0][c] += out.value(r, c);
-        out.leave(row, v[0]);
-    } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const WayOut<1> out(a, item.row0, item.row1, n + c);
-            typename WayOut<1>::Residual r;
+            for (int c = 0; c < 4; ++c) v[0][c] = activate<decltype(act)::value>(form, v[0][c]) * (PAIR ? v[NT - 1][c] : 1.0f);
+        });
+        if constexpr (PAIR) {
+            store_hidden(a, at, n, v[0]);
+        } else if (a.N % 4 == 0) {
+            const WayOut<4> out(a, item.row0, item.row1, n);
+            typename WayOut<4>::Residual r;
             out.ask(row, r);
-            const float u[1] = {v[0][c] + out.value(r, 0)};
-            out.leave(row, u);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[0][c] += out.value(r, c);
+            out.leave(row, v[0]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const WayOut<1> out(a, item.row0, item.row1, n + c);
+                typename WayOut<1>::Residual r;
+                out.ask(row, r);
+                const float u[1] = {v[0][c] + out.value(r, 0)};
+                out.leave(row, u);
+            }
         }
-    }
     }
 }
 
 // ---------------------------------------------------------------- tiles of 128 x 128, one for a block
-// Few rows and a long depth: five stages on their way, one block to a compute unit, bound by the weights' arrival.
+// Some rows and a long depth: five stages on their way, one block to a compute unit, bound by the weights' arrival, or where tiles are fewer than
+// units by a tile's chain of stages, 0.4 to 0.5 us each.  Sums leave through LDS, so that y and r are met in whole lines of a row.
+// Measured, kernel alone: 64 rows, 32000 x 4096, fp32 out, 27 us, 5.2 TB/s; 1003 uneven rows of 5 experts, 1999 x 1008, silu, bias and an fp32
+// residual, one column a lane, 19 us (of 2000 columns, four a lane, 15.6).
 template <bool PAIR, bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 {
@@ -409,7 +418,10 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 }
 
 // ---------------------------------------------------------------- tiles of 128 x 128, a share of them for a block
-// As the kernels of q8_run.hip, two blocks to a compute unit: products of a short depth, whose tiles are mostly beginnings and ends.
+// As the kernels of q8_run.hip, two blocks to a compute unit: products of a few hundred tiles, and of a short depth, whose tiles are mostly
+// beginnings and ends.  Each operand's byte is multiplied half as often as in a 256 x 256 tile; a stage takes 1.0 us for the unit's two tiles, there
+// 1.3 for one of four times the area.  Measured, kernel alone: 8192 rows of 16 experts, 768 x 2048, 23 us, 1.12 POP/s
+// (6000 uneven rows of the same 25.0 us, in tiles of 256 x 256 30.8); 6002 uneven rows of 13 experts, 1008 x 2608, 34 us.
 // WHOLE: N is a multiple of four, and a lane takes four columns of a row on the way out; else one, of 64.
 template <bool WHOLE, bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
 }
 
 // ---------------------------------------------------------------- dispatch
-// codes and scales of the tokens to their slots; a wavefront owns a token
+// codes and scales of the tokens to their slots; a wavefront owns a token, whose codes are read once however many slots it has.  Bound by memory.
 __global__ __launch_bounds__(256) void q8_scatter_kernel(const u32x4 *__restrict__ x, const float *__restrict__ xs,
                                                          const int32_t *__restrict__ slot_of, u32x4 *__restrict__ xe,
                                                          float *__restrict__ xes, int T, int k, int vec, int max_rows)
@@ -588,7 +600,8 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
             hipLaunchKernelGGL((q8_rows_kernel<decltype(ty)::value, TPR, decltype(nv)::value>), dim3(grid), dim3(TPR == kWave ? 256 : TPR),
                                0, st, x, static_cast<uint32_t *>(q), scale, R, K, rows_end);
         };
-        // many rows: a wavefront each, as far as its registers go
+        // Many rows: a wavefront each, without a barrier, as far as its registers go (fp16, K = 2048, 2048 / 8192 / 32768 rows 6.5 / 12.9 /
+        // 38 us, by blocks of 256 threads 6.9 / 17 / 57; three pieces a lane, 6002 rows of 2608, 15.6 where the blocks take 14).
         if (R >= 2048 && K > 1024 && K <= 2048) launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});
         else if (K <= 1024) launch(integral_constant<int, 64>{}, integral_constant<int, 1>{});
         else if (K <= 4096) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
@@ -601,7 +614,9 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
     else with_type(integral_constant<int, kF16>{});
 }
 
-// The kernel of a product of `rows` rows of E experts, by what each would take, us.
+// The kernel of a product of `rows` rows of E experts, by what each would take, us: the weights' arrival, the bytes that pass through LDS, and the
+// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of every kernel over 104 products (1 to 16384 rows, 1
+// to 64 experts, 768 to 32000 columns, depths of 512 to 14336): the kernel chosen takes 1.02 times the fastest one's time on average, 1.27 at worst.
 struct Q8Plan {
     int bm, bn;                            // tile; bm 16 or 32: the kernel for few rows
     bool deep, split;
@@ -629,7 +644,7 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     for (int bm : {16, 32}) {
         const double groups = row_tiles(bm) * ((columns + 15) / 16), bytes = groups * (16 + bm) * depth;
         offer(4.0 + std::max({weights / 5.8e6, bytes / 14.5e6, groups / 768 * 4.5, 0.42 / 4 * stages}), {bm, 0, false, true});
-        offer(4.0 + std::max({weights / 6.9e6, bytes / 19.5e6, groups / 3072 * (2.5 + 0.7 * stages), 0.42 * stages}), {bm, 0, false, false});
+        offer(4.0 + std::max({weights / 6.9e6, bytes / 19.5e6, groups / 768 / 4 * (2.5 + 0.7 * stages), 0.42 * stages}), {bm, 0, false, false});
     }
     const double t128 = row_tiles(128) * ((columns + 127) / 128), t256 = row_tiles(256) * ((columns + 255) / 256);
     const double deep = (E == 1 || few(128) ? row_tiles(128) : static_cast<double>(rows) / 128 + E) * ((columns + 127) / 128);

@@ -1,6 +1,10 @@
 // Tiles of 256 x 256 of products of rows and weights in 8 bits (include/moe_q8.h): the linear map and the gated block's first
 // projections on the loop of gemm_w4_run.h.
 // Both epilogues pass their values through the wavefront's patch (W4Place), without a branch.
+// Bound by the matrix cores, whose rate depends on what they multiply: 16384 x 4096 x 4096 2.4 to 2.6 POP/s of random codes (3.2 of zeros), 8192^3 2.8
+// (3.6); instructions alone, from registers, reach 3.6 of random codes.  A stage of 64 x 2 codes takes 1.3 us.  Tiles of a short depth are bound by
+// their epilogue: of a pair 2050 vector instructions, 256 of them exponentials and reciprocals, beside a single wavefront per SIMD, 5 us
+// (8192 rows of 16 experts, 768 to 2 x 2048, 48 us, 1.07 POP/s; 32768 rows of 32 experts, 2048 to 2 x 8192, 960 to 1090 us, 2.0 to 2.3 POP/s).
 #include "activation.h"
 #include "gated.h"
 #include "moe_q8.h"
@@ -19,7 +23,10 @@ namespace {
 
 constexpr int BM = 256, TM = BM / 32;
 
-// The linear map.  Y32: y is fp32; RES: there is a residual, whose loads are a step of 64 columns ahead.
+// The linear map.  Y32: y is fp32; RES: there is a residual, whose loads are kAhead steps of 16 rows and 64 columns ahead: all units
+// reach their tiles' ends together, and wait for memory there (16384 x 4096 x 4096, GELU, bias, residual and y bf16: without the residual
+// 233 us, one step ahead 275, two 268, three, with 20 registers spilled instead of up to 7, 273).
+constexpr int kAhead = 2;
 template <int ACT, bool Y32, bool RES, bool KTAIL>
 __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
 {
@@ -64,20 +71,21 @@ __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
             const int n = n0 + lane % 16 * 4, step4 = 4 * a.N;
             // value of the lane's first row in 16 rows `j`, half `half`; four rows on is step4 further
             auto at_of = [&](int j, int half) { return n + half * 64 < a.N ? (j * 16 + lane / 16) * a.N + n + half * 64 : 0x1ff00000; };
-            u32x4 rw[4];
-            u32x2 rh[4];
-            auto ask = [&](int j, int half) {
-                int at = at_of(j, half);
+            u32x4 rw[kAhead][4];
+            u32x2 rh[kAhead][4];
+            auto ask = [&](auto stepc) {
+                constexpr int step = decltype(stepc)::value, turn = step % kAhead;
+                int at = at_of(step / 2, step % 2);
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
-                    rw[it] = __builtin_amdgcn_raw_buffer_load_b128(r32, at * 4, 0, 0);
-                    rh[it] = __builtin_amdgcn_raw_buffer_load_b64(r16, at * 2, 0, 0);
+                    rw[turn][it] = __builtin_amdgcn_raw_buffer_load_b128(r32, at * 4, 0, 0);
+                    rh[turn][it] = __builtin_amdgcn_raw_buffer_load_b64(r16, at * 2, 0, 0);
                     at += step4;
                 }
             };
-            if constexpr (RES) ask(0, 0);
+            if constexpr (RES) static_for<kAhead>(ask);
             static_for<2 * TM>([&](auto stepc) {
-                constexpr int step = decltype(stepc)::value, j = step / 2, half = step % 2;
+                constexpr int step = decltype(stepc)::value, j = step / 2, half = step % 2, turn = step % kAhead;
                 lds_handover();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -100,13 +108,13 @@ __global__ __launch_bounds__(256, 1) void q8_run_kernel(Q8Args a)
                     for (int c = 0; c < 4; ++c) {
                         v[it][c] = activate<ACT>(form, __builtin_fmaf(s[c], ahead.ws[half][c], ahead.bias[half][c]));
                         if constexpr (RES)
-                            v[it][c] += wide ? __uint_as_float(rw[it][c])
-                                             : a.res == kF16 ? f16_of(rh[it][c / 2], c % 2) : b16_of(rh[it][c / 2], c % 2);
+                            v[it][c] += wide ? __uint_as_float(rw[turn][it][c])
+                                             : a.res == kF16 ? f16_of(rh[turn][it][c / 2], c % 2) : b16_of(rh[turn][it][c / 2], c % 2);
                     }
                     if (it % 2 == 1) MOE_SB();
                 }
                 // (y may be r: what is asked for is of other rows or columns than what is stored)
-                if constexpr (RES && step + 1 < 2 * TM) ask((step + 1) / 2, (step + 1) % 2);
+                if constexpr (RES && step + kAhead < 2 * TM) ask(std::integral_constant<int, step + kAhead>{});
                 int at = at_of(j, half);
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
