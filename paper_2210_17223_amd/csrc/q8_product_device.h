@@ -128,6 +128,7 @@ struct WayOut {
     };
     __amdgpu_buffer_rsrc_t y32, y16, r32, r16;
     int pitch, column;
+    uint32_t none;                         // without a residual -0 is added, which leaves every value as it is, -0 too
     bool r_wide, r_f16, y_f16;
     __device__ __forceinline__ WayOut(const Q8Args &a, int row0, int row1, int n) : pitch(a.N), column(n < a.N ? n : 0x1ff00000)
     {
@@ -136,7 +137,8 @@ struct WayOut {
         auto resource = [&](const void *p, unsigned size, bool used) {
             return __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(const_cast<void *>(p)) + first * size, 0, used ? values * size : 0u, 0x00020000);
         };
-        r_wide = a.res == kF32;
+        none = a.r != nullptr ? 0u : 0x80000000u;
+        r_wide = a.r == nullptr || a.res == kF32;
         r_f16 = a.res == kF16;
         y_f16 = a.type == kF16;
         y32 = resource(a.y, 4, a.type == kF32);
@@ -161,7 +163,7 @@ struct WayOut {
     __device__ __forceinline__ float value(const Residual &r, int c) const
     {
         const float half = r_f16 ? f16_of(r.half[c / 2], c % 2) : b16_of(r.half[c / 2], c % 2);
-        return r_wide ? __uint_as_float(r.wide[c]) : half;
+        return r_wide ? __uint_as_float(r.wide[c] | none) : half;
     }
     __device__ __forceinline__ void leave(int row, const float (&v)[PER]) const
     {

@@ -227,8 +227,27 @@ def test_the_same_bits_from_every_kernel():
             moe.moe_q8_linear(s, x[:n], xs[:n], offsets_of(counts), w, ws, None if plain else bias, None if plain else r[:n].contiguous(), y)
             if n == R:
                 all_y.copy_(y)
-            assert torch.equal(y, all_y[:n]), (act, n)
+            whole = torch.int32 if out == "f32" else torch.int16              # (zeros' signs too)
+            assert torch.equal(y.view(whole), all_y[:n].view(whole)), (act, n)
         assert len(names) >= 3, names
+
+
+def test_zeros_keep_their_signs_in_every_kernel():
+    """relu of negative sums without a residual, and sums of zero under a negative scale."""
+    g = gen(12)
+    R, E, N, K = 6000, 1, 1028, 1040
+    x, w = codes(g, R, K).abs(), -codes(g, E, N, K).abs()
+    x[1::2] = 0
+    xs, ws = scales(g, R), scales(g, E, N)
+    xs[1::4] *= -1
+    for act, out in (("relu", "f32"), ("identity", "f32"), ("relu", "bf16"), ("identity", "f16")):
+        got = {}
+        for n in (R, 1500, 400, 40, 3):
+            s = moe.Q8Shape.make(n, E, N, K, act=act, y=out)
+            y = torch.empty(n, N, dtype=TYPES[out], device=DEV)
+            moe.moe_q8_linear(s, x[:n], xs[:n], offsets_of([n]), w, ws, None, None, y)
+            got[moe.moe_q8_linear_kernel(s).split(" ")[0]] = y[:3].signbit().tolist()
+        assert len(got) >= 3 and all(v == got[k] for k in got for v in got.values()), (act, list(got))
 
 
 def test_no_rows_at_all():
