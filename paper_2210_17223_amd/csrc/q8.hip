@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
 // Some rows and a long depth: five stages on their way, one block to a compute unit, bound by the weights' arrival, or where tiles are fewer than
 // units by a tile's chain of stages, 0.4 to 0.5 us each.  Sums leave through LDS, so that y and r are met in whole lines of a row.
 // Measured, kernel alone: 64 rows, 32000 x 4096, fp32 out, 27 us, 5.2 TB/s; 1003 uneven rows of 5 experts, 1999 x 1008, silu, bias and an fp32
-// residual, one column a lane, 19 us (of 2000 columns, four a lane, 15.6).
+// residual, 17 us; of 2000 columns 15.6.
 template <bool PAIR, bool KTAIL, bool ONCE>
 __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
 {
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
     const WorkItem mine = items[blockIdx.x];
     if (mine.expert < 0) return;
     constexpr int TM_ = BM / 32;
-    const int l = lane_id(), wm_ = threadIdx.x / kWave & 1, wn_ = threadIdx.x / (2 * kWave);
+    const int l = lane_id(), wm_ = threadIdx.x / kWave & 1, wn_ = __builtin_amdgcn_readfirstlane(threadIdx.x / (2 * kWave));
     int source[TM_];
     float xs[TM_];
 #pragma unroll
@@ -335,8 +335,10 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
         if (row_src != nullptr) source[j] = row_src[source[j]];
         else xs[j] = a.xs[source[j]];
     }
-    // a lane's columns on the way out: four of the wavefront's 64, or one where rows are no multiples of four columns; of a pair four
-    const bool fours = PAIR || N % 4 == 0;
+    // a lane's columns on the way out: four of the wavefront's 64 (of a pair too), as far as rows begin at whole dwords and no four lie across a
+    // row's end; else one (1003 uneven rows of 5 experts, 1999 x 1008, silu, bias and an fp32 residual: one a lane everywhere 19.2 us a pass, so 16.8)
+    const bool dwords = N % 2 == 0 || (a.type == kF32 && (a.r == nullptr || a.res == kF32));
+    const bool fours = PAIR || N % 4 == 0 || (dwords && mine.n0 + wn_ * 64 + 64 <= N);
     const int col = PAIR ? l % 8 * 4 : fours ? l % 16 * 4 : l, width = PAIR ? pair_h : N;
     const int n = PAIR ? mine.n0 / 2 + wn_ * 32 + col : mine.n0 + wn_ * 64 + col;
     const float *const ws = a.ws + static_cast<size_t>(mine.expert) * N;
@@ -394,7 +396,7 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
     };
     const int left = rows - wm * 64;                      // of the wavefront's rows
     const size_t row0 = static_cast<size_t>(item.row0) + wm * 64;
-    with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto actc) {
+    auto way = [&](auto actc) {
         constexpr int ACT = decltype(actc)::value;
         if constexpr (PAIR) {
             const int at = col / 16 * 32 + col % 16;
@@ -414,7 +416,9 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
         } else {
             leave_sums(std::integral_constant<int, 1>{}, actc);
         }
-    });
+    };
+    if constexpr (PAIR) with_activation<MOE_ACT_SILU>(a.act, way);
+    else with_activation<MOE_ACT_SILU, MOE_ACT_IDENTITY>(a.act, way);
 }
 
 // ---------------------------------------------------------------- tiles of 128 x 128, a share of them for a block

@@ -103,16 +103,19 @@ enum { kForm = 8 };
 template <int ACT>
 __device__ __forceinline__ float activate(const ActForm &form, float v)
 {
+#pragma clang fp contract(off)
     if constexpr (ACT == kForm) return form(v);
-    else if constexpr (ACT == MOE_ACT_SILU) return gate_value<ACT>(__builtin_elementwise_maximum(v, -3.4e38f));
+    // (the form's steps without those that change nothing)
+    else if constexpr (ACT == MOE_ACT_SILU)
+        return __builtin_elementwise_maximum(v, -3.4e38f) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * v));
     else return gate_value<ACT>(v);
 }
-// f(integral_constant of GELU_ERF, of `plain`, or of kForm)
-template <int PLAIN, typename F>
+// f(integral_constant of GELU_ERF, of one of `plain`, or of kForm)
+template <int... PLAIN, typename F>
 __host__ __device__ __forceinline__ void with_activation(int act, F f)
 {
     if (act == MOE_ACT_GELU_ERF) f(std::integral_constant<int, MOE_ACT_GELU_ERF>{});
-    else if (act == PLAIN) f(std::integral_constant<int, PLAIN>{});
+    else if (((act == PLAIN ? (f(std::integral_constant<int, PLAIN>{}), true) : false) || ...)) return;
     else f(std::integral_constant<int, kForm>{});
 }
 __device__ __forceinline__ float sum_of(float bits) { return static_cast<float>(__builtin_bit_cast(int, bits)); }

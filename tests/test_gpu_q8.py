@@ -145,7 +145,7 @@ LINEAR = {
     "q8_stream_kernel 32x16 split": [([0, 33, 3], 68, 16), ([70, 1, 49], 65, 144)],
     "q8_stream_kernel 32x16": [([900, 0, 377], 68, 16), ([500, 1, 96, 31, 0, 300, 200, 100], 65, 48)],
     "q8_stream_kernel 32x16 once": [([33, 1, 0, 32, 9, 0, 5, 3], 4100, 2048), ([0, 87, 0, 0, 0, 0, 0, 0], 4097, 2064)],
-    "q8_tile_kernel 128x128 deep": [([700, 1, 900], 2048, 1024), ([2600], 1027, 640)],
+    "q8_tile_kernel 128x128 deep": [([700, 1, 900], 2048, 1024), ([2600], 1027, 640), ([1300, 0, 1200], 1030, 640)],
     "q8_tile_kernel 128x128 deep tail": [([2600], 1028, 656), ([800, 0, 700], 1001, 1040)],
     "q8_tile_kernel 128x128 deep once": [([100, 1, 0, 130, 20, 17, 15, 5], 2052, 4096), ([33], 16385, 4096)],
     "q8_tile_kernel 128x128 deep once tail": [([100, 1, 0, 130, 20, 17, 25, 17], 2048, 4112), ([33], 16385, 4112)],
