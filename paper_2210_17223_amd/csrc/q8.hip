@@ -619,15 +619,15 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
 }
 
 // The kernel of a product of `rows` rows of E experts, by what each would take, us: the weights' arrival, the bytes that pass through LDS, and the
-// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of every kernel over 104 products (1 to 16384 rows, 1
-// to 64 experts, 768 to 32000 columns, depths of 512 to 14336): the kernel chosen takes 1.02 times the fastest one's time on average, 1.27 at worst.
+// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of every kernel over 105 products (1 to 16384 rows, 1
+// to 64 experts, 768 to 32000 columns, depths of 512 to 14336): the kernel chosen takes 1.01 times the fastest one's time on average, 1.27 at worst.
 struct Q8Plan {
     int bm, bn;                            // tile; bm 16 or 32: the kernel for few rows
     bool deep, split;
 };
 Q8Plan plan_product(int64_t rows, int E, int columns, int K)
 {
-    const double depth = 2.0 * K, stages = (K + 63) / 64, used = static_cast<double>(std::min<int64_t>(rows, E));
+    const double depth = 2.0 * K, stages = (K + 63) / 64, used = E * (1.0 - std::pow(1.0 - 1.0 / E, static_cast<double>(rows)));
     const double weights = used * columns * depth;                      // bytes
     // tiles of bm rows: one of every expert while they are a good deal emptier than a tile, else half of one too many
     auto few = [&](int bm) { return rows * 8 <= static_cast<int64_t>(bm) * E * 3; };
@@ -647,8 +647,11 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     };
     for (int bm : {16, 32}) {
         const double groups = row_tiles(bm) * ((columns + 15) / 16), bytes = groups * (16 + bm) * depth;
-        offer(4.0 + std::max({weights / 5.8e6, bytes / 14.5e6, groups / 768 * 4.5, 0.42 / 4 * stages}), {bm, 0, false, true});
-        offer(4.0 + std::max({weights / 6.9e6, bytes / 19.5e6, groups / 768 / 4 * (2.5 + 0.7 * stages), 0.42 * stages}), {bm, 0, false, false});
+        // (few blocks of four tiles side by side: the stages of a unit that has one, two or three of them)
+        const double side = groups / 4 <= 768 ? std::ceil(groups / 4 / 256) : 0.0;
+        const double stage = bm == 16 ? std::max(0.33, 0.28 * side) : std::max(0.42, 0.39 * side);
+        offer(4.0 + std::max({weights / 6.0e6, bytes / 14.5e6, groups / 768 * 4.5, 0.42 / 4 * stages}), {bm, 0, false, true});
+        offer(4.0 + std::max({weights / 6.9e6, bytes / 19.5e6, groups / 768 / 4 * (2.5 + 0.7 * stages), stage * stages}), {bm, 0, false, false});
     }
     const double t128 = row_tiles(128) * ((columns + 127) / 128), t256 = row_tiles(256) * ((columns + 255) / 256);
     const double deep = (E == 1 || few(128) ? row_tiles(128) : static_cast<double>(rows) / 128 + E) * ((columns + 127) / 128);

@@ -140,11 +140,11 @@ def test_values_are_codes_times_scales(R, K, dtype):
 LINEAR = {
     "q8_stream_kernel 16x16 split": [([1], 64, 16), ([0, 17, 1, 31, 0], 100, 1040), ([5, 16], 37, 272), ([1], 4096, 4096), ([20], 1101, 65536)],
     "q8_stream_kernel 16x16 split once": [([0, 2, 0], 4100, 6160), ([1], 16385, 4112)],
-    "q8_stream_kernel 16x16": [([1, 0, 3, 1, 0], 256, 16), ([9], 5001, 128)],
+    "q8_stream_kernel 16x16": [([1, 0, 3, 1, 0], 260, 48), ([9], 5001, 128)],
     "q8_stream_kernel 16x16 once": [([0, 2, 0, 0, 0, 17, 0, 1], 16388, 512), ([1, 0, 0, 0, 0, 0, 0, 0], 16385, 528)],
     "q8_stream_kernel 32x16 split": [([0, 33, 3], 68, 16), ([70, 1, 49], 65, 144)],
     "q8_stream_kernel 32x16": [([900, 0, 377], 68, 16), ([500, 1, 96, 31, 0, 300, 200, 100], 65, 48)],
-    "q8_stream_kernel 32x16 once": [([33, 1, 0, 32, 9, 0, 5, 3], 4100, 2048), ([0, 87, 0, 0, 0, 0, 0, 0], 4097, 2064)],
+    "q8_stream_kernel 32x16 once": [([33, 1, 0, 32, 9, 0, 5, 7], 8196, 1024), ([0, 87, 0, 0, 0, 0, 0, 0], 8193, 1040)],
     "q8_tile_kernel 128x128 deep": [([700, 1, 900], 2048, 1024), ([2600], 1027, 640), ([1300, 0, 1200], 1030, 640)],
     "q8_tile_kernel 128x128 deep tail": [([2600], 1028, 656), ([800, 0, 700], 1001, 1040)],
     "q8_tile_kernel 128x128 deep once": [([100, 1, 0, 130, 20, 17, 15, 5], 2052, 4096), ([33], 16385, 4096)],
@@ -368,10 +368,10 @@ GATED = {
     "q8_stream_kernel 16x32 split": [([1], 256, 512), ([0, 17, 1, 12, 0], 272, 144), ([1, 0, 0], 16, 64)],
     "q8_stream_kernel 16x32 split once": [([0, 1, 0, 2, 0, 0, 1, 0], 4112, 1024)],
     "q8_stream_kernel 16x32": [([0, 2, 1], 16, 256), ([1, 0, 3, 0, 2], 640, 1040)],
-    "q8_stream_kernel 16x32 once": [([0, 2, 0, 0, 0, 1, 0, 2], 2064, 2048)],
+    "q8_stream_kernel 16x32 once": [([0, 2, 0, 0, 0, 1, 0, 2], 2064, 4096)],
     "q8_stream_kernel 32x32 split": [([20, 0, 5], 16, 64), ([32, 3], 1040, 528)],
     "q8_stream_kernel 32x32": [([200, 0, 130], 512, 384), ([500, 0, 258, 0, 0, 0, 0, 0], 16, 64)],
-    "q8_stream_kernel 32x32 once": [([33, 1, 0, 60, 40, 0, 9, 3], 4112, 1024)],
+    "q8_stream_kernel 32x32 once": [([33, 1, 0, 60, 42, 0, 9, 4], 2064, 4096)],
     "q8_tile_kernel 128x128 deep": [([700, 1, 900], 1024, 1024), ([8000, 0, 738], 640, 64)],
     "q8_tile_kernel 128x128 deep tail": [([8000, 0, 600, 0, 79], 656, 64)],
     "q8_tile_kernel 128x128 deep once": [([100, 1, 0, 130, 20, 17, 15, 6], 4224, 1024)],
@@ -433,7 +433,7 @@ def test_gated_block(name, act):
 
 @pytest.mark.parametrize("kernel,T,k,E,d,h,capacity", [
     ("q8_stream_kernel 16x32 split", 5, 2, 8, 1024, 256, 5), ("q8_stream_kernel 32x32", 700, 2, 4, 384, 272, 250),
-    ("q8_stream_kernel 16x32 once", 4, 2, 8, 2064, 2048, 4), ("q8_tile_kernel 128x128 deep tail", 2170, 4, 5, 656, 64, 2170),
+    ("q8_stream_kernel 16x32 once", 4, 2, 8, 2064, 4096, 4), ("q8_tile_kernel 128x128 deep tail", 2170, 4, 5, 656, 64, 2170),
     ("q8_tile_kernel 128x128 deep once", 289, 1, 8, 4224, 1024, 200), ("q8_gated_small_run_kernel 128x128", 1644, 2, 3, 512, 256, 1644),
     ("q8_gated_small_run_kernel 128x128 tail", 338, 3, 3, 16, 1024, 338), ("q8_gated_run_kernel 256x256 tail", 3000, 3, 5, 272, 1552, 2500),
     ("q8_gated_run_kernel 256x256", 9000, 1, 2, 1024, 1040, 9000)])
