@@ -76,17 +76,18 @@ inline int64_t tile_entries(int64_t rows, int E, int bm, int tiles)
     return static_cast<int64_t>(align_up((static_cast<size_t>(rows) / bm + std::min<int64_t>(rows, E)) * tiles, 8));
 }
 
-// All activations but the erf form of the GeLU as factor * v / (1 + 2^-(v (a + b v^2))): silu; its tanh form; relu, whose a is so large
-// that the quotient is 1 or 0 from |v| = 1e-36 on; and identity, 2 v / 2.  An epilogue that holds accumulators takes no branch, and a
+// All activations but the erf form of the GeLU as factor * max(v, lowest) / (1 + 2^-(v (a + b v^2))): silu; its tanh form; and relu and
+// identity, 2 max(v, lowest) / 2, of which nothing is rounded.  An epilogue that holds accumulators takes no branch, and a
 // kernel for each activation is five times the code.  (v^2 is bounded so that 0 v^2 is 0.)
 struct ActForm {
     float a, b, factor, lowest;
     __device__ __forceinline__ explicit ActForm(int act)
     {
-        a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : act == MOE_ACT_RELU ? 1e38f : 0.0f;
+        a = act == MOE_ACT_SILU ? 1.44269504088896341f : act == MOE_ACT_GELU_TANH ? 2.3022082f : 0.0f;
         b = act == MOE_ACT_GELU_TANH ? 0.10294324f : 0.0f;
-        factor = act == MOE_ACT_IDENTITY ? 2.0f : 1.0f;
-        lowest = act == MOE_ACT_IDENTITY ? -__builtin_inff() : -3.4e38f;
+        factor = act == MOE_ACT_IDENTITY || act == MOE_ACT_RELU ? 2.0f : 1.0f;
+        // (of -infinity silu's and the tanh form's limit is 0)
+        lowest = act == MOE_ACT_IDENTITY ? -__builtin_inff() : act == MOE_ACT_RELU ? 0.0f : -3.4e38f;
     }
     __device__ __forceinline__ float operator()(float v) const
     {
@@ -94,7 +95,6 @@ struct ActForm {
         // (the last product is rounded before a residual is added to it, in every kernel)
         const float in = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -1e30f), 1e30f);
         const float slope = __builtin_fmaf(b, __builtin_elementwise_minimum(in * in, 1e30f), a);
-        // (of -infinity the others' limit is 0)
         return __builtin_elementwise_maximum(v, lowest) * (factor * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-(in * slope))));
     }
 };

@@ -308,6 +308,39 @@ def test_activations_of_infinities(name, act):
     assert bool((y[v < 0] == -math.inf).all()) if act == "identity" else bool((y[v < 0].abs() < 1e-6).all())
 
 
+@pytest.mark.parametrize("name", ["q8_stream_kernel 16x16 split 0", "q8_stream_kernel 32x16 0", "q8_tile_kernel 128x128 deep 1",
+                                  "q8_small_run_kernel 128x128 tail 2", "q8_run_kernel 256x256 1"])
+def test_relu_of_the_smallest_sums(name):
+    """relu rounds nothing, down to fp32's smallest normal numbers: the sum itself, or 0."""
+    c = linear_case(name)
+    for size in (2.0 ** -100, 2.0 ** -118, 2.0 ** -126):         # (powers of two: a sum times its scales is a normal number, not rounded again)
+        y = torch.empty(c["R"], c["N"], device=DEV)
+        moe.moe_q8_linear(moe.Q8Shape.make(c["R"], c["E"], c["N"], c["K"], act="relu", y="f32"), c["x"], torch.full_like(c["xs"], size),
+                          c["offsets"], c["w"], torch.ones_like(c["ws"]), None, None, y)
+        assert torch.equal(y, sums(c["x"], c["w"], c["offsets"]).float().clamp(min=0) * size)
+
+
+def test_a_gate_of_the_smallest_values_is_open_or_closed():
+    """relu(G) U with gates of +-2^-126 and values of 2^120 n: 0, or n / 64."""
+    g = gen(13)
+    T, d, h = 33, 64, 64
+    x = torch.zeros(T, d, dtype=torch.int8, device=DEV)
+    x[:, 0] = 1
+    w = torch.zeros(1, 2 * h, d, dtype=torch.int8, device=DEV)
+    w[0, :, 0] = codes(g, 2 * h)
+    w[0, :h, 0] = torch.where(w[0, :h, 0] > 0, 1, -1)
+    ws = torch.full((1, 2 * h), 2.0 ** -126, device=DEV)
+    ws[:, h:] = 2.0 ** 120
+    eye = torch.eye(d, h, dtype=torch.int8, device=DEV)[None] * 64
+    s = moe.Shape.make(T, d, 1, h, 1, T, act="relu")
+    ye, wsp = torch.empty(T, d, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q8(s, x, torch.ones(T, device=DEV), None, offsets_of([T]), w, ws, eye.contiguous(), torch.full((1, d), 1 / 64, device=DEV), ye, wsp)
+    H = (w[0, :h, 0].double().clamp(min=0) * 2.0 ** -126 * w[0, h:, 0].double() * 2.0 ** 120).half()
+    q, scale = held(H[None].expand(T, h))
+    # (the second product: a code times 64, and two scales)
+    assert torch.equal(ye, ((q.double() * 64).float() * scale[:, None] * (1 / 64)).half())
+
+
 @pytest.mark.parametrize("T,d,h", [(3, 64, 64), (300, 512, 256), (9000, 512, 256)])
 def test_gates_of_minus_infinity_are_closed(T, d, h):
     g = gen(T)
