@@ -278,10 +278,12 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args a)
         }
         const size_t at = static_cast<size_t>(item.row0 + row);
         const ActForm form(a.act);
-        with_activation<PAIR ? MOE_ACT_SILU : MOE_ACT_IDENTITY>(a.act, [&](auto act) {
+        auto activated = [&](auto act) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) v[0][c] = activate<decltype(act)::value>(form, v[0][c]) * (PAIR ? v[NT - 1][c] : 1.0f);
-        });
+        };
+        if constexpr (PAIR) with_activation<MOE_ACT_GELU_ERF, MOE_ACT_SILU>(a.act, activated);
+        else with_activation<MOE_ACT_GELU_ERF, kGeluErf32, MOE_ACT_IDENTITY>(a.act, activated);
         if constexpr (PAIR) {
             store_hidden(a, at, n, v[0]);
         } else if (a.N % 4 == 0) {
@@ -417,8 +419,8 @@ __global__ __launch_bounds__(256, 1) void q8_tile_kernel(Q8Args a)
             leave_sums(std::integral_constant<int, 1>{}, actc);
         }
     };
-    if constexpr (PAIR) with_activation<MOE_ACT_SILU>(a.act, way);
-    else with_activation<MOE_ACT_SILU, MOE_ACT_IDENTITY>(a.act, way);
+    if constexpr (PAIR) with_activation<MOE_ACT_GELU_ERF, MOE_ACT_SILU>(a.act, way);
+    else with_activation<MOE_ACT_GELU_ERF, kGeluErf32, MOE_ACT_SILU, MOE_ACT_IDENTITY>(a.act, way);
 }
 
 // ---------------------------------------------------------------- tiles of 128 x 128, a share of them for a block
@@ -481,7 +483,7 @@ __global__ __launch_bounds__(256, 2) void q8_small_run_kernel(Q8Args a)
                 else if constexpr (j + 1 < TM) ask(j + 1);
                 lds_handover();
                 MOE_SB();
-                with_activation<MOE_ACT_IDENTITY>(a.act, [&](auto act) {
+                with_activation<MOE_ACT_GELU_ERF, kGeluErf32, MOE_ACT_IDENTITY>(a.act, [&](auto act) {
 #pragma unroll
                     for (int it = 0; it < 16 / ROWS; ++it) {
                         const int row = it * ROWS + in;
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
             static_for<TM>([&](auto jc) {
                 constexpr int j = decltype(jc)::value;
                 lds_handover();
-                with_activation<MOE_ACT_SILU>(a.act, [&](auto act) {
+                with_activation<MOE_ACT_GELU_ERF, MOE_ACT_SILU>(a.act, [&](auto act) {
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         f16x4 o;
@@ -869,7 +871,7 @@ moe_status moe_q8_linear(const moe_q8_shape *s, const void *x, const float *x_sc
     a.E = s->E;
     a.N = s->N;
     a.K = s->K / 2;
-    a.act = s->act;
+    a.act = activation_of(s->act, s->y == kF32);
     a.res = s->res;
     a.type = s->y;
     launch_product<false>(a, s->R, -1, static_cast<hipStream_t>(stream));

@@ -15,9 +15,13 @@ struct Q8Args {
     int row_div, a_rows;
     int E, N, K;                           // of a pair of projections N = 2 h
     int h;                                 // else 0
-    int act, res, type;
+    int act, res, type;                    // act: a moe_act, of a linear map as activation_of has it
     int tiles, entries, share;
 };
+
+// The erf form of the GeLU under an fp32 output is an activation of its own.
+enum { kGeluErf32 = 8 };
+inline int activation_of(int act, bool y32) { return act == MOE_ACT_GELU_ERF && y32 ? kGeluErf32 : act; }
 
 // q8_run.hip: tiles of 256 x 256; pair: the first projections, else the linear map, N a multiple of 4.
 // whole: the depth is taken in whole stages of 64, four at least.

@@ -218,18 +218,19 @@ void launch_q8_run(bool pair, const Q8Args &args, int64_t entries, bool whole, i
     auto with_tail = [&](auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
         if (pair) {
-            with_activation<MOE_ACT_SILU>(a.act, [&](auto act) {
+            with_activation<MOE_ACT_GELU_ERF, MOE_ACT_SILU>(a.act, [&](auto act) {
                 launch_product_kernel<q8_gated_run_kernel<decltype(act)::value, TAIL>>(a, blocks, kW4RunLds, stage, st);
             });
             return;
         }
-        with_activation<MOE_ACT_IDENTITY>(a.act, [&](auto actc) {
+        auto launch = [&](auto y32, auto actc) {
+            constexpr bool Y32 = decltype(y32)::value;
             constexpr int ACT = decltype(actc)::value;
-            if (a.type == kF32 && a.r != nullptr) launch_product_kernel<q8_run_kernel<ACT, true, true, TAIL>>(a, blocks, kW4RunLds, stage, st);
-            else if (a.type == kF32) launch_product_kernel<q8_run_kernel<ACT, true, false, TAIL>>(a, blocks, kW4RunLds, stage, st);
-            else if (a.r != nullptr) launch_product_kernel<q8_run_kernel<ACT, false, true, TAIL>>(a, blocks, kW4RunLds, stage, st);
-            else launch_product_kernel<q8_run_kernel<ACT, false, false, TAIL>>(a, blocks, kW4RunLds, stage, st);
-        });
+            if (a.r != nullptr) launch_product_kernel<q8_run_kernel<ACT, Y32, true, TAIL>>(a, blocks, kW4RunLds, stage, st);
+            else launch_product_kernel<q8_run_kernel<ACT, Y32, false, TAIL>>(a, blocks, kW4RunLds, stage, st);
+        };
+        if (a.type == kF32) with_activation<kGeluErf32, MOE_ACT_IDENTITY>(a.act, [&](auto act) { launch(std::true_type{}, act); });
+        else with_activation<MOE_ACT_GELU_ERF, MOE_ACT_IDENTITY>(a.act, [&](auto act) { launch(std::false_type{}, act); });
     };
     if (whole) with_tail(std::false_type{});
     else with_tail(std::true_type{});

@@ -341,6 +341,82 @@ def test_a_gate_of_the_smallest_values_is_open_or_closed():
     assert torch.equal(ye, ((q.double() * 64).float() * scale[:, None] * (1 / 64)).half())
 
 
+def gelu_room(v, want, wide):
+    """How far the erf form may be off before a 16-bit output's rounding, as moe_q8.h says: fp32 outputs (wide) by the roundings of t, R, the
+    products and the exponent; 16-bit ones by their polynomial, with 2^-23 for its product and sum."""
+    if wide:
+        return (14 + 1.5 * v * v) * 2.0 ** -24 * want.abs() + 2.0 ** -120
+    return torch.where(v.abs() <= 2, 2.0 ** -17.8, 2.0 ** -13.5) * want.abs() + 2.0 ** -23 * want.abs() + 1e-16
+
+
+@pytest.mark.parametrize("name", ["q8_stream_kernel 16x16 split 1", "q8_stream_kernel 32x16 1", "q8_tile_kernel 128x128 deep 1",
+                                  "q8_small_run_kernel 128x128 tail 2", "q8_run_kernel 256x256 1"])
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_erf_gelu_is_as_good_as_its_output(name, out):
+    """Of sums that scales of powers of two leave exact, from -13 to 13 and close about 0, where it is small itself: within its own error, and half
+    a step of a 16-bit output (fp16's are 2^-24 apart below 2^-14)."""
+    c = linear_case(name)
+    total = sums(c["x"], c["w"], c["offsets"])
+    for spread in (3.0, 0.05):
+        scale = 2.0 ** round(math.log2(spread / (73 * 73 * math.sqrt(c["K"]))))
+        v = total * scale
+        assert float(total.abs().max()) < 2 ** 24 and float(v.min()) < -3 * spread
+        y = torch.empty(c["R"], c["N"], dtype=TYPES[out], device=DEV)
+        moe.moe_q8_linear(moe.Q8Shape.make(c["R"], c["E"], c["N"], c["K"], act="gelu", y=out), c["x"], torch.full_like(c["xs"], scale),
+                          c["offsets"], c["w"], torch.ones_like(c["ws"]), None, None, y)
+        want = v * torch.erfc(-v * math.sqrt(0.5)) / 2        # (torch's ndtr is 1 + erf, and has no digits left below -8)
+        room = gelu_room(v, want, out == "f32")
+        if out != "f32":
+            room = room + EPS[out] * (want.abs() + room) + (2.0 ** -25 if out == "f16" else 2.0 ** -120)
+        over = (y.double() - want).abs() - room
+        assert float(over.max()) <= 0, (spread, float(over.max()), float(v[over > 0][0]), int((over > 0).sum()))
+
+
+@pytest.mark.parametrize("name", ["q8_stream_kernel 16x16 split 1", "q8_tile_kernel 128x128 deep 1", "q8_run_kernel 256x256 1"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_smooth_activations_are_as_good_as_said(name, act):
+    """v / (1 + 2^e): the exponent's roundings (a product and its constant; of the tanh form four), ln 2 each times |e|, and six others."""
+    c = linear_case(name)
+    total = sums(c["x"], c["w"], c["offsets"])
+    for spread in (20.0, 0.05):
+        scale = 2.0 ** round(math.log2(spread / (73 * 73 * math.sqrt(c["K"]))))
+        v = total * scale
+        y = torch.empty(c["R"], c["N"], device=DEV)
+        moe.moe_q8_linear(moe.Q8Shape.make(c["R"], c["E"], c["N"], c["K"], act=act, y="f32"), c["x"], torch.full_like(c["xs"], scale),
+                          c["offsets"], c["w"], torch.ones_like(c["ws"]), None, None, y)
+        e = -v / math.log(2) * (1 if act == "silu" else 2 * math.sqrt(2 / math.pi) * (1 + 0.044715 * v * v))
+        want = v / (1 + torch.exp2(e))
+        room = (8 + 3 * e.abs()) * 2.0 ** -24 * want.abs() + 2.0 ** -110
+        assert bool(((y.double() - want).abs() <= room).all()), spread
+
+
+@pytest.mark.parametrize("T", [3, 700, 9000])
+def test_hidden_rows_of_far_gates_by_erf_gelu(T):
+    """Gates of -5.5 .. -4.5, whose GeLU is 1e-5 to 1e-7, under values of 2^16: H within 2^-13.4 + 2^-11 of itself, its row's largest too, so no code is
+    off by more than one step (127 times twice that is 0.16); the output once more rounded to fp16."""
+    g = gen(T)
+    d, h = 64, 1024
+    x = torch.zeros(T, d, dtype=torch.int8, device=DEV)
+    x[:, 0] = 1
+    w = torch.zeros(1, 2 * h, d, dtype=torch.int8, device=DEV)
+    w[0, :h, 0] = torch.randint(-88, -71, (h,), generator=g, device=DEV, dtype=torch.int8)
+    w[0, h:, 0] = torch.randint(64, 128, (h,), generator=g, device=DEV, dtype=torch.int8)
+    ws = torch.full((1, 2 * h), 1 / 16, device=DEV)
+    ws[:, h:] = 2.0 ** 10
+    take = torch.zeros(1, d, h, dtype=torch.int8, device=DEV)
+    at = torch.randperm(h, generator=g, device=DEV)[:d]
+    at[0] = (act64(w[0, :h, 0].double() / 16, "gelu") * w[0, h:, 0].double()).abs().argmax()
+    take[0, torch.arange(d, device=DEV), at] = 64
+    s = moe.Shape.make(T, d, 1, h, 1, T, act="gelu")
+    ye, wsp = torch.empty(T, d, dtype=torch.float16, device=DEV), torch.empty(moe.moe_gated_q8_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    moe.moe_gated_ffn_q8(s, x, torch.ones(T, device=DEV), None, offsets_of([T]), w, ws, take, torch.full((1, d), 1 / 64, device=DEV), ye, wsp)
+    H = act64(w[0, :h, 0].double() / 16, "gelu") * w[0, h:, 0].double() * 2.0 ** 10
+    most, want = float(H.abs().max()), H[at].expand(T, d)
+    off = (ye.double() - want).abs()
+    assert float(off[:, 0].max()) <= (2.0 ** -13.4 + 2.0 ** -11 + 2.0 ** -11) * most
+    assert bool((off <= (1.5 + 0.16) * most / 127 + 2.0 ** -11 * want.abs()).all())
+
+
 @pytest.mark.parametrize("T,d,h", [(3, 64, 64), (300, 512, 256), (9000, 512, 256)])
 def test_gates_of_minus_infinity_are_closed(T, d, h):
     g = gen(T)
