@@ -35,7 +35,8 @@ extern "C" {
  * themselves, not those of an approximation.  For weights: R = E N. */
 moe_status moe_q8_rows(int64_t R, int32_t K, int32_t type, const void *x, void *q, float *scale, void *stream);
 
-/* The values that codes stand for, rounded once to `type`; K as above. */
+/* The values that codes stand for: the fp32 products code * scale, of which 16-bit types are rounded from (so twice in all: where the first
+ * rounding meets a border of two values, one of 2^14 in fp16, the one that is farther by 2^-24 may be taken); K as above. */
 moe_status moe_q8_values(int64_t R, int32_t K, int32_t type, const void *q, const float *scale, void *x, void *stream);
 
 /* moe_norm_before and moe_norm_after (moe_norm.h) with next also, or (next NULL) only, in 8 bits: q [T, d], scale [T], of

@@ -135,6 +135,18 @@ def test_values_are_codes_times_scales(R, K, dtype):
     assert torch.equal(x, (q.float() * s[:, None]).to(TYPES[dtype]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_values_in_16_bits_are_roundings_of_the_fp32_product(dtype):
+    """Against 64 bits: half a step of the type and half one of fp32."""
+    g = gen(21)
+    q, s = codes(g, 4096, 256), scales(g, 4096, of=0.002)
+    x = torch.empty(4096, 256, dtype=TYPES[dtype], device=DEV)
+    moe.moe_q8_values(q, s, x)
+    want = q.double() * s.double()[:, None]
+    assert bool(((x.double() - want).abs() <= (EPS[dtype] + 2.0 ** -24) * want.abs() + (2.0 ** -25 if dtype == "f16" else 0)).all())
+    assert torch.equal(x, (q.float() * s[:, None]).to(TYPES[dtype]))
+
+
 # ---------------------------------------------------------------------------- linear map
 # every kernel and form: (rows by expert, N, K)
 LINEAR = {
