@@ -72,9 +72,9 @@ moe_status moe_q8_linear(const moe_q8_shape *s, const void *x, const float *x_sc
 
 /* Which kernel moe_q8_linear launches for the shape, and moe_gated_ffn_q8 for its product `which` (0: first projections; 1: second), written
  * to name (host, len bytes, always terminated) as "<kernel> <tile rows>x<tile columns>", with " split" behind it where a block shares out
- * a tile's depth, " deep" where five stages of loads are on their way, " once" where the weights go past the caches and " tail" where the
- * depth is not taken in whole stages of 128, so that a measurement or a test can say which kernel it ran.  MOE_EINVAL for a null name,
- * len == 0 or another which; else as the call that launches it. */
+ * a tile's depth, " deep" where five stages of loads are on their way, " once" where the weights go past the caches and " tail" for the form of a
+ * kernel of tiles that takes depths of no whole stages of 128, and, of those without " deep", of fewer than four; so that a measurement or a
+ * test can say which kernel it ran.  MOE_EINVAL for a null name, len == 0 or another which; else as the call that launches it. */
 moe_status moe_q8_linear_kernel(const moe_q8_shape *s, char *name, size_t len);
 moe_status moe_gated_q8_kernel(const moe_shape *s, int32_t which, char *name, size_t len);
 

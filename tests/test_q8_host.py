@@ -162,3 +162,11 @@ def test_kernel_names():
         assert L.moe_gated_q8_kernel(C.byref(s), which, buf, 8) == 1
     with pytest.raises(moe.MoeError):
         name(moe.Q8Shape.make(1, 1, 64, 72))
+
+
+def test_tails_in_kernel_names():
+    """Depths of no whole stages of 128, and below four of them where loads run on from tile to tile; kernels for few rows have no such form."""
+    linear = lambda R, N, K: moe.moe_q8_linear_kernel(moe.Q8Shape.make(R, 1, N, K))  # noqa: E731
+    assert [linear(9000, 4096, K) for K in (256, 384, 512, 528)] == [f"q8_run_kernel 256x256{t}" for t in (" tail", " tail", "", " tail")]
+    assert [linear(2600, 1028, K) for K in (640, 656)] == [f"q8_tile_kernel 128x128 deep{t}" for t in ("", " tail")]
+    assert not linear(1, 4096, 1040).endswith("tail")
