@@ -716,6 +716,32 @@ def test_a_step_of_them_together():
     assert torch.equal(outs > 0, torch.ones_like(outs, dtype=torch.bool))
 
 
+def test_a_steps_norms_against_64_bits():
+    """The step's first codes, its residual stream and its last codes.  next and hats as the norms' test bounds them (2^-18 (1 + |hat|) |w|); a code
+    stands for its value within half a step, and what that value is off."""
+    t = Step()
+    nx, q, qs, y, z, r, out, outs = t.run()
+
+    def hat(v):
+        v = v.double()
+        return v * torch.rsqrt(v.square().mean(1, keepdim=True) + 1e-5)
+
+    def holds(codes, scale, want, room):
+        scale = scale.double()[:, None]
+        assert int(codes.abs().max(1).values.min()) == 127
+        assert bool(((codes.double() * scale - want).abs() <= (0.5 + 2.0 ** -20) * scale + room).all())
+
+    hx = hat(t.x)
+    want, room = hx * t.w0, 2.0 ** -18 * (1 + hx.abs()) * t.w0.abs() + 2.0 ** -22
+    assert bool(((nx.double() - want).abs() <= room + EPS["bf16"] * (want.abs() + room)).all())
+    holds(q, qs, want, room)
+    hz = hat(z)
+    want = t.x.double() + t.n.scale * hz * t.w1
+    assert bool(((r.double() - want).abs() <= 2.0 ** -18 * (1 + hz.abs()) * t.w1.abs() + 2.0 ** -23 * (t.x.abs() + want.abs()) + 2.0 ** -22).all())
+    hr = hat(r)
+    holds(out, outs, hr * t.w0, 2.0 ** -18 * (1 + hr.abs()) * t.w0.abs() + 2.0 ** -22)
+
+
 def test_steps_captured_and_replayed_beside_eager_ones():
     """Two graphs with buffers of their own, replayed in turn with the eager step and other streams' work between."""
     a, b = Step(seed=1), Step(T=200, seed=2)
