@@ -163,7 +163,9 @@ constexpr int row_vec(int res, int z) { return res == kB16 && z != kF32 ? 8 : 4;
 
 // Forward.  Columns of thread t: (v TPR + t) VEC .. + VEC - 1.  Q8: next leaves in 8 bits too, or only so; and what is read or written
 // once goes past the caches, where the codes then stay for the product that reads them (32768 rows of 2048, fp32 x, fp16 z, 0.87 GB: 168 us,
-// 5.2 TB/s, instead of 188).
+// 5.2 TB/s, instead of 188).  Codes alone, TB/s, RMS, behind a block with fp32 x and fp16 z / with bf16 x and z / in front of the first one with
+// fp32 x, 64 M values: d = 2048 5.4 / 4.6 / 5.1, 4096 5.7 / 4.3 / 4.9, 8192 5.6 / 3.8 / 4.7, 12288 2.4 / 2.5 / 4.9, 16384 2.8 / 2.8 / 5.3: past 8192 the
+// kernels behind a block spill 38 to 93 registers, those in front none.
 template <int RES, int Z, int TPR, int EPT, bool Q8>
 __device__ __forceinline__ void norm_forward(const NormArgs &a)
 {

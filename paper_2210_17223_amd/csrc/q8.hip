@@ -575,7 +575,8 @@ __global__ __launch_bounds__(256, 2) void q8_gated_small_run_kernel(Q8Args a)
 }
 
 // ---------------------------------------------------------------- dispatch
-// codes and scales of the tokens to their slots; a wavefront owns a token, whose codes are read once however many slots it has.  Bound by memory.
+// codes and scales of the tokens to their slots; a wavefront owns a token, whose codes are read once however many slots it has.  Bound by memory:
+// 32768 tokens of 2048 to two of 32 experts each, 0.2 GB, take the dispatch from 10.1 to 41.4 us, 6.4 TB/s; 64 of 4096 from 9.6 to 12.9, a launch.
 __global__ __launch_bounds__(256) void q8_scatter_kernel(const u32x4 *__restrict__ x, const float *__restrict__ xs,
                                                          const int32_t *__restrict__ slot_of, u32x4 *__restrict__ xe,
                                                          float *__restrict__ xes, int T, int k, int vec, int max_rows)
@@ -621,8 +622,11 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
 }
 
 // The kernel of a product of `rows` rows of E experts, by what each would take, us: the weights' arrival, the bytes that pass through LDS, and the
-// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of every kernel over 105 products (1 to 16384 rows, 1
-// to 64 experts, 768 to 32000 columns, depths of 512 to 14336): the kernel chosen takes 1.01 times the fastest one's time on average, 1.27 at worst.
+// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of the kernels over 112 products (1 to 16384 rows, 1
+// to 64 experts, 768 to 32000 columns, depths of 512 to 14336; profiles/eight_bit_product_kernels_sweep.txt): the kernel chosen takes 1.024 times the
+// fastest one's time on average and more than 1.1 times in six.  The worst are 1.45 and 1.47, where uneven experts of some 96 rows get tiles of
+// 256 x 256: one row tile is counted for each, 256 tiles in a round, and an expert of more than 256 rows makes it two (1536 rows of 16 experts,
+// 768 to 4096 columns, 38.1 us, in 128 x 128 26.3).
 struct Q8Plan {
     int bm, bn;                            // tile; bm 16 or 32: the kernel for few rows
     bool deep, split;
@@ -663,8 +667,10 @@ Q8Plan plan_product(int64_t rows, int E, int columns, int K)
     return best;
 }
 
-// How a product is launched.  once: weights that one tile of rows reads, and more of them than stay in the last level of cache until
-// the next call (64 MiB; a matrix of 25 MB, passed by, takes 8.2 us where it took 8.0 of what the cache kept, of 940 MB 150 where it took 168).
+// How a product is launched.  once: weights that one tile of rows reads, and more of them (of all experts, whichever have rows) than 64 MiB, a quarter of
+// the last level of cache, go past the caches.  us kept / past, with 1.2 GB of other weights between two calls and, in brackets, of the same
+// weights again: 1 row, 34 MB 10.1 / 9.2 (6.5 / 6.7), 67 MB 15.1 / 13.3 (12.6 / 11.7), 134 MB 27.3 / 24.6 (21.0 / 21.7); 64 rows, 50 MB 24.3 / 23.3
+// (19.8 / 21.8), 67 MB 25.9 / 23.9 (20.4 / 22.8), 134 MB 31.5 / 28.0 (26.4 / 27.1).  So below the line what a program's next call may find again stays.
 constexpr int64_t kKeptBytes = 64 << 20, kMostTiles = 1 << 23;
 struct Q8Launch {
     Q8Plan plan;
