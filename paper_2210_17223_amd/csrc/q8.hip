@@ -943,8 +943,10 @@ moe_status moe_dispatch_q8(const moe_shape *s, const void *x, const float *x_sca
     prof_end(kStagePlan, st);
     if (plan != MOE_OK) return plan;
     if (xe != nullptr) {
+        prof_begin(kStageScatter, st);
         hipLaunchKernelGGL(q8_scatter_kernel, dim3(std::min(parts_of(s->T, 4), 1 << 20)), dim3(256), 0, st, static_cast<const u32x4 *>(x), x_scale, slot_of,
                            static_cast<u32x4 *>(xe), xe_scale, s->T, s->k, s->d_model / 16, static_cast<int>(moe_max_rows(s)));
+        prof_end(kStageScatter, st);
         MOE_TRY_HIP(hipGetLastError());
     }
     return MOE_OK;

@@ -184,3 +184,27 @@ def test_a_dispatch_over_64_experts():
     assert torch.equal(plans[0]["src_of"][:A], plans[1]["src_of"][:A])
     token = plans[0]["src_of"][:A].long() // k
     assert torch.equal(xe[:A], x[token]) and torch.equal(xes[:A], xs[token])
+
+
+def test_stages_of_the_8_bit_calls_are_timed():
+    """moe_profile_enable's stages: the dispatch's plan and, where rows move, their copies; the block's two products."""
+    g = gen(5)
+    T, d, E, h, k = 256, 64, 4, 48, 2
+    s = moe.Shape.make(T, d, E, h, k, T, act="silu")
+    rows = moe.moe_max_rows(s)
+    x, xs = codes(g, T, d), scales(g, T)
+    idx = torch.rand(T, E, generator=g, device=DEV).argsort(1)[:, :k].contiguous().int().view(-1)
+    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=DEV)  # noqa: E731
+    plan = [i32(E), i32(E + 1), i32(T * k), i32(rows)]
+    xe, xes = torch.empty(rows, d, dtype=torch.int8, device=DEV), torch.empty(rows, device=DEV)
+    ws, gws = (torch.empty(n, dtype=torch.uint8, device=DEV) for n in (moe.moe_workspace_bytes(s, 1), moe.moe_gated_q8_workspace_bytes(s)))
+    q13, q2, ye = codes(g, E, 2 * h, d), codes(g, E, d, h), torch.empty(rows, d, dtype=torch.float16, device=DEV)
+    moe.moe_profile_enable((1 << 12) - 1, 64)
+    try:
+        moe.moe_dispatch_q8(s, x, xs, idx, *plan, None, None, ws)
+        moe.moe_dispatch_q8(s, x, xs, idx, *plan, xe, xes, ws)
+        moe.moe_gated_ffn_q8(s, xe, xes, None, plan[1], q13, scales(g, E, 2 * h), q2, scales(g, E, d), ye, gws)
+        torch.cuda.synchronize()
+        assert [len(moe.moe_profile_read(stage)) for stage in (1, 3, 4, 5)] == [2, 1, 1, 1]
+    finally:
+        moe.moe_profile_enable(0, 0)
