@@ -208,3 +208,23 @@ def test_stages_of_the_8_bit_calls_are_timed():
         assert [len(moe.moe_profile_read(stage)) for stage in (1, 3, 4, 5)] == [2, 1, 1, 1]
     finally:
         moe.moe_profile_enable(0, 0)
+
+
+@pytest.mark.parametrize("counts,kernel", [([1, 2], "q8_stream_kernel 16x16"), ([24, 40], "q8_tile_kernel"), ([70, 50], "q8_small_run_kernel"), ([300, 220], "q8_run_kernel")])
+def test_weights_past_32_bit_offsets(counts, kernel):
+    """Two matrices of 4.3 GB each: the second one's last columns, and some between."""
+    N, K, E = (1 << 18) + 260, 16384, 2
+    g, R = gen(8), sum(counts)
+    assert moe.moe_q8_linear_kernel(moe.Q8Shape.make(R, E, N, K)).startswith(kernel)
+    x, xs, ws = codes(g, R, K), scales(g, R, of=1 / 73), scales(g, E, N, of=1 / (73 * 128))
+    w = torch.zeros(E, N, K, dtype=torch.int8, device=DEV)
+    at = torch.tensor([0, 1, 131071, 131072, N // 2, N - 257, N - 256, N - 2, N - 1], device=DEV)
+    some = codes(g, E, len(at), K)
+    w[:, at] = some
+    y = torch.full((R, N), 7.0, device=DEV)
+    offsets = offsets_of(counts)
+    moe.moe_q8_linear(moe.Q8Shape.make(R, E, N, K, y="f32"), x, xs, offsets, w, ws, None, None, y)
+    e = expert_of(offsets, R)
+    assert torch.equal(y[:, at], sums(x, some, offsets).float() * xs[:, None] * ws[e][:, at])
+    y[:, at] = 0
+    assert not bool(y.any())
