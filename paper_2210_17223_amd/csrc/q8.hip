@@ -622,7 +622,7 @@ void launch_rows(int64_t R, int K, int type, const void *x, void *q, float *scal
 }
 
 // The kernel of a product of `rows` rows of E experts, by what each would take, us: the weights' arrival, the bytes that pass through LDS, and the
-// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of the kernels over 112 products (1 to 16384 rows, 1
+// rounds of tiles with their stages, whichever is longest.  The numbers are fitted to sweeps of the kernels over 111 products (1 to 16384 rows, 1
 // to 64 experts, 768 to 32000 columns, depths of 512 to 14336; profiles/eight_bit_product_kernels_sweep.txt): the kernel chosen takes 1.024 times the
 // fastest one's time on average and more than 1.1 times in six.  The worst are 1.45 and 1.47, where uneven experts of some 96 rows get tiles of
 // 256 x 256: one row tile is counted for each, 256 tiles in a round, and an expert of more than 256 rows makes it two (1536 rows of 16 experts,
