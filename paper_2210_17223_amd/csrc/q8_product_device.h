@@ -122,7 +122,7 @@ __device__ __forceinline__ float gelu_erf_32(float v)
     return __builtin_fmaf(-a, r * t * __builtin_amdgcn_exp2f(a * a * -0.72134752f), __builtin_elementwise_maximum(v, 0.0f));
 }
 // Phi(-a) = 2^P(a), P a polynomial of degree 7 with P(0) = -1, minimax of the error over the smaller of 2^-14 of a Phi(-a) and 2e-7 on [0, 8], and
-// falling on from there: 2^-17.8 of the result's size for |v| <= 2, 2^-13.5 down to -8 (an eighth of fp16's half step), and below
+// falling on from there: 2^-17.8 of the result's size for |v| <= 2, 2^-13.5 down to -8 (a third of fp16's half step at most), and below
 // that, where the result is under 5e-15, within 1e-16.
 __device__ __forceinline__ float gelu_erf_16(float v)
 {
